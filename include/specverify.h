@@ -14,6 +14,10 @@
  *   ss_spec_accept       accept/reject walk over the k drafts and the draw of
  *                        the one new token (residual or bonus distribution)
  *
+ * In front of them, what fills the cache: ss_block_map (block tables and slot maps from the
+ * requests' lengths), ss_kv_write (a chunk's keys and values by slot) and ss_chunk_attn
+ * (attention of a chunk of new tokens, of any length, over the cache).
+ *
  * Around them, the other steps of a decode loop: ss_kv_append (write the new
  * tokens' K/V before verification), ss_kv_commit (valid lengths after
  * acceptance), for tree-shaped drafts ss_batch.tree_mask,
@@ -334,6 +338,87 @@ int32_t ss_kv_commit(int32_t batch, const int32_t *q_indptr, const int32_t *acce
                      void *stream);
 
 /*
+ * Filling the cache (paper Sections 2.4 and 3.4: a request's prefill puts the keys and values of its prompt into the
+ * paged cache that decoding then appends to).  A step takes a chunk of new tokens of every request, from none to whole
+ * prompts, single tokens of decoding requests among them:
+ *     ss_block_map      once a step: blocks for the new tokens, and where each goes
+ *     ss_kv_write       once a layer: their keys and values
+ *     ss_chunk_attn     once a layer: their attention
+ * In these three calls a request may have any number of new tokens, none included, q_indptr[batch] may be smaller than
+ * total_rows (rows behind the last request's belong to no one), and ss_batch.max_q_len is an upper bound of any size
+ * (0 = unknown).  SS_BATCH_REUSE_PLAN has no effect, and tree_mask must be NULL where the batch is read.
+ */
+
+/*
+ * The free blocks of a cache.
+ *   num_blocks  blocks of the cache, and entries of free_ids (below 2^27)
+ *   free_ids    device int32 [num_blocks]: ids of the blocks no request holds, in the first *free_count entries
+ *   free_count  device int32 [1]
+ */
+typedef struct ss_block_pool {
+    int32_t num_blocks;
+    int32_t *free_ids;
+    int32_t *free_count;
+} ss_block_pool;
+
+/*
+ * Block tables and slot maps from the requests' lengths.  Request b is to hold ceil(kv_len[b]/16) blocks after the call, kv_len
+ * counting the step's new tokens as elsewhere; it holds held[b] before (the first held[b] entries of its row of the table).
+ *     held < needed: it takes blocks (a request that comes, held 0; one that grows);
+ *     held > needed: it gives the last ones back (rejected drafts; a request that has ended, kv_len 0 and no rows).
+ * First the returned blocks are put on top of the free list, in the order of (request, logical block); then blocks are taken
+ * from its top, in the same order.  So a block can pass from one request to another within a call, and equal arguments give equal tables.
+ *   batch       block_table (WRITTEN through, although the struct declares it const): entries held .. needed-1 of a row that grows
+ *               are set; all others keep what they hold.  kv_len, q_indptr: as above, q_indptr[0] = 0.
+ *   held        device int32 [batch], updated to ceil(kv_len/16)
+ *   slot_map    device int32 [total_rows]: block * 16 + place of each new token; -1 for rows behind the last request's
+ *   positions   device int32 [total_rows] or NULL: the cache position of each new token (what a rotary embedding takes); -1 as above
+ *   status      device int32 [1]: 0, or why nothing was done: s > 0: s blocks are missing; s < 0: request -1-s has impossible
+ *               lengths (kv_len below its rows, rows outside [0, total_rows], more blocks than the table has columns), s = -1-batch:
+ *               the free list's length has.  Then table, held and free list are as they were and every slot is -1, so that
+ *               ss_kv_write writes nothing.
+ *   workspace   device, >= ss_block_map_workspace(batch) bytes, 256-byte aligned; contents are scratch
+ * One call at a time for one pool; a block belongs to one request only (shared prefixes are the caller's).
+ */
+size_t ss_block_map_workspace(int32_t batch);
+int32_t ss_block_map(const ss_batch *batch, const ss_block_pool *pool, int32_t *held, int32_t total_rows, int32_t *slot_map,
+                     int32_t *positions, int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The write of new keys and values by slot: row r goes to place slot_map[r] % 16 of block slot_map[r] / 16, for every KV head.
+ * Rows whose slot is negative or outside the cache are left out.  Values are stored as by ss_kv_append: SS_F32 the value, SS_BF16
+ * nearest, ties to even, SS_FP8_E4M3 nearest e4m3fn of clamp(x / scale, +-448), the scale of a block whose place 0 is written by the
+ * call being amax / 448 (1.0 if amax is 0) over what the call brings for that block and head; other blocks keep theirs.
+ *   kv              the cache; k, v, k_scale and v_scale are WRITTEN through although the struct declares them const
+ *   slot_map        device int32 [total_rows], no slot twice.  For SS_FP8_E4M3 the rows of one block must stand as far apart in the
+ *                   call as their slots, as ss_block_map gives them (rows that are left out may stand between)
+ *   k_new, v_new    device, rows of [num_kv_heads][head_dim] in new_dtype (SS_F32 or SS_BF16), k_stride / v_stride elements
+ *                   apart (so they may be parts of wider rows); rows start 16-byte aligned
+ */
+int32_t ss_kv_write(const ss_paged_kv *kv, const int32_t *slot_map, const void *k_new, int64_t k_stride, const void *v_new,
+                    int64_t v_stride, int32_t new_dtype, int32_t total_rows, void *stream);
+
+/*
+ * Attention of a chunk of new tokens over the paged cache, in which their keys and values already are: the formulas of
+ * ss_spec_verify_attn for chains, without its bound on the new tokens.  Row i of request b is at position
+ * kv_len_b - q_len_b + i and attends positions 0 up to its own.  A row whose position is negative (kv_len below the
+ * request's rows) attends nothing: zeros, and lse minus infinity.
+ *   q          device, rows of [num_q_heads][head_dim] in q_dtype (SS_F32 or SS_BF16), q_stride elements apart (>= num_q_heads *
+ *              head_dim); rows start 16-byte aligned
+ *   out        device, dense [total_rows][num_q_heads][head_dim] in q_dtype; lse device float [total_rows][num_q_heads] or NULL.
+ *              Rows from q_indptr[batch] on keep what they hold
+ *   workspace  device, >= ss_chunk_attn_workspace(...) bytes, 256-byte aligned; contents are scratch.  It follows from the
+ *              host-visible arguments and is largest for a few hundred rows against a wide table (up to 70 MB)
+ * bf16 queries over bf16 or e4m3 caches take bf16 matrix instructions with fp32 scores, sums and outputs, the probabilities
+ * rounded to bf16 for the product with the values; fp32 queries or caches are computed in fp32 throughout.  Up to 16 query
+ * heads per KV head.  Batches with nothing but 1..21 new tokens per request are what ss_spec_verify_attn is for.
+ */
+size_t ss_chunk_attn_workspace(const ss_paged_kv *kv, const ss_batch *batch, int32_t q_dtype, int32_t num_q_heads, int32_t total_rows);
+int32_t ss_chunk_attn(const ss_paged_kv *kv, const ss_batch *batch, const void *q, int64_t q_stride, int32_t q_dtype, int32_t num_q_heads,
+                      int32_t total_rows, float sm_scale, void *out, float *lse, void *workspace, size_t workspace_bytes,
+                      void *stream);
+
+/*
  * Speculation-depth controller (paper Section 3.5, Eq. 8-16, Algorithm 4): host arithmetic only, no
  * device work.  One ss_depth_state is the state of one stream of updates (the flow vector of the last h
  * acceptance gradients, its write index, the smoothed throughput).  ss_depth_init fills a state with the
@@ -389,9 +474,9 @@ int32_t ss_route_select(const ss_worker_metrics *workers, int32_t n, const doubl
  *                   unit together it counts four times (twice up to 32 query rows per KV head); 0 = partitions of equal
  *                   cost of the tiles alone.  3 (the default) = automatic: two pairs of tiles up to 32 query rows per KV head, costs
  *                   measured by row blocks and cache type above that.  Not used where every unit is a partition (few short units)
- *   "validate"      1 = before launching, ss_spec_verify_attn, ss_kv_append and ss_spec_accept check the
+ *   "validate"      1 = before launching, ss_spec_verify_attn, ss_chunk_attn, ss_kv_append, ss_kv_write and ss_spec_accept check the
  *                   device-resident metadata with a small kernel (row offsets, lengths against block counts,
- *                   block ids, draft tokens, temperatures, uniforms), synchronise the stream and return
+ *                   block ids, slots, draft tokens, temperatures, uniforms), synchronise the stream and return
  *                   SS_ERR_INVALID_ARG naming the first inconsistency; 0 (default) = contents are trusted
  * Returns SS_ERR_INVALID_ARG for an unknown name or value.
  */

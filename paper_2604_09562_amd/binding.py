@@ -24,7 +24,8 @@ _DT = {"f32": SS_F32, "bf16": SS_BF16, "fp8": SS_FP8_E4M3}
 EXPORTS = ("ss_version", "ss_last_error", "ss_spec_verify_attn_workspace", "ss_spec_verify_attn",
            "ss_spec_accept_workspace", "ss_spec_accept", "ss_spec_accept_static", "ss_spec_accept_static_capacity",
            "ss_spec_accept_tree_greedy", "ss_spec_accept_tree_sample_workspace",
-           "ss_spec_accept_tree_sample", "ss_kv_append", "ss_kv_compact", "ss_kv_commit", "ss_depth_init",
+           "ss_spec_accept_tree_sample", "ss_block_map_workspace", "ss_block_map", "ss_kv_write", "ss_chunk_attn_workspace",
+           "ss_chunk_attn", "ss_kv_append", "ss_kv_compact", "ss_kv_commit", "ss_depth_init",
            "ss_depth_update", "ss_route_select", "ss_set_option",
            "ss_profile_begin", "ss_profile_collect")
 
@@ -45,6 +46,10 @@ class ss_batch(ctypes.Structure):
                 ("max_q_len", ctypes.c_int32), ("flags", ctypes.c_int32),
                 ("block_table", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("q_indptr", ctypes.c_void_p),
                 ("tree_mask", ctypes.c_void_p)]
+
+
+class ss_block_pool(ctypes.Structure):
+    _fields_ = [("num_blocks", ctypes.c_int32), ("free_ids", ctypes.c_void_p), ("free_count", ctypes.c_void_p)]
 
 
 SS_FLOW_MAX = 64
@@ -114,6 +119,22 @@ def lib() -> ctypes.CDLL:
         L.ss_kv_compact.argtypes = [ctypes.POINTER(ss_paged_kv), ctypes.POINTER(ss_batch), ctypes.c_void_p,
                                     ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p]
         L.ss_kv_compact.restype = ctypes.c_int32
+        L.ss_block_map_workspace.restype = ctypes.c_size_t
+        L.ss_block_map_workspace.argtypes = [ctypes.c_int32]
+        L.ss_block_map.restype = ctypes.c_int32
+        L.ss_block_map.argtypes = [ctypes.POINTER(ss_batch), ctypes.POINTER(ss_block_pool), ctypes.c_void_p, ctypes.c_int32,
+                                   ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                                   ctypes.c_void_p]
+        L.ss_kv_write.restype = ctypes.c_int32
+        L.ss_kv_write.argtypes = [ctypes.POINTER(ss_paged_kv), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                  ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p]
+        L.ss_chunk_attn_workspace.restype = ctypes.c_size_t
+        L.ss_chunk_attn_workspace.argtypes = [ctypes.POINTER(ss_paged_kv), ctypes.POINTER(ss_batch), ctypes.c_int32, ctypes.c_int32,
+                                              ctypes.c_int32]
+        L.ss_chunk_attn.restype = ctypes.c_int32
+        L.ss_chunk_attn.argtypes = [ctypes.POINTER(ss_paged_kv), ctypes.POINTER(ss_batch), ctypes.c_void_p, ctypes.c_int64,
+                                    ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p,
+                                    ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
         L.ss_kv_commit.argtypes = [ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
         L.ss_depth_init.restype = ctypes.c_int32
         L.ss_depth_init.argtypes = [ctypes.POINTER(ss_depth_state)]
@@ -255,6 +276,79 @@ def alloc_attention_outputs(d: Dict[str, object], device="cuda:0", max_q_len: in
     lse = torch.empty(shape[:2], dtype=torch.float32, device=device)
     ws = torch.empty(max(ss_spec_verify_attn_workspace(d, max_q_len), 256), dtype=torch.uint8, device=device)
     return out, lse, ws
+
+
+# --------------------------------------------------------------------------------------------
+# filling the cache
+# --------------------------------------------------------------------------------------------
+def _row_stride(t: torch.Tensor, rows: int, heads: int, head_dim: int) -> int:
+    """Elements from one row of [rows][heads][head_dim] to the next; a row's own values have to be side by side."""
+    if t.dim() != 3 or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != head_dim:
+        raise SpecVerifyError(f"expected {rows} rows of [{heads}][{head_dim}], got a tensor of shape {tuple(t.shape)}")
+    r, h, e = t.stride()
+    if (e != 1 and head_dim > 1) or (h != head_dim and heads > 1):
+        raise SpecVerifyError("the values of a row must be side by side (only the rows themselves may be apart)")
+    return r if t.shape[0] > 1 else heads * head_dim
+
+
+def _cache_descriptor(d: Dict[str, object]) -> ss_paged_kv:
+    return ss_paged_kv(d["num_blocks"], d["block_size"], d["num_kv_heads"], d["head_dim"], _DT[d["kv_dtype"]], _ptr(d["k_cache"]),
+                       _ptr(d["v_cache"]), _ptr(d["k_scale"]), _ptr(d["v_scale"]))
+
+
+def _batch_descriptor(d: Dict[str, object], max_q_len: int = 0) -> ss_batch:
+    return ss_batch(d["batch"], d["max_blocks_per_seq"], max_q_len, 0, _ptr(d["block_table"]), _ptr(d["kv_len"]), _ptr(d["q_indptr"]),
+                    _ptr(d.get("tree_mask")))
+
+
+def ss_block_map(d: Dict[str, object], slot_map: torch.Tensor, positions: Optional[torch.Tensor], status: torch.Tensor,
+                 workspace: torch.Tensor) -> None:
+    """Enqueue the update of `block_table`, `held`, `free_ids` and `free_count` (all in place) for the lengths in `kv_len` and
+    `q_indptr`, and the slots and positions of the new tokens.  What stands in `status` after it says whether it was done."""
+    bt = _batch_descriptor(d)
+    pool = ss_block_pool(d["num_blocks"], _ptr(d["free_ids"]), _ptr(d["free_count"]))
+    _check(lib().ss_block_map(ctypes.byref(bt), ctypes.byref(pool), _ptr(d["held"]), d["total_rows"], _ptr(slot_map), _ptr(positions),
+                              _ptr(status), _ptr(workspace), workspace.nbytes, _stream()))
+
+
+def alloc_block_map_workspace(d: Dict[str, object], device="cuda:0") -> torch.Tensor:
+    n = lib().ss_block_map_workspace(d["batch"])
+    if n == 0:
+        raise SpecVerifyError(lib().ss_last_error().decode())
+    return torch.empty(int(n), dtype=torch.uint8, device=device)
+
+
+def ss_kv_write(d: Dict[str, object], slot_map: torch.Tensor) -> None:
+    """Enqueue the write of `k_new`/`v_new` [rows][kv heads][head_dim] (rows may be apart) to the slots of the device batch's paged cache."""
+    kv = _cache_descriptor(d)
+    rows, heads, dim = d["total_rows"], d["num_kv_heads"], d["head_dim"]
+    _check(lib().ss_kv_write(ctypes.byref(kv), _ptr(slot_map), _ptr(d["k_new"]), _row_stride(d["k_new"], rows, heads, dim), _ptr(d["v_new"]),
+                             _row_stride(d["v_new"], rows, heads, dim), _DT[d["new_dtype"]], rows, _stream()))
+
+
+def ss_chunk_attn_workspace(d: Dict[str, object], max_q_len: int = 0) -> int:
+    kv, bt = _cache_descriptor(d), _batch_descriptor(d, max_q_len)
+    n = lib().ss_chunk_attn_workspace(ctypes.byref(kv), ctypes.byref(bt), _DT[d["q_dtype"]], d["num_q_heads"], d["total_rows"])
+    if n == 0:
+        raise SpecVerifyError(lib().ss_last_error().decode())
+    return int(n)
+
+
+def ss_chunk_attn(d: Dict[str, object], out: torch.Tensor, lse: Optional[torch.Tensor], workspace: torch.Tensor,
+                  max_q_len: int = 0) -> None:
+    """Enqueue attention of a device batch's chunks; `q` [rows][heads][head_dim] may have its rows apart, `out` is dense."""
+    kv, bt = _cache_descriptor(d), _batch_descriptor(d, max_q_len)
+    _check(lib().ss_chunk_attn(ctypes.byref(kv), ctypes.byref(bt), _ptr(d["q"]), _row_stride(d["q"], d["total_rows"], d["num_q_heads"], d["head_dim"]),
+                               _DT[d["q_dtype"]], d["num_q_heads"], d["total_rows"], d["sm_scale"], _ptr(out), _ptr(lse),
+                               _ptr(workspace), workspace.nbytes, _stream()))
+
+
+def alloc_chunk_outputs(d: Dict[str, object], device="cuda:0", max_q_len: int = 0):
+    """Allocate (out, lse, workspace) for a device batch's chunks.  `out` holds raw storage (int16 = bf16 bits)."""
+    shape = (d["total_rows"], d["num_q_heads"], d["head_dim"])
+    out = torch.empty(shape, dtype=torch.float32 if d["q_dtype"] == "f32" else torch.int16, device=device)
+    lse = torch.empty(shape[:2], dtype=torch.float32, device=device)
+    return out, lse, torch.empty(ss_chunk_attn_workspace(d, max_q_len), dtype=torch.uint8, device=device)
 
 
 def ss_kv_append(d: Dict[str, object], max_q_len: int = 0) -> None:

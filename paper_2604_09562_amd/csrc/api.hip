@@ -6,7 +6,7 @@
 #include <atomic>
 #include <vector>
 
-#include "common.h"
+#include "prefill.h"
 
 namespace ss {
 
@@ -34,6 +34,8 @@ constexpr int64_t kUnitWeightAuto = 3;    // the option's default: what was meas
 static int64_t g_unit_weight = kUnitWeightAuto;
 static std::vector<hipEvent_t> g_events;  // pairs
 static int g_prof_cap = 0, g_prof_used = 0;
+
+bool option_validate() { return g_validate != 0; }
 
 static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

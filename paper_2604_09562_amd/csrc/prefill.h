@@ -1,0 +1,75 @@
+// Internal declarations of the calls that fill the paged cache: block tables and slot maps, the write of a chunk's keys and values,
+// and attention of a chunk of new tokens (not part of the C ABI).
+#pragma once
+
+#include "common.h"
+
+namespace ss {
+
+bool option_validate();   // option "validate"
+
+// ---- block tables and slot maps ----------------------------------------------------------------
+struct BlockMapArgs {
+    int32_t batch, max_blocks, num_blocks, total_rows;
+    int32_t *block_table;
+    const int32_t *kv_len, *q_indptr;
+    int32_t *free_ids, *free_count, *held;
+    int32_t *slot_map, *positions, *status;   // positions may be nullptr
+    int32_t *scratch;                         // block_map_scratch_ints(batch) ints
+};
+size_t block_map_scratch_ints(int batch);
+int32_t block_map_launch(const BlockMapArgs &a, hipStream_t stream);
+
+// ---- the write of keys and values by slot ------------------------------------------------------
+struct KvWriteArgs {
+    void *k, *v;
+    float *k_scale, *v_scale;
+    int32_t num_kv_heads, head_dim, kv_dtype, num_blocks;
+    const int32_t *slot_map;
+    const void *k_new, *v_new;
+    int64_t k_stride, v_stride;   // elements from one row to the next
+    int32_t new_dtype, total_rows;
+};
+int32_t kv_write_launch(const KvWriteArgs &a, hipStream_t stream);
+
+// ---- attention of a chunk ----------------------------------------------------------------------
+struct ChunkArgs {
+    const void *k, *v;
+    const float *k_scale, *v_scale;
+    int32_t num_kv_heads, head_dim, kv_dtype;
+    int32_t batch, max_blocks;
+    const int32_t *block_table, *kv_len, *q_indptr;
+    const void *q;
+    int64_t q_stride;             // elements from one row to the next
+    void *out;
+    float *lse;
+    int32_t q_dtype, num_q_heads;
+    float sm_scale;
+    // how the work is cut (chunk_plan.h)
+    int32_t target;               // workgroups that run at a time
+    int32_t cap;                  // partial results the workspace has room for, 0: no tile is cut
+    int32_t *head;                // [1] tiles that were cut
+    int32_t *rec;                 // [cap / 2 rounded up][kChunkRecInts] one record per tile that was cut
+    float *part_ml, *part_o;      // [cap] partial results
+};
+constexpr int kChunkRecInts = 8;
+constexpr int kChunkRows = 128, kChunkRowsF32 = 64;   // query rows of a tile: bf16 matrix-core kernel, fp32 kernel
+
+struct ChunkShape {               // host-visible sizes a launch and its workspace follow from
+    int32_t rows;                 // query rows of a tile
+    int64_t tiles;                // upper bound of the tiles of one KV head
+    int32_t cap;
+};
+int chunk_target();
+bool chunk_mfma_supported(int head_dim, int kv_dtype, int q_dtype);
+ChunkShape chunk_shape(bool mfma, int batch, int max_blocks, int num_q_heads, int num_kv_heads, int total_rows);
+size_t chunk_workspace_bytes(const ChunkShape &s, int head_dim);
+void chunk_carve(ChunkArgs &a, const ChunkShape &s, void *workspace);
+int32_t chunk_f32_launch(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream);
+
+// ---- optional checks of device-resident metadata -----------------------------------------------
+int32_t validate_chunk(const int32_t *block_table, const int32_t *kv_len, const int32_t *q_indptr, int batch, int max_blocks,
+                       int num_blocks, int total_rows, int max_q_len, hipStream_t stream, const char *what);
+int32_t validate_slots(const int32_t *slot_map, int total_rows, int64_t slots, bool runs, hipStream_t stream, const char *what);
+
+}  // namespace ss

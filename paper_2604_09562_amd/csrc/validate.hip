@@ -3,7 +3,7 @@
 // kernel and a stream synchronisation.  With the option on, a single workgroup walks the metadata first,
 // reading nothing beyond the sizes the arguments declare, and reports the first inconsistency through a
 // small pinned host record, so that a bad batch becomes an error code instead of a wild read.
-#include "common.h"
+#include "prefill.h"
 
 namespace ss {
 namespace {
@@ -15,7 +15,8 @@ struct CheckRecord {
     int32_t aux;
 };
 
-enum { CK_QLEN = 1, CK_QSTART, CK_QTOTAL, CK_KVLEN, CK_BLOCKS, CK_BLOCK_ID, CK_TOKEN, CK_TEMP, CK_UNIFORM, CK_TREE };
+enum { CK_QLEN = 1, CK_QSTART, CK_QTOTAL, CK_KVLEN, CK_BLOCKS, CK_BLOCK_ID, CK_TOKEN, CK_TEMP, CK_UNIFORM, CK_TREE,
+       CK_CHUNK_ROWS, CK_SLOT, CK_SLOT_TWICE, CK_SLOT_RUN };
 
 __global__ __launch_bounds__(256) void validate_batch_kernel(const int32_t *block_table, const int32_t *kv_len,
                                                              const int32_t *q_indptr, const uint32_t *tree_mask, int batch,
@@ -113,6 +114,75 @@ __global__ __launch_bounds__(256) void validate_accept_kernel(const int32_t *dra
     __threadfence_system();
 }
 
+// Chunks of any length, requests without new tokens, rows behind the last request's.
+__global__ __launch_bounds__(256) void validate_chunk_kernel(const int32_t *block_table, const int32_t *kv_len, const int32_t *q_indptr, int batch,
+                                                             int max_blocks, int num_blocks, int total_rows, int max_q_len, CheckRecord *out)
+{
+    __shared__ int bad_req, bad_block;
+    const int tid = threadIdx.x;
+    if (tid == 0) bad_req = bad_block = 0x7fffffff;
+    __syncthreads();
+    CheckRecord r = {0, 0, 0, 0};
+    for (int b = tid; b < batch; b += 256) {
+        const int q0 = q_indptr[b], q1 = q_indptr[b + 1], L = kv_len[b];
+        const long long nblk = ((long long)L + kTile - 1) / kTile;
+        if (q0 < 0 || q1 < q0 || q1 > total_rows || q1 - q0 > max_q_len || (b == 0 && q0 != 0) || L < 0 || nblk > max_blocks) atomicMin(&bad_req, b);
+    }
+    __syncthreads();
+    const int good = min(bad_req, batch);   // the lengths of the requests in front of the first bad one bound the reads of the table
+    for (int b = 0; b < good; ++b) {
+        const int n = (kv_len[b] + kTile - 1) / kTile;
+        for (int t = tid; t < n; t += 256) {
+            const int id = block_table[(long long)b * max_blocks + t];
+            if (id < 0 || id >= num_blocks) atomicMin(&bad_block, t);
+        }
+        __syncthreads();
+        if (bad_block != 0x7fffffff) {   // uniform: read after the barrier
+            r = {CK_BLOCK_ID, b, block_table[(long long)b * max_blocks + bad_block], bad_block};
+            break;
+        }
+        __syncthreads();
+    }
+    if (r.code == 0 && bad_req != 0x7fffffff) {
+        const int b = bad_req, q0 = q_indptr[b], q1 = q_indptr[b + 1], L = kv_len[b];
+        if (b == 0 && q0 != 0) r = {CK_QSTART, b, q0, 0};
+        else if (q1 < q0 || q1 - q0 > max_q_len) r = {CK_CHUNK_ROWS, b, q1 - q0, max_q_len};
+        else if (q0 < 0 || q1 > total_rows) r = {CK_CHUNK_ROWS, b, q1, total_rows};
+        else if (L < 0) r = {CK_KVLEN, b, L, q1 - q0};
+        else r = {CK_BLOCKS, b, L, max_blocks};
+    }
+    if (tid != 0) return;
+    *out = r;
+    __threadfence_system();
+}
+
+// Slots inside the cache, each named once; where a block's rows have to be a run, one run.
+__global__ __launch_bounds__(1024) void validate_slots_kernel(const int32_t *slot_map, int total_rows, long long slots, int runs, CheckRecord *out)
+{
+    __shared__ int range, twice, run;
+    const int tid = threadIdx.x;
+    if (tid == 0) range = twice = run = 0x7fffffff;
+    __syncthreads();
+    for (int r = tid; r < total_rows; r += 1024) {
+        const int x = slot_map[r];
+        if (x < 0) continue;
+        if (x >= slots) atomicMin(&range, r);
+        for (int i = 0; i < r; ++i) {
+            const int y = slot_map[i];
+            if (y == x) atomicMin(&twice, r);
+            else if (runs && y >= 0 && y / kTile == x / kTile && x - y != r - i) atomicMin(&run, r);
+        }
+    }
+    __syncthreads();
+    if (tid != 0) return;
+    CheckRecord r = {0, 0, 0, 0};
+    if (range != 0x7fffffff) r = {CK_SLOT, range, slot_map[range], 0};
+    else if (twice != 0x7fffffff) r = {CK_SLOT_TWICE, twice, slot_map[twice], 0};
+    else if (run != 0x7fffffff) r = {CK_SLOT_RUN, run, slot_map[run], 0};
+    *out = r;
+    __threadfence_system();
+}
+
 CheckRecord *g_record = nullptr;   // pinned host memory, mapped into the device's address space
 
 int32_t record(CheckRecord **host, CheckRecord **dev)
@@ -137,6 +207,10 @@ int32_t report(const CheckRecord &r, const char *what)
     case CK_TOKEN: return fail(SS_ERR_INVALID_ARG, "%s: draft token %d at draft row %d is outside the vocabulary", what, r.value, r.where);
     case CK_TEMP: return fail(SS_ERR_INVALID_ARG, "%s: request %d has a non-positive temperature", what, r.where);
     case CK_TREE: return fail(SS_ERR_INVALID_ARG, "%s: request %d, row %d has tree mask 0x%x (own bit missing or a bit past its query rows)", what, r.where, r.value, (unsigned)r.aux);
+    case CK_CHUNK_ROWS: return fail(SS_ERR_INVALID_ARG, "%s: request %d has rows or an end of rows of %d (at most %d)", what, r.where, r.value, r.aux);
+    case CK_SLOT: return fail(SS_ERR_INVALID_ARG, "%s: row %d has slot %d, outside the cache", what, r.where, r.value);
+    case CK_SLOT_TWICE: return fail(SS_ERR_INVALID_ARG, "%s: row %d has slot %d, as an earlier row has", what, r.where, r.value);
+    case CK_SLOT_RUN: return fail(SS_ERR_INVALID_ARG, "%s: row %d (slot %d): the rows of an e4m3 block must stand as far apart as their slots, ascending", what, r.where, r.value);
     default: return fail(SS_ERR_INVALID_ARG, "%s: uniform %d is outside [0, 1)", what, r.where);
     }
 }
@@ -152,6 +226,30 @@ int32_t validate_batch(const int32_t *block_table, const int32_t *kv_len, const 
     hipLaunchKernelGGL(validate_batch_kernel, dim3(1), dim3(256), 0, stream, block_table, kv_len, q_indptr, tree_mask, batch, max_blocks,
                        num_blocks, total_rows, max_q_len > 0 ? max_q_len : SS_OUT_WIDTH, dev);
     SS_HIP_CHECK(hipGetLastError(), "launch validate_batch_kernel");
+    SS_HIP_CHECK(hipStreamSynchronize(stream), "hipStreamSynchronize (validation)");
+    return report(*host, what);
+}
+
+int32_t validate_chunk(const int32_t *block_table, const int32_t *kv_len, const int32_t *q_indptr, int batch, int max_blocks,
+                       int num_blocks, int total_rows, int max_q_len, hipStream_t stream, const char *what)
+{
+    CheckRecord *host = nullptr, *dev = nullptr;
+    const int32_t rc = record(&host, &dev);
+    if (rc != SS_OK) return rc;
+    hipLaunchKernelGGL(validate_chunk_kernel, dim3(1), dim3(256), 0, stream, block_table, kv_len, q_indptr, batch, max_blocks, num_blocks, total_rows,
+                       max_q_len, dev);
+    SS_HIP_CHECK(hipGetLastError(), "launch validate_chunk_kernel");
+    SS_HIP_CHECK(hipStreamSynchronize(stream), "hipStreamSynchronize (validation)");
+    return report(*host, what);
+}
+
+int32_t validate_slots(const int32_t *slot_map, int total_rows, int64_t slots, bool runs, hipStream_t stream, const char *what)
+{
+    CheckRecord *host = nullptr, *dev = nullptr;
+    const int32_t rc = record(&host, &dev);
+    if (rc != SS_OK) return rc;
+    hipLaunchKernelGGL(validate_slots_kernel, dim3(1), dim3(1024), 0, stream, slot_map, total_rows, (long long)slots, runs ? 1 : 0, dev);
+    SS_HIP_CHECK(hipGetLastError(), "launch validate_slots_kernel");
     SS_HIP_CHECK(hipStreamSynchronize(stream), "hipStreamSynchronize (validation)");
     return report(*host, what);
 }

@@ -1,0 +1,204 @@
+"""ss_chunk_attn against attention in 64 bits, within bounds that follow from the roundings."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_09562_amd import binding
+from tests import prefill_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def run(inp, lse=True, label=""):
+    out, z, ws = binding.alloc_chunk_outputs(inp)
+    out.view(torch.uint8).fill_(0x5A)
+    z.fill_(123.0)
+    ws.fill_(0xFF)                               # what a workspace holds is of no account
+    binding.ss_chunk_attn(inp, out, z if lse else None, ws)
+    torch.cuda.synchronize()
+    used = int(inp["q_indptr"][-1])
+    assert (out.view(torch.uint8)[used:] == 0x5A).all() and (z[used:] == 123.0).all(), "rows of no request are left as they were"
+    if not lse:
+        assert (z == 123.0).all()
+        z = ref.chunk_reference(inp)[1].float()
+    ref.check_chunk(inp, out, z, label)
+    return out, z
+
+
+# one token to many, lengths on both sides of blocks (16), steps (64) and tiles, requests without rows or without a cache
+EDGES = [(1, 1), (1, 16), (1, 17), (2, 2), (15, 15), (16, 16), (17, 17), (31, 63), (32, 64), (33, 65), (63, 64), (64, 64), (65, 65), (1, 640),
+         (0, 0), (0, 50), (127, 130), (128, 128), (129, 300)]
+
+
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32"), ("bf16", "f32"), ("f32", "bf16"), ("f32", "fp8")])
+@pytest.mark.parametrize("d", [64, 128])
+def test_edge_lengths(q, kv, d):
+    run(ref.chunk_batch(EDGES, 8, 2, d, kv, q, seed=d, spare_rows=5, spare_columns=2))
+
+
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32")])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (4, 2), (6, 2), (5, 1), (14, 2), (16, 2), (32, 8), (16, 1), (26, 2)])
+def test_head_groupings(q, kv, hq, hkv):
+    run(ref.chunk_batch([(40, 100), (1, 70), (97, 97), (3, 300)], hq, hkv, 128, kv, q, seed=hq))
+
+
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32")])
+@pytest.mark.parametrize("lengths", [[(700, 700)], [(300, 2100)], [(64, 5000)], [(1, 9000)], [(130, 1500), (1, 4000), (500, 500), (7, 20)]],
+                         ids=["prompt", "last_piece", "few_rows_long_cache", "one_row", "mixed"])
+def test_long(q, kv, lengths):
+    run(ref.chunk_batch(lengths, 8, 2, 128, kv, q, seed=len(lengths)))
+
+
+def test_the_same_table_wider_and_without_lse():
+    for extra in (0, 1, 50, 3000):
+        run(ref.chunk_batch([(90, 333), (5, 900)], 8, 2, 128, spare_columns=extra, seed=4), lse=False)
+
+
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32")])
+def test_rows_that_see_nothing(q, kv):
+    """A cache shorter than the request's rows: the first rows are in front of it."""
+    lengths = [(40, 40), (30, 10), (20, 0), (200, 130), (1, 0)]
+    inp = ref.chunk_batch(lengths, 8, 2, 64, kv, q, seed=9)
+    out, z = run(inp)
+    assert torch.isinf(z[40:60]).all() and (out[40:60] == 0).all() and torch.isfinite(z[60:70]).all()
+
+
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("f32", "f32")])
+def test_queries_in_wider_rows(q, kv):
+    inp = ref.chunk_batch([(50, 120), (1, 30)], 8, 2, 128, kv, q, row_pad=264, seed=2)
+    a, za = run(inp)
+    dense = dict(inp, q=inp["q"].contiguous())
+    b, zb = run(dense)
+    assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)) and torch.equal(za, zb)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+def test_sharp_and_flat_scores(kv):
+    for sharp in (0.0, 0.01, 30.0):
+        run(ref.chunk_batch([(70, 400), (200, 200)], 4, 1, 128, kv, sharp=sharp, seed=6), label=f"sharp {sharp}")
+
+
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("f32", "f32")])
+def test_scores_that_grow_along_the_cache(q, kv):
+    """Each step's largest score is far above the last one's, and the other way round."""
+    for sign in (1.0, -1.0):
+        inp = ref.chunk_batch([(90, 700)], 4, 1, 128, kv, q, seed=8)
+        n = 700
+        ids = inp["block_table"][0].long()
+        ramp = torch.arange(ids.numel() * 16, device="cuda").view(-1, 16).float() / n * 40.0 * sign
+        k = torch.zeros_like(inp["k_cache"])
+        k[ids, 0, :, 0] = ramp.to(k.dtype)
+        inp["k_cache"] = k
+        inp["q"] = inp["q"].clone()
+        inp["q"][:, :, 0] = 11.25
+        run(inp, label=f"ramp {sign}")
+
+
+def test_negative_and_zero_scales():
+    inp = ref.chunk_batch([(90, 300), (3, 40)], 8, 2, 128, "fp8", seed=12)
+    inp["k_scale"][::3] *= -1.0
+    inp["v_scale"][1::4] = 0.0
+    run(inp)
+
+
+@pytest.mark.parametrize("kv,d", [("bf16", 128), ("fp8", 128), ("bf16", 64)])
+def test_what_later_rows_see_may_be_infinite(kv, d):
+    """A key or value that is not finite reaches the rows that see it and no other."""
+    inp = ref.chunk_batch([(150, 200)], 4, 1, d, kv, seed=3)
+    clean = dict(inp, k_cache=inp["k_cache"].clone(), v_cache=inp["v_cache"].clone())
+    pos = 120                                            # seen from row 70 on
+    blk, place = int(inp["block_table"][0, pos // 16]), pos % 16
+    for name in ("k_cache", "v_cache"):
+        raw = inp[name].view(torch.uint8) if kv == "fp8" else inp[name]
+        raw[blk, 0, place, 5] = 0x7F if kv == "fp8" else float("inf") if name == "v_cache" else float("nan")
+    out, z, ws = binding.alloc_chunk_outputs(inp)
+    binding.ss_chunk_attn(inp, out, z, ws)
+    want, zw, _ = binding.alloc_chunk_outputs(clean)
+    binding.ss_chunk_attn(clean, want, zw, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(out[:70], want[:70]) and torch.equal(z[:70], zw[:70])
+    assert not torch.isfinite(out[70:].view(torch.bfloat16).float()).all()
+
+
+def test_equal_calls_give_equal_bits():
+    inp = ref.chunk_batch([(64, 6000), (500, 900), (1, 40)], 8, 2, 128, seed=5)
+    a, za = run(inp)
+    for _ in range(3):
+        b, zb = run(inp)
+        assert torch.equal(a, b) and torch.equal(za, zb)
+
+
+def test_many_requests():
+    rng = np.random.default_rng(3)
+    lengths = []
+    for _ in range(300):
+        q = int(rng.integers(0, 12))
+        lengths.append((q, q + int(rng.integers(0, 90))))
+    run(ref.chunk_batch(lengths, 4, 2, 64, seed=7))
+    run(ref.chunk_batch(lengths[:65], 4, 2, 128, "fp8", seed=7))
+
+
+def test_single_rows_agree_with_verify_attention(oracle):
+    """Chains of up to 21 new tokens: what the call for them is bound to, too."""
+    from paper_2604_09562_amd import synth
+    cfg = synth.CONFIGS[1].scaled(batch=9, ctx=("uniform", 21, 900), depth=("uniform", 0, 20))
+    host = synth.make_attention_inputs(cfg, seed=3)
+    want, lse = oracle.verify_attn(host)
+    d = binding.attention_to_device(host)
+    out, z, ws = binding.alloc_chunk_outputs(d)
+    binding.ss_chunk_attn(d, out, z, ws)
+    torch.cuda.synchronize()
+    got = binding.bf16_bits_to_float(out)
+    assert np.all(np.abs(got - want) <= 2e-2 + 1e-2 * np.abs(want))
+    assert np.all(np.abs(z.cpu().numpy() - lse) <= 1e-3 + 1e-3 * np.abs(lse))
+
+
+def test_another_stream():
+    inp = ref.chunk_batch([(64, 3000), (300, 300)], 8, 2, 128, seed=5)
+    want, zw = run(inp)
+    out, z, ws = binding.alloc_chunk_outputs(inp)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        binding.ss_chunk_attn(inp, out, z, ws)
+    s.synchronize()
+    assert torch.equal(out, want) and torch.equal(z, zw)
+
+
+def test_captured_and_replayed_with_other_lengths():
+    """A graph for a padded batch: the lengths, rows and tables in it change from replay to replay."""
+    big = ref.chunk_batch([(200, 900), (64, 3000), (1, 500), (30, 30)], 8, 2, 128, seed=5, spare_rows=20)
+    out, z, ws = binding.alloc_chunk_outputs(big)
+    binding.ss_chunk_attn(big, out, z, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.ss_chunk_attn(big, out, z, ws)
+    for lengths in ([(200, 900), (64, 3000), (1, 500), (30, 30)], [(1, 900), (300, 2500), (0, 0), (0, 0)], [(0, 5), (0, 0), (0, 1), (1, 1)]):
+        q = [n for n, _ in lengths]
+        big["q_indptr"].copy_(torch.tensor([0] + list(np.cumsum(q)), dtype=torch.int32))
+        big["kv_len"].copy_(torch.tensor([n for _, n in lengths], dtype=torch.int32))
+        for _ in range(2):
+            out.fill_(0)
+            graph.replay()
+            torch.cuda.synchronize()
+            ref.check_chunk(big, out, z, str(lengths))
+
+
+def test_option_validate_names_the_request():
+    binding.ss_set_option("validate", 1)
+    try:
+        good = ref.chunk_batch([(20, 40), (0, 0), (3, 50)], 4, 2, 64, spare_rows=4)
+        run(good)
+        for change, text in ((lambda d: d["kv_len"].__setitem__(2, 16 * 99), "request 2"), (lambda d: d["block_table"].__setitem__((0, 1), 77777), "block 1"),
+                             (lambda d: d["q_indptr"].__setitem__(1, 30), "request 0"), (lambda d: d["q_indptr"].__setitem__(3, 99), "request 2"),
+                             (lambda d: d["kv_len"].__setitem__(0, -1), "kv_len -1")):
+            bad = ref.chunk_batch([(20, 40), (0, 0), (3, 50)], 4, 2, 64, spare_rows=4)
+            out, z, ws = binding.alloc_chunk_outputs(bad)
+            change(bad)
+            with pytest.raises(binding.SpecVerifyError, match=text):
+                binding.ss_chunk_attn(bad, out, z, ws)
+        with pytest.raises(binding.SpecVerifyError, match="at most 19"):
+            binding.ss_chunk_attn(good, *binding.alloc_chunk_outputs(good), max_q_len=19)
+    finally:
+        binding.ss_set_option("validate", 0)

@@ -1,0 +1,162 @@
+"""ss_kv_write against plain indexing: every byte of both caches and every scale equal, what is not written included."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_09562_amd import binding
+from tests import prefill_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def batch(lengths, hkv, d, kv, new, seed=0, row_pad=0, spare_rows=0, sigma=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    counts = [ref.blocks(n) for _, n in lengths]
+    total = sum(counts) + 3
+    perm = torch.randperm(total, generator=gen).tolist()
+    slots, at = [], 0
+    for (q, n), c in zip(lengths, counts):
+        slots += [perm[at + p // 16] * 16 + p % 16 for p in range(n - q, n)]
+        at += c
+    slots += [-1] * spare_rows
+    rows = len(slots)
+    k, ks = ref.cache_values((total, hkv, 16, d), kv, gen, "cpu")
+    v, vs = ref.cache_values((total, hkv, 16, d), kv, gen, "cpu")
+    wide = (torch.randn((rows, 2 * hkv * d + row_pad), generator=gen) * sigma).to(ref.TORCH[new])
+    return dict(num_kv_heads=hkv, head_dim=d, block_size=16, num_blocks=total, kv_dtype=kv, k_cache=k, v_cache=v, k_scale=ks, v_scale=vs,
+                wide=wide, new_dtype=new, total_rows=rows, slots=torch.tensor(slots, dtype=torch.int32))
+
+
+def plain(c):
+    """The caches and scales after the write, on the CPU: one float32 division and torch's own casts."""
+    hkv, d = c["num_kv_heads"], c["head_dim"]
+    res = []
+    for cache, scale, new in ((c["k_cache"], c["k_scale"], c["wide"][:, :hkv * d]), (c["v_cache"], c["v_scale"], c["wide"][:, hkv * d:2 * hkv * d])):
+        cache, scale = cache.clone(), None if scale is None else scale.clone()
+        new = new.reshape(-1, hkv, d)
+        by_block = {}
+        for r, s in enumerate(c["slots"].tolist()):
+            if 0 <= s < c["num_blocks"] * 16:
+                by_block.setdefault(s // 16, []).append((r, s % 16))
+        for blk, entries in by_block.items():
+            rows, places = [r for r, _ in entries], [p for _, p in entries]
+            x = new[rows]
+            if scale is None:
+                cache[blk][:, places] = x.transpose(0, 1).to(cache.dtype)
+                continue
+            x = x.float()
+            if 0 in places:
+                top = x.abs().amax((0, 2)) / torch.tensor(448.0)
+                scale[blk] = torch.where(top > 0, top, torch.ones(()))
+            code = (x / scale[blk][None, :, None]).clamp(-448.0, 448.0).to(torch.float8_e4m3fn)
+            cache.view(torch.uint8)[blk][:, places] = code.view(torch.uint8).transpose(0, 1)
+        res += [cache, scale]
+    return res
+
+
+def run(c):
+    hkv, d = c["num_kv_heads"], c["head_dim"]
+    dev = {k: (v.cuda() if isinstance(v, torch.Tensor) else v) for k, v in c.items()}
+    dev["k_new"] = dev["wide"][:, :hkv * d].unflatten(1, (hkv, d))
+    dev["v_new"] = dev["wide"][:, hkv * d:2 * hkv * d].unflatten(1, (hkv, d))
+    binding.ss_kv_write(dev, dev["slots"])
+    torch.cuda.synchronize()
+    for name, want in zip(("k_cache", "k_scale", "v_cache", "v_scale"), plain(c)):
+        if want is not None:
+            got = dev[name].cpu()
+            a, b = got.contiguous().view(torch.uint8), want.contiguous().view(torch.uint8)
+            assert torch.equal(a, b), f"{name}: {int((a != b).sum())} bytes differ"
+
+
+LENGTHS = [(1, 1), (16, 16), (17, 17), (5, 36), (40, 45), (1, 32), (1, 33), (33, 100), (0, 20), (100, 100)]
+
+
+@pytest.mark.parametrize("kv", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("new", ["f32", "bf16"])
+@pytest.mark.parametrize("hkv,d", [(1, 64), (8, 128), (2, 128), (3, 64)])
+def test_types_and_heads(kv, new, hkv, d):
+    run(batch(LENGTHS, hkv, d, kv, new, seed=hkv, row_pad=8 * hkv, spare_rows=3))
+
+
+@pytest.mark.parametrize("rows", [1, 3, 15, 16, 17, 64, 1023, 1024, 1025, 2048, 4095, 4100])
+def test_windows_of_rows(rows):
+    """e4m3 blocks whose runs begin anywhere in the windows that the rows are taken in."""
+    rng = np.random.default_rng(rows)
+    lengths, left = [], rows
+    while left:
+        q = min(left, int(rng.integers(1, 40)))
+        lengths.append((q, q + int(rng.integers(0, 50))))
+        left -= q
+    run(batch(lengths, 8, 64, "fp8", "bf16", seed=rows))
+
+
+def test_single_rows_of_many_requests():
+    run(batch([(1, n) for n in range(1, 130)], 2, 128, "fp8", "f32", seed=3))
+    run(batch([(1, n) for n in range(1, 130)], 2, 128, "bf16", "f32", seed=3))
+
+
+def test_rows_that_are_left_out():
+    for kv in ("bf16", "fp8"):
+        c = batch(LENGTHS, 2, 128, kv, "bf16", seed=5)
+        s = c["slots"]
+        s[4:9] = -1                              # in the middle of a run: what follows opens no block
+        s[20] = c["num_blocks"] * 16             # behind the cache
+        s[21] = 0x7FFFFFFF
+        s[22] = -0x80000000
+        run(c)
+
+
+def test_e4m3_rounding():
+    """Values on, between and beside neighbouring codes, a block of zeros, and one of a single tiny value."""
+    codes = torch.arange(0x7F, dtype=torch.uint8).view(torch.float8_e4m3fn).float()
+    mids = (codes[:-1] + codes[1:]) / 2
+    ladder = torch.cat([codes, mids, torch.nextafter(mids, torch.tensor(1e9)), torch.nextafter(mids, torch.tensor(-1e9))])
+    ladder = torch.cat([ladder, -ladder])
+    c = batch([(64, 64)], 2, 128, "fp8", "f32", seed=1)
+    n = c["wide"].numel()
+    c["wide"] = ladder.repeat(n // ladder.numel() + 1)[:n].reshape(c["wide"].shape).clone()
+    c["wide"][:, ::128] = 448.0                  # every block's scale is one
+    c["wide"][16:32] = 0.0
+    c["wide"][32:48] = 0.0
+    c["wide"][40, 5] = 1e-38
+    run(c)
+
+
+def test_large_and_small_magnitudes():
+    for sigma in (1e-30, 1e-3, 1e4, 1e30):
+        run(batch(LENGTHS, 2, 64, "fp8", "f32", seed=7, sigma=sigma))
+
+
+def test_against_the_append_of_a_decode_step(oracle):
+    """Up to 21 new tokens of a request: the bytes that ss_kv_append writes."""
+    from paper_2604_09562_amd import synth
+    cfg = synth.CONFIGS[4].scaled(batch=24, ctx=("uniform", 9, 200))
+    inp = synth.make_append_inputs(cfg, seed=1)
+    a, w = binding.append_to_device(inp), binding.append_to_device(inp)
+    binding.ss_kv_append(a)
+    slots = []
+    for b in range(inp["batch"]):
+        q = int(inp["q_indptr"][b + 1] - inp["q_indptr"][b])
+        n = int(inp["kv_len"][b])
+        slots += [int(inp["block_table"][b, p // 16]) * 16 + p % 16 for p in range(n - q, n)]
+    binding.ss_kv_write(w, torch.tensor(slots, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    for name in ("k_cache", "v_cache", "k_scale", "v_scale"):
+        assert torch.equal(a[name].view(torch.uint8), w[name].view(torch.uint8)), name
+
+
+def test_option_validate_names_the_row():
+    binding.ss_set_option("validate", 1)
+    try:
+        for kv, change, text in (("bf16", lambda s: s.__setitem__(7, s[3]), "row 7"), ("bf16", lambda s: s.__setitem__(2, 99999), "outside"),
+                                 ("fp8", lambda s: s.__setitem__(slice(1, 3), s[[2, 1]]), "ascending")):
+            c = batch([(20, 20)], 2, 64, kv, "bf16")
+            change(c["slots"])
+            dev = {k: (v.cuda() if isinstance(v, torch.Tensor) else v) for k, v in c.items()}
+            dev["k_new"] = dev["v_new"] = dev["wide"][:, :128].unflatten(1, (2, 64))
+            with pytest.raises(binding.SpecVerifyError, match=text):
+                binding.ss_kv_write(dev, dev["slots"])
+        c = batch(LENGTHS, 2, 64, "fp8", "bf16", spare_rows=2)
+        run(c)
+    finally:
+        binding.ss_set_option("validate", 0)
