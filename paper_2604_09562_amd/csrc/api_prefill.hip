@@ -200,7 +200,7 @@ int32_t ss_chunk_attn(const ss_paged_kv *kv, const ss_batch *batch, const void *
     a.block_table = batch->block_table; a.kv_len = batch->kv_len; a.q_indptr = batch->q_indptr;
     a.q = q; a.q_stride = q_stride; a.out = out; a.lse = lse; a.q_dtype = q_dtype; a.num_q_heads = num_q_heads; a.sm_scale = sm_scale;
     chunk_carve(a, s, workspace);
-    return chunk_f32_launch(a, s, static_cast<hipStream_t>(stream));
+    return mfma ? chunk_mfma_launch(a, s, static_cast<hipStream_t>(stream)) : chunk_f32_launch(a, s, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

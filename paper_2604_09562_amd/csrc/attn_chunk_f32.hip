@@ -197,8 +197,6 @@ int32_t launch_kv(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream)
 
 }  // namespace
 
-bool chunk_mfma_supported(int, int, int) { return false; }
-
 int32_t chunk_f32_launch(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream)
 {
     if (a.head_dim == 128) return a.q_dtype == SS_F32 ? launch_kv<128, SS_F32>(a, s, stream) : launch_kv<128, SS_BF16>(a, s, stream);

@@ -65,6 +65,7 @@ bool chunk_mfma_supported(int head_dim, int kv_dtype, int q_dtype);
 ChunkShape chunk_shape(bool mfma, int batch, int max_blocks, int num_q_heads, int num_kv_heads, int total_rows);
 size_t chunk_workspace_bytes(const ChunkShape &s, int head_dim);
 void chunk_carve(ChunkArgs &a, const ChunkShape &s, void *workspace);
+int32_t chunk_mfma_launch(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream);
 int32_t chunk_f32_launch(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream);
 
 // ---- optional checks of device-resident metadata -----------------------------------------------
