@@ -5,6 +5,8 @@
 //   S^T[key][row]  = K[key][:] . Q[row][:]       v_mfma_f32_32x32x16_bf16, queries in registers
 //   O^T[d][row]   += V^T[d][key] P^T[key][row]    the same shape; P is taken straight from the accumulators of S^T, V^T by transposing LDS reads
 // so that a lane holds one row: maximum, sum and rescaling of the softmax need no exchange but with the lane that has the row's other keys.
+#include <type_traits>
+
 #include "chunk_merge.h"
 
 namespace ss {
@@ -69,11 +71,17 @@ struct ChunkLds {
     int odd[2][kWaves];
 };
 
+// The largest of three, or NaN (the other kind of maximum costs an instruction more for each operand that may be a signalling NaN).
+__device__ __forceinline__ float max3(float x, float y, float z) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x, y), z); }
+
 template <int D, bool FP8>
-__global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(ChunkArgs a)
+__global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(ChunkArgs a, const int32_t *__restrict__ block_table, const float *__restrict__ k_scale,
+                                                               const float *__restrict__ v_scale)
 {
+    // (table and scales come in as no-alias arguments of their own, so that they are scalar loads)
     constexpr int KS = D / 16, DB = D / 32;
-    constexpr int LOADS = kTile * D * (FP8 ? 1 : 2) / (64 * 16);   // 16-byte loads of a lane for a cache block
+    constexpr int BLOCK_BYTES = kTile * D * (FP8 ? 1 : 2), LOADS = BLOCK_BYTES / (64 * 16);   // 16-byte loads of a lane for a cache block
+    constexpr int STEP_BLOCKS = kStepKeys / kTile;
     __shared__ ChunkLds<D> lds;
     const int g = blockIdx.x % a.num_kv_heads, item = blockIdx.x / a.num_kv_heads;
     ChunkShare s;
@@ -90,7 +98,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(ChunkArgs a)
     const int lim = ctx + qi;                                           // the last position this lane's row sees
     // steps up to which all rows of the wavefront see everything, from which none sees anything; the same of the tile
     const int all = max((ctx + min(n_first, rows - 1) / G + 1) / kStepKeys, 0);
-    const int none = (max(ctx + min(n_first + 31, rows - 1) / G + 1, 0) + kStepKeys - 1) / kStepKeys;
+    const int none = min((max(ctx + min(n_first + 31, rows - 1) / G + 1, 0) + kStepKeys - 1) / kStepKeys, s.s1);
     const int full = max((ctx + s.tile * kRows / G + 1) / kStepKeys, 0);
     const float c = a.sm_scale * kLog2e;
 
@@ -106,60 +114,70 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(ChunkArgs a)
         }
     }
 
-    const int32_t *table = a.block_table + (int64_t)s.b * a.max_blocks;
-    const int blocks = (int)(((unsigned)s.kv_len + kTile - 1) / kTile);
-    u32x4 kin[LOADS], vin[LOADS];
-    // this wavefront's block of a step (the last block again where there is none: what stands there is masked)
-    auto block_id = [&](int step) { return table[min(step * (kStepKeys / kTile) + wave, blocks - 1)]; };
-    auto load = [&](int id) {
-        const int64_t tile = (int64_t)id * a.num_kv_heads + g;
-        const char *kp = static_cast<const char *>(a.k) + tile * (kTile * D * (FP8 ? 1 : 2)) + lane * 16;
-        const char *vp = static_cast<const char *>(a.v) + tile * (kTile * D * (FP8 ? 1 : 2)) + lane * 16;
+    const int32_t *table = block_table + (int64_t)s.b * a.max_blocks;
+    const int last_block = (int)(((unsigned)s.kv_len + kTile - 1) / kTile) - 1;
+    // block j of a step (the last block again where there is none: what stands there is masked)
+    auto block_id = [&](int step, int j) { return table[min(step * STEP_BLOCKS + j, last_block)]; };
+    u32x4 in[LOADS];   // this wavefront's block of a step's keys, or of its values
+    auto load = [&](const void *cache, int id) {
+        const char *p = static_cast<const char *>(cache) + ((int64_t)id * a.num_kv_heads + g) * BLOCK_BYTES + lane * 16;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) kin[i] = *reinterpret_cast<const u32x4 *>(kp + i * 1024);
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) vin[i] = *reinterpret_cast<const u32x4 *>(vp + i * 1024);
+        for (int i = 0; i < LOADS; ++i) in[i] = *reinterpret_cast<const u32x4 *>(p + i * 1024);
     };
-    auto store = [&](int step, int buf) {
+    auto as_bf16 = [&](int i, u32x4 (&w)[FP8 ? 2 : 1]) {
+        if constexpr (FP8) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                w[j / 2][j % 2 * 2] = fp8x2_to_bf16x2<false>(in[i][j]);
+                w[j / 2][j % 2 * 2 + 1] = fp8x2_to_bf16x2<true>(in[i][j]);
+            }
+        } else {
+            w[0] = in[i];
+        }
+    };
+    auto put = [&](Tile<D> &tile, int i, const u32x4 (&w)[FP8 ? 2 : 1]) {
+        const int e = (i * 64 + lane) * (FP8 ? 16 : 8), t = wave * kTile + e / D, col = e % D / 8;   // first element: row, piece
+#pragma unroll
+        for (int p = 0; p < (FP8 ? 2 : 1); ++p) tile.w[t][(col + p) ^ Tile<D>::turn(t & 15)] = w[p];
+    };
+    auto store_keys = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            u32x4 w[FP8 ? 2 : 1];
+            as_bf16(i, w);
+            put(lds.k[buf], i, w);
+        }
+    };
+    auto store_values = [&](auto fast, int step, int buf) {
+        if (decltype(fast)::value || step < full) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                u32x4 w[FP8 ? 2 : 1];
+                as_bf16(i, w);
+                put(lds.v[buf], i, w);
+            }
+            return;
+        }
+        // Some row does not see all of the step.  What stands behind the last token is of no one; a value that is not finite is taken out
+        // of the product, in which it would reach every row (0 * inf), and added to the rows that see it.
         bool odd = false;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int e = (i * 64 + lane) * (FP8 ? 16 : 8), t = wave * kTile + e / D, col = e % D / 8;   // first element: row, piece
-            const int turn = Tile<D>::turn(t & 15);
-            u32x4 kw[FP8 ? 2 : 1], vw[FP8 ? 2 : 1];
-            if constexpr (FP8) {
+            u32x4 w[FP8 ? 2 : 1];
+            as_bf16(i, w);
+            const bool dead = step * kStepKeys + wave * kTile + (i * 64 + lane) * (FP8 ? 16 : 8) / D >= s.kv_len;
+#pragma unroll
+            for (int p = 0; p < (FP8 ? 2 : 1); ++p)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    kw[j / 2][j % 2 * 2] = fp8x2_to_bf16x2<false>(kin[i][j]);
-                    kw[j / 2][j % 2 * 2 + 1] = fp8x2_to_bf16x2<true>(kin[i][j]);
-                    vw[j / 2][j % 2 * 2] = fp8x2_to_bf16x2<false>(vin[i][j]);
-                    vw[j / 2][j % 2 * 2 + 1] = fp8x2_to_bf16x2<true>(vin[i][j]);
+                    uint32_t x = dead ? 0u : w[p][j];
+                    if ((x & 0x7f80u) == 0x7f80u) { x &= 0xffff0000u; odd = true; }
+                    if ((x & 0x7f800000u) == 0x7f800000u) { x &= 0xffffu; odd = true; }
+                    w[p][j] = x;
                 }
-            } else {
-                kw[0] = kin[i];
-                vw[0] = vin[i];
-            }
-            if (step >= full) {
-                // Some row does not see all of the step.  What stands behind the last token is of no one; a value that is not finite is taken out
-                // of the product, in which it would reach every row (0 * inf), and added to the rows that see it.
-                const bool dead = step * kStepKeys + t >= s.kv_len;
-#pragma unroll
-                for (int p = 0; p < (FP8 ? 2 : 1); ++p)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t w = dead ? 0u : vw[p][j];
-                        if ((w & 0x7f80u) == 0x7f80u) { w &= 0xffff0000u; odd = true; }
-                        if ((w & 0x7f800000u) == 0x7f800000u) { w &= 0xffffu; odd = true; }
-                        vw[p][j] = w;
-                    }
-            }
-#pragma unroll
-            for (int p = 0; p < (FP8 ? 2 : 1); ++p) {
-                lds.k[buf].w[t][(col + p) ^ turn] = kw[p];
-                lds.v[buf].w[t][(col + p) ^ turn] = vw[p];
-            }
+            put(lds.v[buf], i, w);
         }
-        if (step >= full) lds.odd[buf][wave] = __ballot(odd) != 0;
+        lds.odd[buf][wave] = __ballot(odd) != 0;
     };
 
     float m = kChunkNoMax, l = 0.f;
@@ -169,45 +187,53 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(ChunkArgs a)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
 
-    if (s.s0 < s.s1) {
-        load(block_id(s.s0));
-        store(s.s0, 0);
-    }
-    int next_id = s.s0 + 1 < s.s1 ? block_id(s.s0 + 1) : 0;
-    for (int step = s.s0; step < s.s1; ++step) {
-        const int buf = (step - s.s0) & 1;
-        team_barrier();
-        const bool more = step + 1 < s.s1;
-        if (more) {
-            load(next_id);
-            if (step + 2 < s.s1) next_id = block_id(step + 2);
+    // scores of 32 keys: the lane has row r32 and keys 8 (i / 4) + 4 half + i % 4
+    auto scores = [&](int buf, int b, float16v &x) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = 0.f;
+        const int t = b * 32 + r32, turn = Tile<D>::turn(t & 15);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const bf16x8 kk = __builtin_bit_cast(bf16x8, lds.k[buf].w[t][(2 * k + half) ^ turn]);
+            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, q[k], x, 0, 0, 0);
         }
-        if (step < none) {
-            // ---- scores: lane has row r32 and keys 8 (i / 4) + 4 half + i % 4 of either block of 32 ----
-            float16v x[2];
+    };
+
+    struct Scales {
+        float k[FP8 ? STEP_BLOCKS : 1], v[FP8 ? STEP_BLOCKS : 1];
+    };
+    auto scales_of = [&](int step) {
+        Scales r;
+        if constexpr (FP8)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[b][i] = 0.f;
-                const int t = b * 32 + r32, turn = Tile<D>::turn(t & 15);
-#pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    const bf16x8 kk = __builtin_bit_cast(bf16x8, lds.k[buf].w[t][(2 * k + half) ^ turn]);
-                    x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, q[k], x[b], 0, 0, 0);
-                }
+            for (int j = 0; j < STEP_BLOCKS; ++j) {
+                const int64_t tile = (int64_t)block_id(step, j) * a.num_kv_heads + g;
+                r.k[j] = k_scale[tile] * c;
+                r.v[j] = v_scale[tile];
             }
-            float vscale[4];
-            if constexpr (FP8) {   // one scale to 16 keys: they are in eight accumulators
+        return r;
+    };
+
+    // One step: the scores of the next one are computed between the exponentials of this one.  buf: of this step's keys and values.
+    // At its beginning LDS holds the step's values and the next step's keys, id1 and id2 are this wavefront's blocks of the next two steps.
+    int id1 = 0, id2 = 0;
+    // FAST: every row of the tile sees all of this step and the next (what would be read behind the share's last step is read as well, from the last block).
+    auto step_of = [&](auto fast, int step, int buf, float16v (&x)[2], float16v (&y)[2]) {
+        constexpr bool FAST = decltype(fast)::value;
+        const bool more = FAST || step + 1 < s.s1, more2 = FAST || step + 2 < s.s1;
+        if (more2) load(a.k, id2);
+        const int id3 = block_id(step + 3, wave);
+        const bool live = FAST || step < none, next = FAST || step + 1 < none;
+        if (next) scores(buf ^ 1, 0, y[0]);
+        Scales sc;
+        if (live) {
+            sc = scales_of(step);
+            if constexpr (FP8)   // one scale to 16 keys: they are in eight accumulators
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int64_t tile = (int64_t)table[min(step * (kStepKeys / kTile) + j, blocks - 1)] * a.num_kv_heads + g;
-                    const float ks = a.k_scale[tile] * c;
-                    vscale[j] = a.v_scale[tile];
+                for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[j / 2][j % 2 * 8 + i] *= ks;
-                }
-            }
-            if (step >= all) {
+                    for (int i = 0; i < 16; ++i) x[b][i] *= sc.k[b * 2 + i / 8];
+            if (!FAST && step >= all) {
                 const int seen = lim - step * kStepKeys - 4 * half;    // keys up to this one, counted from the lane's first
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
@@ -215,12 +241,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(ChunkArgs a)
                     for (int i = 0; i < 16; ++i)
                         if (b * 32 + i / 4 * 8 + i % 4 > seen) x[b][i] = -__builtin_inff();
             }
-            // ---- softmax: the reference follows the largest score when that has risen by kLag ----
-            float top = x[0][0];
+            // the reference follows the largest score when that has risen by kLag
+            float top = max3(x[0][0], x[0][1], x[0][2]);
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, x[b][i]);
+            for (int i = 3; i < 31; i += 2) top = max3(top, x[i / 16][i % 16], x[(i + 1) / 16][(i + 1) % 16]);
+            top = max3(top, x[1][15], x[1][15]);
             top = max_of_halves(top);
             if constexpr (!FP8) top *= c;
             if (__ballot(top > m + kLag || m == kChunkNoMax)) {
@@ -232,22 +257,31 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(ChunkArgs a)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[b][i] *= down;
             }
+        }
+        if (next) scores(buf ^ 1, 1, y[1]);
+        u32x4 pw[4];
+        if (live) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const float p = __builtin_amdgcn_exp2f(FP8 ? x[b][i] - m : __builtin_fmaf(x[b][i], c, -m));
                     l += p;
-                    x[b][i] = FP8 ? p * vscale[b * 2 + i / 8] : p;
+                    x[b][i] = FP8 ? p * sc.v[b * 2 + i / 8] : p;
                 }
-            // ---- output: a contraction takes 16 keys, the lane's eight of them in the order of its accumulators ----
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) pw[k][j] = pack_bf16(x[k / 2][k % 2 * 8 + 2 * j], x[k / 2][k % 2 * 8 + 2 * j + 1]);
+        }
+        if (more2) store_keys(buf);
+        if (more) load(a.v, id1);
+        if (live) {
+            // a contraction takes 16 keys, the lane's eight of them in the order of its accumulators
             const int group = lane >> 4, i16 = lane & 15;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                u32x4 pw;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) pw[j] = pack_bf16(x[k / 2][k % 2 * 8 + 2 * j], x[k / 2][k % 2 * 8 + 2 * j + 1]);
-                const bf16x8 pk = __builtin_bit_cast(bf16x8, pw);
+                const bf16x8 pk = __builtin_bit_cast(bf16x8, pw[k]);
 #pragma unroll
                 for (int b = 0; b < DB; ++b) {
                     s16x4 vv[2];
@@ -262,7 +296,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(ChunkArgs a)
                     o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vk, pk, o[b], 0, 0, 0);
                 }
             }
-            if (step >= full && (lds.odd[buf][0] | lds.odd[buf][1] | lds.odd[buf][2] | lds.odd[buf][3])) {
+            if (!FAST && step >= full && (lds.odd[buf][0] | lds.odd[buf][1] | lds.odd[buf][2] | lds.odd[buf][3])) {
                 for (int pos = step * kStepKeys; pos < min((step + 1) * kStepKeys, lim + 1); ++pos) {
                     const int64_t tile = (int64_t)table[pos / kTile] * a.num_kv_heads + g;
                     const int64_t from = (tile * kTile + pos % kTile) * D + half * 4;
@@ -279,7 +313,40 @@ __global__ __launch_bounds__(64 * kWaves, 2) void chunk_kernel(ChunkArgs a)
                 }
             }
         }
-        if (more) store(step + 1, buf ^ 1);
+        if (more) store_values(fast, step + 1, buf ^ 1);
+        id1 = id2;
+        id2 = id3;
+        team_barrier();
+    };
+
+    if (s.s0 < s.s1) {
+        const int id0 = block_id(s.s0, wave);
+        id1 = block_id(s.s0 + 1, wave);
+        id2 = block_id(s.s0 + 2, wave);
+        load(a.k, id0);
+        store_keys(0);
+        load(a.v, id0);
+        store_values(std::false_type{}, s.s0, 0);
+        if (s.s0 + 1 < s.s1) {
+            load(a.k, id1);
+            store_keys(1);
+        }
+        team_barrier();
+        float16v x[2], y[2];
+        if (s.s0 < none) {
+            scores(0, 0, x[0]);
+            scores(0, 1, x[1]);
+        }
+        team_barrier();   // (the first step brings new keys into the buffer that these scores came from)
+        int step = s.s0;
+        for (const int end = min(full, s.s1) - 2; step < end; step += 2) {
+            step_of(std::true_type{}, step, 0, x, y);
+            step_of(std::true_type{}, step + 1, 1, y, x);
+        }
+        for (; step < s.s1; step += 2) {
+            step_of(std::false_type{}, step, 0, x, y);
+            if (step + 1 < s.s1) step_of(std::false_type{}, step + 1, 1, y, x);
+        }
     }
 
     l = sum_of_halves(l);
@@ -312,7 +379,8 @@ template <int D, bool FP8>
 int32_t launch(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream)
 {
     const int64_t shares = s.tiles + s.cap / a.num_kv_heads;
-    hipLaunchKernelGGL((chunk_kernel<D, FP8>), dim3((unsigned)(shares * a.num_kv_heads)), dim3(64 * kWaves), 0, stream, a);
+    hipLaunchKernelGGL((chunk_kernel<D, FP8>), dim3((unsigned)(shares * a.num_kv_heads)), dim3(64 * kWaves), 0, stream, a,
+                       a.block_table, a.k_scale, a.v_scale);
     SS_HIP_CHECK(hipGetLastError(), "launch chunk_kernel");
     if (s.cap >= 2 * a.num_kv_heads) {
         const int64_t fit = s.cap / (2 * a.num_kv_heads), cuts = s.tiles < fit ? s.tiles : fit;
