@@ -1,4 +1,5 @@
 // C-ABI entry points of the calls that fill the paged cache: argument validation, workspace sizing, dispatch.  No arithmetic here.
+#include <stdlib.h>
 #include "chunk_plan.h"
 
 namespace ss {
@@ -65,11 +66,12 @@ int32_t check_chunk(const ss_paged_kv *kv, const ss_batch *b, int32_t q_dtype, i
 ChunkShape chunk_shape(bool mfma, int batch, int max_blocks, int num_q_heads, int num_kv_heads, int total_rows)
 {
     ChunkShape s;
-    s.rows = mfma ? kChunkRows : kChunkRowsF32;
     const int64_t G = num_q_heads / num_kv_heads;
+    s.rows = mfma ? (getenv("SS_NB") ? atoi(getenv("SS_NB")) : 2) * kChunkRows : kChunkRowsF32;
+    s.target = mfma && s.rows > kChunkRows ? chunk_target() / 2 : chunk_target();
     s.tiles = (int64_t)total_rows * G / s.rows + (batch < total_rows ? batch : total_rows);
     const int64_t steps = ((int64_t)max_blocks * SS_BLOCK_SIZE + kStepKeys - 1) / kStepKeys, pieces = (steps + kMinPiece - 1) / kMinPiece;
-    const int64_t most = s.tiles * pieces * num_kv_heads, fit = 2ll * chunk_target();
+    const int64_t most = s.tiles * pieces * num_kv_heads, fit = 2ll * s.target;
     s.cap = pieces < 2 ? 0 : (int32_t)(most < fit ? most : fit);
     return s;
 }
@@ -86,7 +88,7 @@ size_t chunk_workspace_bytes(const ChunkShape &s, int head_dim)
 void chunk_carve(ChunkArgs &a, const ChunkShape &s, void *workspace)
 {
     char *w = static_cast<char *>(workspace);
-    a.target = chunk_target();
+    a.target = s.target;
     a.cap = s.cap;
     a.head = reinterpret_cast<int32_t *>(w);
     w += 256;

@@ -76,9 +76,8 @@ struct ChunkShare {
     int cuts;                   // tiles that are cut, over all requests
 };
 
-// The share number `item`, for a whole wavefront (all results uniform); false if there are not so many.
 template <int ROWS>
-__device__ bool chunk_share(const ChunkArgs &a, int item, ChunkShare &out)
+__device__ __forceinline__ bool chunk_find(const ChunkArgs &a, int item, ChunkShare &out)
 {
     const ChunkCut<ROWS> c = {a.num_q_heads / a.num_kv_heads};
     const int lane = threadIdx.x & 63;
@@ -149,6 +148,27 @@ __device__ bool chunk_share(const ChunkArgs &a, int item, ChunkShare &out)
     }
     out.cuts = __builtin_amdgcn_readfirstlane(cuts);
     return false;
+}
+
+// The share number `item`, for a whole wavefront, in scalar registers; false if there are not so many.
+template <int ROWS>
+__device__ __forceinline__ bool chunk_share(const ChunkArgs &a, int item, ChunkShare &out)
+{
+    ChunkShare s = {};
+    const bool any = chunk_find<ROWS>(a, item, s);
+    out.b = __builtin_amdgcn_readfirstlane(s.b);
+    out.q0 = __builtin_amdgcn_readfirstlane(s.q0);
+    out.q_len = __builtin_amdgcn_readfirstlane(s.q_len);
+    out.kv_len = __builtin_amdgcn_readfirstlane(s.kv_len);
+    out.tile = __builtin_amdgcn_readfirstlane(s.tile);
+    out.s0 = __builtin_amdgcn_readfirstlane(s.s0);
+    out.s1 = __builtin_amdgcn_readfirstlane(s.s1);
+    out.piece = __builtin_amdgcn_readfirstlane(s.piece);
+    out.pieces = __builtin_amdgcn_readfirstlane(s.pieces);
+    out.slot = __builtin_amdgcn_readfirstlane(s.slot);
+    out.cut = __builtin_amdgcn_readfirstlane(s.cut);
+    out.cuts = __builtin_amdgcn_readfirstlane(s.cuts);
+    return __builtin_amdgcn_readfirstlane(any);
 }
 
 }  // namespace ss

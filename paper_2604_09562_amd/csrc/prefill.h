@@ -53,11 +53,12 @@ struct ChunkArgs {
     float *part_ml, *part_o;      // [cap] partial results
 };
 constexpr int kChunkRecInts = 8;
-constexpr int kChunkRows = 128, kChunkRowsF32 = 64;   // query rows of a tile: bf16 matrix-core kernel, fp32 kernel
+constexpr int kChunkRows = 128, kChunkRowsF32 = 64;   // query rows of a tile: bf16 matrix-core kernel (or twice as many), fp32 kernel
 
 struct ChunkShape {               // host-visible sizes a launch and its workspace follow from
     int32_t rows;                 // query rows of a tile
     int64_t tiles;                // upper bound of the tiles of one KV head
+    int32_t target;               // workgroups that run at a time
     int32_t cap;
 };
 int chunk_target();
