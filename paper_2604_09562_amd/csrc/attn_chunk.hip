@@ -22,7 +22,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kWaves = 4;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // How far (in powers of two) a row's scores may rise above the reference of its exponentials before the sums are rescaled.
-constexpr float kLag = 6.0f;
+constexpr float kLag = 16.0f;
 
 __device__ __forceinline__ uint32_t pack_bf16(float x, float y)
 {
@@ -55,6 +55,16 @@ __device__ __forceinline__ void team_barrier()
     __builtin_amdgcn_s_waitcnt(LOADS ? 0x0070 : 0xc07f);   // vmcnt(0) lgkmcnt(0) | lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+}
+
+// f(LO), f(LO + 1), .. f(HI - 1), each with its number as a type
+template <int LO, int HI, typename F>
+__device__ __forceinline__ void each(F &&f)
+{
+    if constexpr (LO < HI) {
+        f(std::integral_constant<int, LO>{});
+        each<LO + 1, HI>(f);
+    }
 }
 
 constexpr int kKeys = 32;    // keys that are taken at a time, two cache blocks
@@ -96,13 +106,13 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
     int lim[NB];                                                        // the last position this lane's rows see
 #pragma unroll
     for (int e = 0; e < NB; ++e) lim[e] = ctx + min(n_first + e * 32 + r32, rows - 1) / G;
-    // In steps of 32 keys: the share's, up to where all rows of the wavefront see everything, from where none sees anything; all rows of the tile
+    // In steps of 32 keys: the share's, and up to where all rows of the tile see everything
     const int first = s.s0 * (kStepKeys / kKeys);
     const int end = min(s.s1 * (kStepKeys / kKeys), (max(ctx + min((s.tile + 1) * ROWS - 1, rows - 1) / G + 1, 0) + kKeys - 1) / kKeys);
-    const int all = max((ctx + min(n_first, rows - 1) / G + 1) / kKeys, 0);
-    const int none = n_first < rows ? min((max(ctx + min(n_first + 32 * NB - 1, rows - 1) / G + 1, 0) + kKeys - 1) / kKeys, end) : 0;
     const int full = max((ctx + s.tile * ROWS / G + 1) / kKeys, 0);
     const float c = a.sm_scale * kLog2e;
+#pragma unroll
+    for (int e = 0; e < NB; ++e) lim[e] = min(lim[e], end * kKeys - 1);   // (what a step reads behind the share is another one's)
 
     bf16x8 q[NB][KS];
 #pragma unroll
@@ -125,30 +135,38 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
     const int last_block = (int)(((unsigned)s.kv_len + kTile - 1) / kTile) - 1;
     // block j of a step (the last block again where there is none: what stands there is masked)
     auto block_id = [&](int step, int j) __attribute__((always_inline)) { return table[min(step * 2 + j, last_block)]; };
-    auto block_of = [&](const void *cache, int id) __attribute__((always_inline)) { return static_cast<const char *>(cache) + ((int64_t)id * a.num_kv_heads + g) * BLOCK_BYTES; };
+    const uint32_t block_stride = (uint32_t)a.num_kv_heads * BLOCK_BYTES;
+    const char *k_base = static_cast<const char *>(a.k) + (int64_t)g * BLOCK_BYTES, *v_base = static_cast<const char *>(a.v) + (int64_t)g * BLOCK_BYTES;
 
     // ---- a cache block into a quarter of a tile ----
     // bf16: straight into LDS, where a lane's 16 bytes stand behind those of the lane in front of it: the lanes read the pieces in the order of their places.
     // e4m3: through registers, turned into bf16.
-    int piece_at[FP8 ? 1 : LOADS];
+    uint32_t piece_at[FP8 ? 1 : LOADS];
     if constexpr (!FP8)
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int p = i * 64 + lane, t = p / PIECES;
-            piece_at[i] = (t * PIECES + ((p % PIECES) ^ turn<D>(t))) * 16;
+            piece_at[i] = (uint32_t)(t * PIECES + ((p % PIECES) ^ turn<D>(t))) * 16;
         }
     u32x4 in_k[FP8 ? LOADS : 1], in_v[FP8 ? LOADS : 1];
-    auto bring = [&](const void *cache, int id, Tile<D> &tile, int quarter, u32x4 (&in)[FP8 ? LOADS : 1]) __attribute__((always_inline)) {
-        const char *p = block_of(cache, id);
-        if constexpr (FP8) {
+    // (a descriptor of its own for each block, so that a lane's place in it is all that the vector unit has to keep)
+    auto block_at = [&](const char *cache, int id) __attribute__((always_inline)) {
+        return cache + (uint64_t)(uint32_t)id * block_stride;
+    };
+    auto bring_part = [&](const char *at, int i, Tile<D> &tile, int quarter, u32x4 (&in)[FP8 ? LOADS : 1]) __attribute__((always_inline)) {
+        const __amdgpu_buffer_rsrc_t block = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, BLOCK_BYTES, 0x00020000);
+        if constexpr (FP8)
+            in[i] = __builtin_amdgcn_raw_buffer_load_b128(block, (i * 64 + lane) * 16, 0, 0);
+#ifdef __HIP_DEVICE_COMPILE__   // (the host's pass does not know that this GPU brings 16 bytes at a time)
+        else
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(block, (__attribute__((address_space(3))) void *)(&tile.w[quarter * kTile + i * 64 / PIECES][0]), 16,
+                                                     piece_at[i], 0, 0, 0);
+#endif
+    };
+    auto bring = [&](const char *cache, int id, Tile<D> &tile, int quarter, u32x4 (&in)[FP8 ? LOADS : 1]) __attribute__((always_inline)) {
+        const char *block = block_at(cache, id);
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) in[i] = *reinterpret_cast<const u32x4 *>(p + (i * 64 + lane) * 16);
-        } else {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i)
-                __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) const void *)(p + piece_at[i]),
-                                                 (__attribute__((address_space(3))) void *)(&tile.w[quarter * kTile + i * 64 / PIECES][0]), 16, 0, 0);
-        }
+        for (int i = 0; i < LOADS; ++i) bring_part(block, i, tile, quarter, in);
     };
     auto put = [&](const u32x4 (&in)[FP8 ? LOADS : 1], Tile<D> &tile, int quarter) __attribute__((always_inline)) {
         if constexpr (FP8)
@@ -203,25 +221,19 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
     }
 
     const int turn32 = turn<D>(r32 & 15), group = lane >> 4, i16 = lane & 15;
-    auto read_keys = [&](const Tile<D> &tile, int part, bf16x8 (&kf)[KS]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int k = 0; k < KS; ++k) kf[k] = __builtin_bit_cast(bf16x8, tile.w[part * kKeys + r32][(2 * k + half) ^ turn32]);
+    auto read_keys = [&](const Tile<D> &tile, int part, int k) __attribute__((always_inline)) {
+        return __builtin_bit_cast(bf16x8, tile.w[part * kKeys + r32][(2 * k + half) ^ turn32]);
     };
     // values as the other operand: a contraction takes 16 keys, the lane's eight of them in the order of its scores
-    auto read_values = [&](const Tile<D> &tile, int part, bf16x8 (&vf)[2][DB]) __attribute__((always_inline)) {
+    auto read_values = [&](const Tile<D> &tile, int part, int k, int b) __attribute__((always_inline)) {
+        s16x4 vv[2];
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int b = 0; b < DB; ++b) {
-                s16x4 vv[2];
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const int t = k * 16 + r * 8 + half * 4 + i16 / 4, d = b * 32 + (group & 1) * 16 + i16 % 4 * 4;
-                    const auto *p = reinterpret_cast<const char *>(&tile.w[part * kKeys + t][(d / 8) ^ turn<D>(t & 15)]) + d % 8 * 2;
-                    vv[r] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p));
-                }
-                vf[k][b] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(vv[0], vv[1], 0, 1, 2, 3, 4, 5, 6, 7));
-            }
+        for (int r = 0; r < 2; ++r) {
+            const int t = k * 16 + r * 8 + half * 4 + i16 / 4, d = b * 32 + (group & 1) * 16 + i16 % 4 * 4;
+            const auto *p = reinterpret_cast<const char *>(&tile.w[part * kKeys + t][(d / 8) ^ turn<D>(t & 15)]) + d % 8 * 2;
+            vv[r] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p));
+        }
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(vv[0], vv[1], 0, 1, 2, 3, 4, 5, 6, 7));
     };
     // scores of 32 keys: the lane has row r32 of each block of rows and keys 8 (i / 4) + 4 half + i % 4
     auto scores = [&](const bf16x8 (&kf)[KS], float16v (&x)[NB]) __attribute__((always_inline)) {
@@ -234,42 +246,39 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
 #pragma unroll
             for (int e = 0; e < NB; ++e) x[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], q[e][k], x[e], 0, 0, 0);
     };
-    // What scores need before their exponentials: scales, mask, and a reference that follows the largest score when that has risen by kLag.
-    float vs[2] = {1.f, 1.f};
-    auto settle = [&](auto fast, int step, float16v (&x)[NB]) __attribute__((always_inline)) {
-        if constexpr (FP8) {   // one scale to 16 keys: they are in eight accumulators
+    // What scores need before their exponentials: scales (one to 16 keys: they are in eight accumulators), mask, the largest of each row, and a reference that
+    // follows it when it has risen by kLag.
+    float vs[2] = {1.f, 1.f}, vs_next[2] = {1.f, 1.f}, ks_next[2] = {1.f, 1.f};   // of this step's values, of the next step's values and keys
+    int sid[2] = {0, 0};                                                           // blocks of the step whose scales are read next
+    auto scales = [&](int step) __attribute__((always_inline)) {
+        if constexpr (FP8)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int64_t tile = (int64_t)block_id(step, j) * a.num_kv_heads + g;
-                const float ks = k_scales[tile] * c;
-                vs[j] = v_scales[tile];
-#pragma unroll
-                for (int e = 0; e < NB; ++e)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[e][j * 8 + i] *= ks;
+                const int64_t tile = (int64_t)sid[j] * a.num_kv_heads + g;
+                ks_next[j] = k_scales[tile] * c;
+                vs_next[j] = v_scales[tile];
+                sid[j] = block_id(step + 1, j);
             }
-        }
-        if (!decltype(fast)::value && step >= all) {
+    };
+    // The largest of a row's 16 scores in the lane, in eight parts; the scores are scaled and masked on the way.
+    auto largest = [&](auto masked, int step, int e, float16v &x, int part, float top) __attribute__((always_inline)) {
+        const int lo = part ? 2 * part + 1 : 0, hi = part < 7 ? 2 * part + 3 : 16;
+        const int seen = lim[e] - step * kKeys - 4 * half;    // keys up to this one, counted from the lane's first
 #pragma unroll
-            for (int e = 0; e < NB; ++e) {
-                const int seen = lim[e] - step * kKeys - 4 * half;    // keys up to this one, counted from the lane's first
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (i / 4 * 8 + i % 4 > seen) x[e][i] = -__builtin_inff();
-            }
+        for (int i = lo; i < hi; ++i) {
+            if constexpr (FP8) x[i] *= ks_next[i / 8];
+            if constexpr (decltype(masked)::value)
+                if (i / 4 * 8 + i % 4 > seen) x[i] = -__builtin_inff();
         }
-        float top[NB];
+        if (part == 0) return max3(x[0], x[1], x[2]);
+        return part < 7 ? max3(top, x[lo], x[lo + 1]) : __builtin_elementwise_maximum(top, x[15]);
+    };
+    auto whole_row = [&](float top) __attribute__((always_inline)) { return FP8 ? max_of_halves(top) : max_of_halves(top) * c; };
+    auto follow = [&](const float (&top)[NB]) __attribute__((always_inline)) {
         bool rise = false;
 #pragma unroll
-        for (int e = 0; e < NB; ++e) {
-            float t = max3(x[e][0], x[e][1], x[e][2]);
-#pragma unroll
-            for (int i = 3; i < 15; i += 2) t = max3(t, x[e][i], x[e][i + 1]);
-            t = max_of_halves(__builtin_elementwise_maximum(t, x[e][15]));
-            top[e] = FP8 ? t : t * c;
-            rise = rise || top[e] > m[e] + kLag;
-        }
-        if (__ballot(rise)) {
+        for (int e = 0; e < NB; ++e) rise = rise || top[e] > m[e] + kLag;
+        if (__builtin_expect(__ballot(rise) != 0, 0)) {
 #pragma unroll
             for (int e = 0; e < NB; ++e) {
                 const float up = fmaxf(m[e], top[e]), down = __builtin_amdgcn_exp2f(m[e] - up);
@@ -282,26 +291,25 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
             }
         }
     };
-    auto weights = [&](float16v &x, int e, bf16x8 (&pk)[2]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float p = __builtin_amdgcn_exp2f(FP8 ? x[i] - m[e] : __builtin_fmaf(x[i], c, -m[e]));
-            l[e] += p;
-            x[i] = FP8 ? p * vs[i / 8] : p;
+    // Score j of the lane's 16 NB on its way to a weight: the exponents of the next one, its exponential, the sum and the rounding of those in front of it.
+    auto advance = [&](float16v (&x)[NB], int j, bf16x8 (&pk)[NB][2]) __attribute__((always_inline)) {
+        auto exponent = [&](int i) __attribute__((always_inline)) {
+            const float v = x[i / 16][i % 16];
+            x[i / 16][i % 16] = FP8 ? v - m[i / 16] : __builtin_fmaf(v, c, -m[i / 16]);
+        };
+        if (j == 0) exponent(0);
+        if (j + 1 < 16 * NB) exponent(j + 1);
+        if (j < 16 * NB) x[j / 16][j % 16] = __builtin_amdgcn_exp2f(x[j / 16][j % 16]);
+        if (j > 0) {
+            const int i = j - 1;
+            l[i / 16] += x[i / 16][i % 16];
+            if constexpr (FP8) x[i / 16][i % 16] *= vs[i % 16 / 8];
+            if (i % 2) {
+                u32x4 w = __builtin_bit_cast(u32x4, pk[i / 16][i % 16 / 8]);
+                w[i % 8 / 2] = pack_bf16(x[i / 16][i % 16 - 1], x[i / 16][i % 16]);
+                pk[i / 16][i % 16 / 8] = __builtin_bit_cast(bf16x8, w);
+            }
         }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            u32x4 w;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = pack_bf16(x[k * 8 + 2 * j], x[k * 8 + 2 * j + 1]);
-            pk[k] = __builtin_bit_cast(bf16x8, w);
-        }
-    };
-    auto output = [&](const bf16x8 (&vf)[2][DB], const bf16x8 (&pk)[2], int e) __attribute__((always_inline)) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int b = 0; b < DB; ++b) o[e][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k][b], pk[k], o[e][b], 0, 0, 0);
     };
     auto add_odd = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
@@ -328,53 +336,101 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
     // FAST: every row of the tile sees all that is in LDS (what would be read behind the share's last step is read as well, from the last block).
     // k_read: the tile of step t + 2's keys, v_read: of step t's values; k_next, v_next: those that are free after the meeting.
     bf16x8 kf[KS];
-    auto step_of = [&](auto fast, auto parity, int t, float16v (&x)[NB], float16v (&y)[NB], Tile<D> &k_read, Tile<D> &v_read, Tile<D> &k_next, Tile<D> &v_next,
-                       int pair) __attribute__((always_inline)) {
-        constexpr bool FAST = decltype(fast)::value, ODD = decltype(parity)::value;
-        const bool live = FAST || t < none, next = FAST || t + 1 < none, next2 = FAST || t + 2 < none;
-        bf16x8 vf[2][DB], pk[2];
-        if (live) read_values(v_read, ODD, vf);
-        if (next) scores(kf, y);
-        if (live) weights(x[0], 0, pk);
-        if constexpr (ODD) {
-            if constexpr (FP8) put(in_v, pair ? v_even : v_odd, wave);
-            const int vstep = t + 1 + (wave >> 1);   // of the values that this wavefront has brought
-            if (!FAST && vstep >= full) {
-                if constexpr (!FP8) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
-                clean(vstep, pair ? v_even : v_odd, pair ^ 1);
-            }
-            team_barrier<!FP8>();
-            bring(a.k, block_id(t + 4, wave), k_next, wave, in_k);
-            bring(a.v, block_id(t + 3, wave), v_next, wave, in_v);
-        } else {
-            put(in_k, pair ? k_odd : k_even, wave);
+    int kid = 0, vid = 0;   // this wavefront's blocks to bring next
+    // the meeting of the wavefronts; dirty: values of theirs have to be cleaned in front of it
+    auto meet = [&](bool dirty, int t, Tile<D> &v_new, int pair) __attribute__((always_inline)) {
+        if constexpr (FP8) put(in_v, v_new, wave);
+        const int vstep = t + 1 + (wave >> 1);   // of the values that this wavefront has brought
+        if (dirty && vstep >= full) {
+            if constexpr (!FP8) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+            clean(vstep, v_new, pair);
         }
-        if (next2) read_keys(k_read, !ODD, kf);
-        if (live) {
-            output(vf, pk, 0);
-            if constexpr (NB == 2) {
-                bf16x8 pk1[2];
-                weights(x[1], 1, pk1);
-                output(vf, pk1, 1);
-            }
-            if (!FAST && t >= full && (odd_flags[pair][2 * ODD] | odd_flags[pair][2 * ODD + 1])) add_odd(t);
-        }
-        if (next) settle(fast, t + 1, y);
+        team_barrier<!FP8>();
     };
-    auto four_steps = [&](auto fast, int t, float16v (&x)[NB], float16v (&y)[NB]) __attribute__((always_inline)) {
-        constexpr bool FAST = decltype(fast)::value;
-        step_of(fast, std::false_type{}, t, x, y, k_odd, v_even, k_even, v_even, 0);
-        if (FAST || t + 1 < end) step_of(fast, std::true_type{}, t + 1, y, x, k_even, v_even, k_odd, v_even, 0);
-        if (FAST || t + 2 < end) step_of(fast, std::false_type{}, t + 2, x, y, k_even, v_odd, k_odd, v_odd, 1);
-        if (FAST || t + 3 < end) step_of(fast, std::true_type{}, t + 3, y, x, k_odd, v_odd, k_even, v_odd, 1);
+    auto step_of = [&](auto masked, auto parity, int t, float16v (&x)[NB], float16v (&y)[NB], Tile<D> &k_read, Tile<D> &v_read, Tile<D> &k_new, Tile<D> &v_new,
+                       Tile<D> &k_next, Tile<D> &v_next, int pair) __attribute__((always_inline)) {
+        // Both parts are as many matrix instructions and between them, in this order, what the vector unit and LDS have to do: the first EXPS of the 16 NB
+        // exponentials and the values' operands (in its first half), the others, the next keys' operands (in its first half) and the largest scores.
+        constexpr bool ODD = decltype(parity)::value, MASKED = decltype(masked)::value;
+        constexpr int M1 = NB * KS, M2 = NB * 2 * DB, ELS = 16 * NB, EXPS = NB == 2 ? 20 : 12, LAST = NB == 2 ? M2 * 3 / 4 : M2 / 2, FRAGS = 2 * DB;
+        constexpr auto least = [](int u, int v) { return u < v ? u : v; };
+        constexpr auto exps_by = [](int i) { return i == 0 ? EXPS : i >= LAST ? ELS + 1 : EXPS + i * (ELS - EXPS) / LAST; };
+        // (two blocks of rows: over half of a part; one, which has fewer registers: each takes the place of one that has been used)
+        constexpr auto values_by = [least](int i) { return least(FRAGS, NB * i * FRAGS / M1); };
+        constexpr auto keys_by = [least](int i) { return least(KS, NB * i * KS / M2); };
+        constexpr auto parts_by = [](int i) { return i <= 2 ? 0 : (i - 2) * 8 * NB / (M2 - 2); };
+        bf16x8 vf[2][DB], pk[NB][2];
+        __builtin_amdgcn_sched_barrier(0);
+        each<0, M1>([&](auto number) __attribute__((always_inline)) {
+            constexpr int I = decltype(number)::value, E = I % NB, K = I / NB;
+            if constexpr (K == 0)
+#pragma unroll
+                for (int z = 0; z < 16; ++z) y[E][z] = 0.f;
+            y[E] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[K], q[E][K], y[E], 0, 0, 0);
+            each<values_by(I), values_by(I + 1)>([&](auto f) __attribute__((always_inline)) { vf[f / DB][f % DB] = read_values(v_read, ODD, f / DB, f % DB); });
+            each<I * EXPS / M1, (I + 1) * EXPS / M1>([&](auto j) __attribute__((always_inline)) { advance(x, j, pk); });
+            if constexpr (I == M1 / 2) {   // (scalar loads, which whoever waits for LDS waits for: where nothing is waited for until the second part)
+                if constexpr (!ODD) {
+                    kid = block_id(t + 5, wave);
+                    vid = block_id(t + 4, wave);
+                }
+                scales(t + 1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if constexpr (ODD) meet(MASKED, t, v_new, pair ^ 1);
+        else put(in_k, k_new, wave);
+        const char *k_block = block_at(k_base, kid), *v_block = block_at(v_base, vid);
+        float top[NB];
+        __builtin_amdgcn_sched_barrier(0);
+        each<0, M2>([&](auto number) __attribute__((always_inline)) {
+            constexpr int I = decltype(number)::value, E = I / FRAGS, F = I % FRAGS;
+            each<exps_by(I), exps_by(I + 1)>([&](auto j) __attribute__((always_inline)) { advance(x, j, pk); });
+            o[E][F % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[F / DB][F % DB], pk[E][F / DB], o[E][F % DB], 0, 0, 0);
+            each<keys_by(I), keys_by(I + 1)>([&](auto f) __attribute__((always_inline)) { kf[f] = read_keys(k_read, !ODD, f); });
+            if constexpr (ODD)
+                each<least(2 * LOADS, 2 * I * 2 * LOADS / M2), least(2 * LOADS, 2 * (I + 1) * 2 * LOADS / M2)>([&](auto i) __attribute__((always_inline)) {
+                    if constexpr (i < LOADS) bring_part(k_block, i, k_next, wave, in_k);
+                    else bring_part(v_block, i - LOADS, v_next, wave, in_v);
+                });
+            each<parts_by(I), parts_by(I + 1)>([&](auto part) __attribute__((always_inline)) {
+                top[part / 8] = largest(masked, t + 1, part / 8, y[part / 8], part % 8, top[part / 8]);
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if (MASKED && t >= full && (odd_flags[pair][2 * ODD] | odd_flags[pair][2 * ODD + 1])) add_odd(t);
+#pragma unroll
+        for (int e = 0; e < NB; ++e) top[e] = whole_row(top[e]);
+        follow(top);
+        vs[0] = vs_next[0];
+        vs[1] = vs_next[1];
+    };
+    // a wavefront without rows
+    auto idle_step = [&](auto parity, int t, Tile<D> &k_new, Tile<D> &v_new, Tile<D> &k_next, Tile<D> &v_next, int pair) __attribute__((always_inline)) {
+        if constexpr (decltype(parity)::value) {
+            meet(true, t, v_new, pair ^ 1);
+            bring(k_base, kid, k_next, wave, in_k);
+            bring(v_base, vid, v_next, wave, in_v);
+        } else {
+            put(in_k, k_new, wave);
+            kid = block_id(t + 5, wave);
+            vid = block_id(t + 4, wave);
+        }
+    };
+    auto four_steps = [&](auto masked, int t, float16v (&x)[NB], float16v (&y)[NB]) __attribute__((always_inline)) {
+        constexpr bool MASKED = decltype(masked)::value;   // (the others are not near the share's end)
+        step_of(masked, std::false_type{}, t, x, y, k_odd, v_even, k_even, v_odd, k_odd, v_even, 0);
+        if (!MASKED || t + 1 < end) step_of(masked, std::true_type{}, t + 1, y, x, k_even, v_even, k_even, v_odd, k_odd, v_even, 0);
+        if (!MASKED || t + 2 < end) step_of(masked, std::false_type{}, t + 2, x, y, k_even, v_odd, k_odd, v_even, k_even, v_odd, 1);
+        if (!MASKED || t + 3 < end) step_of(masked, std::true_type{}, t + 3, y, x, k_odd, v_odd, k_odd, v_even, k_even, v_odd, 1);
     };
 
     if (first < end) {
         // keys of the first three steps, values of the first two
         u32x4 in_0[FP8 ? LOADS : 1];
-        if (wave < 2) bring(a.k, block_id(first, wave), k_even, 2 + wave, in_0);
-        bring(a.k, block_id(first + 1, wave), k_odd, wave, in_k);
-        bring(a.v, block_id(first, wave), v_even, wave, in_v);
+        if (wave < 2) bring(k_base, block_id(first, wave), k_even, 2 + wave, in_0);
+        bring(k_base, block_id(first + 1, wave), k_odd, wave, in_k);
+        bring(v_base, block_id(first, wave), v_even, wave, in_v);
         if (wave < 2) put(in_0, k_even, 2 + wave);
         put(in_k, k_odd, wave);
         put(in_v, v_even, wave);
@@ -383,20 +439,44 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
             clean(first + (wave >> 1), v_even, 0);
         }
         team_barrier<!FP8>();
-        float16v x[NB], y[NB];
-        if (first < none) {
-            read_keys(k_even, 1, kf);
+        if (n_first < rows) {
+            float16v x[NB], y[NB];
+#pragma unroll
+            for (int k = 0; k < KS; ++k) kf[k] = read_keys(k_even, 1, k);
+            if constexpr (FP8) {
+                sid[0] = block_id(first, 0);
+                sid[1] = block_id(first, 1);
+            }
+            scales(first);
             scores(kf, x);
-            settle(std::false_type{}, first, x);
+            float top[NB];
+#pragma unroll
+            for (int e = 0; e < NB; ++e) {
+                each<0, 8>([&](auto part) __attribute__((always_inline)) { top[e] = largest(std::true_type{}, first, e, x[e], part, top[e]); });
+                top[e] = whole_row(top[e]);
+            }
+            follow(top);
+            vs[0] = vs_next[0];
+            vs[1] = vs_next[1];
+#pragma unroll
+            for (int k = 0; k < KS; ++k) kf[k] = read_keys(k_odd, 0, k);
+            team_barrier<false>();   // (new keys come to where these were)
+            bring(k_base, block_id(first + 3, wave), k_even, wave, in_k);
+            bring(v_base, block_id(first + 2, wave), v_odd, wave, in_v);
+            int t = first;
+            for (const int fast_end = min(full, end) - 5; t < fast_end; t += 4) four_steps(std::false_type{}, t, x, y);
+            for (; t < end; t += 4) four_steps(std::true_type{}, t, x, y);
+        } else {
+            team_barrier<false>();
+            bring(k_base, block_id(first + 3, wave), k_even, wave, in_k);
+            bring(v_base, block_id(first + 2, wave), v_odd, wave, in_v);
+            for (int t = first; t < end; t += 4) {
+                idle_step(std::false_type{}, t, k_even, v_odd, k_odd, v_even, 0);
+                if (t + 1 < end) idle_step(std::true_type{}, t + 1, k_even, v_odd, k_odd, v_even, 0);
+                if (t + 2 < end) idle_step(std::false_type{}, t + 2, k_odd, v_even, k_even, v_odd, 1);
+                if (t + 3 < end) idle_step(std::true_type{}, t + 3, k_odd, v_even, k_even, v_odd, 1);
+            }
         }
-        if (first + 1 < none) read_keys(k_odd, 0, kf);
-        team_barrier<false>();   // (new keys come to where these were)
-        bring(a.k, block_id(first + 3, wave), k_even, wave, in_k);
-        bring(a.v, block_id(first + 2, wave), v_odd, wave, in_v);
-        int t = first;
-        if (none > 0)   // (a wavefront without rows only brings keys and values)
-            for (const int fast_end = min(full, end) - 5; t < fast_end; t += 4) four_steps(std::true_type{}, t, x, y);
-        for (; t < end; t += 4) four_steps(std::false_type{}, t, x, y);
         if constexpr (!FP8) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): nothing is on its way into LDS when the workgroup ends
     }
 
