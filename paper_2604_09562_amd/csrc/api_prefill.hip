@@ -68,32 +68,31 @@ ChunkShape chunk_shape(bool mfma, int batch, int max_blocks, int num_q_heads, in
     ChunkShape s;
     const int64_t G = num_q_heads / num_kv_heads;
     s.rows = mfma ? (getenv("SS_NB") ? atoi(getenv("SS_NB")) : 2) * kChunkRows : kChunkRowsF32;
-    s.target = mfma && s.rows > kChunkRows ? chunk_target() / 2 : chunk_target();
-    s.tiles = (int64_t)total_rows * G / s.rows + (batch < total_rows ? batch : total_rows);
-    const int64_t steps = ((int64_t)max_blocks * SS_BLOCK_SIZE + kStepKeys - 1) / kStepKeys, pieces = (steps + kMinPiece - 1) / kMinPiece;
-    const int64_t most = s.tiles * pieces * num_kv_heads, fit = 2ll * s.target;
-    s.cap = pieces < 2 ? 0 : (int32_t)(most < fit ? most : fit);
+    const int64_t wgs = chunk_target() / (s.rows > kChunkRows ? 2 : 1), tiles = (int64_t)total_rows * G / s.rows + (batch < total_rows ? batch : total_rows);
+    // as many spans as workgroups run at a time, if there can be work enough
+    const int64_t keys = mfma ? kChunkKeys : kChunkKeysF32, steps = ((int64_t)max_blocks * SS_BLOCK_SIZE + keys - 1) / keys;
+    const int64_t most = tiles * ((steps + kMinPiece - 1) / kMinPiece), each = wgs > num_kv_heads ? wgs / num_kv_heads : 1;
+    s.spans = (int32_t)(most < each ? (most < 1 ? 1 : most) : each);
+    s.cap = s.spans > 1 ? 2 * s.spans * num_kv_heads : 0;
     return s;
 }
 
-// A wavefront of either kernel is one of two on a SIMD, four make a workgroup.
+// A wavefront is one of two on a SIMD (tiles of 128 rows, fp32), four make a workgroup.
 int chunk_target() { return attn_chip_waves() / 2; }
 
 size_t chunk_workspace_bytes(const ChunkShape &s, int head_dim)
 {
-    return 256 + align_up(sizeof(int32_t) * kChunkRecInts * ((size_t)s.cap / 2 + 1), 256) + align_up((size_t)s.cap * s.rows * 2 * sizeof(float), 256) +
+    return align_up(sizeof(int32_t) * kChunkRecInts * (size_t)s.spans, 256) + align_up((size_t)s.cap * s.rows * 2 * sizeof(float), 256) +
            (size_t)s.cap * s.rows * head_dim * sizeof(float);
 }
 
 void chunk_carve(ChunkArgs &a, const ChunkShape &s, void *workspace)
 {
     char *w = static_cast<char *>(workspace);
-    a.target = s.target;
+    a.spans = s.spans;
     a.cap = s.cap;
-    a.head = reinterpret_cast<int32_t *>(w);
-    w += 256;
     a.rec = reinterpret_cast<int32_t *>(w);
-    w += align_up(sizeof(int32_t) * kChunkRecInts * ((size_t)s.cap / 2 + 1), 256);
+    w += align_up(sizeof(int32_t) * kChunkRecInts * (size_t)s.spans, 256);
     a.part_ml = reinterpret_cast<float *>(w);
     w += align_up((size_t)s.cap * s.rows * 2 * sizeof(float), 256);
     a.part_o = reinterpret_cast<float *>(w);
@@ -186,7 +185,6 @@ int32_t ss_chunk_attn(const ss_paged_kv *kv, const ss_batch *batch, const void *
     if (!(sm_scale > 0.0f) || sm_scale > 3.4e38f) return fail(SS_ERR_INVALID_ARG, "sm_scale must be positive and finite");
     const bool mfma = chunk_mfma_supported(kv->head_dim, kv->dtype, q_dtype);
     const ChunkShape s = chunk_shape(mfma, batch->batch, batch->max_blocks_per_seq, num_q_heads, kv->num_kv_heads, total_rows);
-    if ((s.tiles * kv->num_kv_heads + s.cap) > 0x7fffffffll / 4) return fail(SS_ERR_UNSUPPORTED, "too many rows for one launch");
     const size_t need = chunk_workspace_bytes(s, kv->head_dim);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return fail(SS_ERR_INVALID_ARG, "workspace must be a 256-byte aligned device buffer");
     if (workspace_bytes < need) return fail(SS_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
@@ -202,7 +200,7 @@ int32_t ss_chunk_attn(const ss_paged_kv *kv, const ss_batch *batch, const void *
     a.block_table = batch->block_table; a.kv_len = batch->kv_len; a.q_indptr = batch->q_indptr;
     a.q = q; a.q_stride = q_stride; a.out = out; a.lse = lse; a.q_dtype = q_dtype; a.num_q_heads = num_q_heads; a.sm_scale = sm_scale;
     chunk_carve(a, s, workspace);
-    return mfma ? chunk_mfma_launch(a, s, static_cast<hipStream_t>(stream)) : chunk_f32_launch(a, s, static_cast<hipStream_t>(stream));
+    return mfma ? chunk_mfma_launch(a, s.rows, static_cast<hipStream_t>(stream)) : chunk_f32_launch(a, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

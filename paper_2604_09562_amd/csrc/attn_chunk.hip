@@ -67,7 +67,10 @@ __device__ __forceinline__ void each(F &&f)
     }
 }
 
-constexpr int kKeys = 32;    // keys that are taken at a time, two cache blocks
+constexpr int kKeys = kChunkKeys;   // keys that are taken at a time, two cache blocks
+// What a tile costs beside its steps, in steps.
+template <int NB>
+constexpr int kOpen = NB == 2 ? 6 : 8;
 constexpr int kPairKeys = 2 * kKeys;
 
 // 64 keys or values in LDS, rows of D bf16 in pieces of 16 bytes.  Piece c of row t stands at place c ^ turn(t): 16 rows' pieces
@@ -92,24 +95,27 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
     // Variables of their own: a tile's reads then do not wait for what is on its way into another one.
     __shared__ Tile<D> k_even, k_odd, v_even, v_odd;   // steps 3, 4, 7, 8, ..; 1, 2, 5, 6, ..; 0, 1, 4, 5, ..; 2, 3, 6, 7, .. (from the first)
     __shared__ int odd_flags[2][kWaves];
-    const int g = blockIdx.x % a.num_kv_heads, item = blockIdx.x / a.num_kv_heads;
-    ChunkShare s;
-    const bool any = chunk_share<ROWS>(a, item, s);
-    if (a.cap > 0 && blockIdx.x == 0 && threadIdx.x == 0) a.head[0] = s.cuts;
-    if (!any) return;
-    chunk_record<ROWS>(a, s, g);
+    const int g = blockIdx.x % a.num_kv_heads, span = blockIdx.x / a.num_kv_heads;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    ChunkWalk<ROWS, kKeys, kOpen<NB>> s;
+    int begun = 0, begun_q0 = 0, begun_rows = 0, begun_row0 = 0;   // of the tile that the span begins and does not end
+    for (bool any = s.begin(a, span); any; any = s.next(a)) {
+    if (s.part == 2 * span + 1) {
+        begun = s.pieces();
+        begun_q0 = s.u.q0;
+        begun_rows = s.u.q_len * s.u.G;
+        begun_row0 = s.t * ROWS;
+    }
     const int r32 = lane & 31, half = lane >> 5;
     const int G = a.num_q_heads / a.num_kv_heads;
-    const int rows = s.q_len * G, ctx = s.kv_len - s.q_len;
-    const int n_first = s.tile * ROWS + wave * 32 * NB;
+    const int rows = s.u.q_len * G, ctx = s.u.kv_len - s.u.q_len;
+    const int n_first = s.t * ROWS + wave * 32 * NB;
     int lim[NB];                                                        // the last position this lane's rows see
 #pragma unroll
     for (int e = 0; e < NB; ++e) lim[e] = ctx + min(n_first + e * 32 + r32, rows - 1) / G;
     // In steps of 32 keys: the share's, and up to where all rows of the tile see everything
-    const int first = s.s0 * (kStepKeys / kKeys);
-    const int end = min(s.s1 * (kStepKeys / kKeys), (max(ctx + min((s.tile + 1) * ROWS - 1, rows - 1) / G + 1, 0) + kKeys - 1) / kKeys);
-    const int full = max((ctx + s.tile * ROWS / G + 1) / kKeys, 0);
+    const int first = s.s0, end = s.s1;
+    const int full = max((ctx + s.t * ROWS / G + 1) / kKeys, 0);
     const float c = a.sm_scale * kLog2e;
 #pragma unroll
     for (int e = 0; e < NB; ++e) lim[e] = min(lim[e], end * kKeys - 1);   // (what a step reads behind the share is another one's)
@@ -118,7 +124,7 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
 #pragma unroll
     for (int e = 0; e < NB; ++e) {
         const int n = n_first + e * 32 + r32;
-        const char *src = static_cast<const char *>(a.q) + ((int64_t)(s.q0 + min(n, rows - 1) / G) * a.q_stride + (int64_t)(g * G + n % G) * D + half * 8) * 2;
+        const char *src = static_cast<const char *>(a.q) + ((int64_t)(s.u.q0 + min(n, rows - 1) / G) * a.q_stride + (int64_t)(g * G + n % G) * D + half * 8) * 2;
         const u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
@@ -132,7 +138,7 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
     typedef const __attribute__((address_space(4))) float *scalar_floats;
     const scalar_ints table = (scalar_ints)(uintptr_t)(block_table + (int64_t)s.b * a.max_blocks);
     const scalar_floats k_scales = (scalar_floats)(uintptr_t)k_scale, v_scales = (scalar_floats)(uintptr_t)v_scale;
-    const int last_block = (int)(((unsigned)s.kv_len + kTile - 1) / kTile) - 1;
+    const int last_block = (int)(((unsigned)s.u.kv_len + kTile - 1) / kTile) - 1;
     // block j of a step (the last block again where there is none: what stands there is masked)
     auto block_id = [&](int step, int j) __attribute__((always_inline)) { return table[min(step * 2 + j, last_block)]; };
     const uint32_t block_stride = (uint32_t)a.num_kv_heads * BLOCK_BYTES;
@@ -194,7 +200,7 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
             const int p = i * 64 + lane, t = p / PIECES;
             u32x4 &at = tile.w[wave * kTile + t][p % PIECES];
             u32x4 w = at;
-            const bool dead = step * kKeys + (wave & 1) * kTile + t >= s.kv_len;
+            const bool dead = step * kKeys + (wave & 1) * kTile + t >= s.u.kv_len;
             bool changed = dead;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -484,8 +490,8 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
     for (int e = 0; e < NB; ++e) {
         const int n = n_first + e * 32 + r32;
         const float sum = sum_of_halves(l[e]);
-        if (s.pieces > 1) {
-            const int64_t part = (int64_t)s.slot * a.num_kv_heads + g;
+        if (s.part >= 0) {
+            const int64_t part = (int64_t)s.part * a.num_kv_heads + g;
             float4v *po = reinterpret_cast<float4v *>(a.part_o) + part * (ROWS * D / 4) + (wave * NB + e) * (32 * D / 4) + lane;
 #pragma unroll
             for (int b = 0; b < DB; ++b)
@@ -497,7 +503,7 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
                 ml[1] = sum;
             }
         } else if (n < rows) {
-            const int64_t at = (int64_t)(s.q0 + n / G) * a.num_q_heads + g * G + n % G;
+            const int64_t at = (int64_t)(s.u.q0 + n / G) * a.num_q_heads + g * G + n % G;
             const float r = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;   // (a row that sees nothing: zeros; NaN stays)
 #pragma unroll
             for (int b = 0; b < DB; ++b)
@@ -508,27 +514,23 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
             if (a.lse && half == 0) a.lse[at] = sum == 0.f ? -__builtin_inff() : (m[e] + __builtin_amdgcn_logf(sum)) * kLn2;
         }
     }
+    team_barrier<false>();   // (the next tile's keys come to where the others may still read)
+    }
+    chunk_record(a, span, g, begun, begun_q0, begun_rows, begun_row0);
 }
 
 template <int D, bool FP8, int NB>
-int32_t launch(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream)
+int32_t launch(const ChunkArgs &a, hipStream_t stream)
 {
-    constexpr int ROWS = 128 * NB;
-    const int64_t shares = s.tiles + s.cap / a.num_kv_heads;
-    hipLaunchKernelGGL((chunk_kernel<D, FP8, NB>), dim3((unsigned)(shares * a.num_kv_heads)), dim3(64 * kWaves), 0, stream, a, a.block_table, a.k_scale, a.v_scale);
+    hipLaunchKernelGGL((chunk_kernel<D, FP8, NB>), dim3((unsigned)(a.spans * a.num_kv_heads)), dim3(64 * kWaves), 0, stream, a, a.block_table, a.k_scale, a.v_scale);
     SS_HIP_CHECK(hipGetLastError(), "launch chunk_kernel");
-    if (s.cap >= 2 * a.num_kv_heads) {
-        const int64_t fit = s.cap / (2 * a.num_kv_heads), cuts = s.tiles < fit ? s.tiles : fit;
-        hipLaunchKernelGGL((chunk_merge_kernel<ROWS, 32, D, SS_BF16>), dim3((unsigned)(cuts * a.num_kv_heads * (ROWS * D / 1024))), dim3(256), 0, stream, a);
-        SS_HIP_CHECK(hipGetLastError(), "launch chunk_merge_kernel");
-    }
-    return SS_OK;
+    return chunk_merge_launch<128 * NB, 32, D, SS_BF16>(a, stream);
 }
 
 template <int D, bool FP8>
-int32_t launch_rows(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream)
+int32_t launch_rows(const ChunkArgs &a, int rows, hipStream_t stream)
 {
-    return s.rows == 256 ? launch<D, FP8, 2>(a, s, stream) : launch<D, FP8, 1>(a, s, stream);
+    return rows > kChunkRows ? launch<D, FP8, 2>(a, stream) : launch<D, FP8, 1>(a, stream);
 }
 
 }  // namespace
@@ -538,11 +540,11 @@ bool chunk_mfma_supported(int head_dim, int kv_dtype, int q_dtype)
     return (head_dim == 64 || head_dim == 128) && q_dtype == SS_BF16 && (kv_dtype == SS_BF16 || kv_dtype == SS_FP8_E4M3);
 }
 
-int32_t chunk_mfma_launch(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream)
+int32_t chunk_mfma_launch(const ChunkArgs &a, int rows, hipStream_t stream)
 {
     const bool fp8 = a.kv_dtype == SS_FP8_E4M3;
-    if (a.head_dim == 128) return fp8 ? launch_rows<128, true>(a, s, stream) : launch_rows<128, false>(a, s, stream);
-    return fp8 ? launch_rows<64, true>(a, s, stream) : launch_rows<64, false>(a, s, stream);
+    if (a.head_dim == 128) return fp8 ? launch_rows<128, true>(a, rows, stream) : launch_rows<128, false>(a, rows, stream);
+    return fp8 ? launch_rows<64, true>(a, rows, stream) : launch_rows<64, false>(a, rows, stream);
 }
 
 }  // namespace ss

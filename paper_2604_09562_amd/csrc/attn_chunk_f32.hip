@@ -17,7 +17,7 @@ typedef float float2v __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kRows = kChunkRowsF32, kWaves = 4;
+constexpr int kRows = kChunkRowsF32, kWaves = 4, kStepKeys = kChunkKeysF32, kOpen = 3;
 
 // four consecutive elements (from a multiple of four) as fp32
 template <int DT>
@@ -41,24 +41,28 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
     constexpr int PAD = D + 4, PIECES = kStepKeys * D / 4 / (64 * kWaves);   // fours of a step's keys to a thread
     __shared__ float ks[kStepKeys][PAD];
     __shared__ float vs[kStepKeys][PAD];
-    const int g = blockIdx.x % a.num_kv_heads, item = blockIdx.x / a.num_kv_heads;
-    ChunkShare s;
-    const bool any = chunk_share<kRows>(a, item, s);
-    if (a.cap > 0 && blockIdx.x == 0 && threadIdx.x == 0) a.head[0] = s.cuts;
-    if (!any) return;
-    chunk_record<kRows>(a, s, g);
+    const int g = blockIdx.x % a.num_kv_heads, span = blockIdx.x / a.num_kv_heads;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    ChunkWalk<kRows, kStepKeys, kOpen> s;
+    int begun = 0, begun_q0 = 0, begun_rows = 0, begun_row0 = 0;
+    for (bool any = s.begin(a, span); any; any = s.next(a)) {
+    if (s.part == 2 * span + 1) {
+        begun = s.pieces();
+        begun_q0 = s.u.q0;
+        begun_rows = s.u.q_len * s.u.G;
+        begun_row0 = s.t * kRows;
+    }
     const int n16 = lane & 15, jq = lane >> 4;
     const int G = a.num_q_heads / a.num_kv_heads;
-    const int rows = s.q_len * G, n = s.tile * kRows + wave * 16 + n16;
+    const int rows = s.u.q_len * G, n = s.t * kRows + wave * 16 + n16;
     const int qi = min(n, rows - 1) / G, hh = n % G;
-    const int lim = s.kv_len - s.q_len + qi;                     // the last position this lane's row sees
-    const int64_t at = (int64_t)(s.q0 + qi) * a.num_q_heads + g * G + hh;
+    const int lim = s.u.kv_len - s.u.q_len + qi;                     // the last position this lane's row sees
+    const int64_t at = (int64_t)(s.u.q0 + qi) * a.num_q_heads + g * G + hh;
     float4v q[D / 16];   // B operand: d = 16 c + 4 jq ..
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
         q[c] = float4v{0.f, 0.f, 0.f, 0.f};
-        if (n < rows) q[c] = load4<QDT>(a.q, (int64_t)(s.q0 + qi) * a.q_stride + (int64_t)(g * G + hh) * D + 16 * c + 4 * jq);
+        if (n < rows) q[c] = load4<QDT>(a.q, (int64_t)(s.u.q0 + qi) * a.q_stride + (int64_t)(g * G + hh) * D + 16 * c + 4 * jq);
     }
     // scores are taken to powers of two; the factor in two parts, since fp32 holds it to 2^-24 of a score's size only
     const double c64 = (double)a.sm_scale * 1.4426950408889634;
@@ -71,7 +75,7 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
 
     // Steps from `full` on hold keys that some row of the tile does not see.  There a value that is not finite is taken out of the product, in
     // which it would reach every row (0 * inf), and added to the rows that see it.
-    const int full = max((s.kv_len - s.q_len + s.tile * kRows / G + 1) / kStepKeys, 0);
+    const int full = max((s.u.kv_len - s.u.q_len + s.t * kRows / G + 1) / kStepKeys, 0);
     for (int step = s.s0; step < s.s1; ++step) {
         bool odd = false;
         __syncthreads();
@@ -80,7 +84,7 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
             const int e = i * 64 * kWaves + tid, t = e / (D / 4), d = e % (D / 4) * 4;
             const int pos = step * kStepKeys + t;
             float4v k = {0.f, 0.f, 0.f, 0.f}, v = k;
-            if (pos < s.kv_len) {   // what stands behind the last token is of no one
+            if (pos < s.u.kv_len) {   // what stands behind the last token is of no one
                 const int64_t tile = (int64_t)table[pos / kTile] * a.num_kv_heads + g, from = (tile * kTile + pos % kTile) * D + d;
                 k = load4<KV>(a.k, from);
                 v = load4<KV>(a.v, from);
@@ -152,8 +156,8 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (s.pieces > 1) {
-        const int64_t part = (int64_t)s.slot * a.num_kv_heads + g;
+    if (s.part >= 0) {
+        const int64_t part = (int64_t)s.part * a.num_kv_heads + g;
         float4v *po = reinterpret_cast<float4v *>(a.part_o) + part * (kRows * D / 4) + wave * (16 * D / 4) + lane;
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) po[c * 64] = o[c];
@@ -162,45 +166,42 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
             ml[0] = m;
             ml[1] = l;
         }
-        return;
+        continue;
     }
-    if (n >= rows) return;
-    const float r = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
+    if (n < rows) {   // (the walk takes whole wavefronts)
+        const float r = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) chunk_store4<QDT>(a.out, at * D + 16 * c + 4 * jq, o[c] * r);
-    if (a.lse && jq == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+        for (int c = 0; c < D / 16; ++c) chunk_store4<QDT>(a.out, at * D + 16 * c + 4 * jq, o[c] * r);
+        if (a.lse && jq == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    }
+    }
+    chunk_record(a, span, g, begun, begun_q0, begun_rows, begun_row0);
 }
 
 template <int D, int KV, int QDT>
-int32_t launch(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream)
+int32_t launch(const ChunkArgs &a, hipStream_t stream)
 {
-    const int64_t shares = s.tiles + s.cap / a.num_kv_heads;
-    hipLaunchKernelGGL((chunk_f32_kernel<D, KV, QDT>), dim3((unsigned)(shares * a.num_kv_heads)), dim3(64 * kWaves), 0, stream, a);
+    hipLaunchKernelGGL((chunk_f32_kernel<D, KV, QDT>), dim3((unsigned)(a.spans * a.num_kv_heads)), dim3(64 * kWaves), 0, stream, a);
     SS_HIP_CHECK(hipGetLastError(), "launch chunk_f32_kernel");
-    if (s.cap >= 2 * a.num_kv_heads) {
-        const int64_t fit = s.cap / (2 * a.num_kv_heads), cuts = s.tiles < fit ? s.tiles : fit;
-        hipLaunchKernelGGL((chunk_merge_kernel<kRows, 16, D, QDT>), dim3((unsigned)(cuts * a.num_kv_heads * (kRows * D / 1024))), dim3(256), 0, stream, a);
-        SS_HIP_CHECK(hipGetLastError(), "launch chunk_merge_kernel");
-    }
-    return SS_OK;
+    return chunk_merge_launch<kRows, 16, D, QDT>(a, stream);
 }
 
 template <int D, int QDT>
-int32_t launch_kv(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream)
+int32_t launch_kv(const ChunkArgs &a, hipStream_t stream)
 {
     switch (a.kv_dtype) {
-    case SS_F32: return launch<D, SS_F32, QDT>(a, s, stream);
-    case SS_BF16: return launch<D, SS_BF16, QDT>(a, s, stream);
-    default: return launch<D, SS_FP8_E4M3, QDT>(a, s, stream);
+    case SS_F32: return launch<D, SS_F32, QDT>(a, stream);
+    case SS_BF16: return launch<D, SS_BF16, QDT>(a, stream);
+    default: return launch<D, SS_FP8_E4M3, QDT>(a, stream);
     }
 }
 
 }  // namespace
 
-int32_t chunk_f32_launch(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream)
+int32_t chunk_f32_launch(const ChunkArgs &a, hipStream_t stream)
 {
-    if (a.head_dim == 128) return a.q_dtype == SS_F32 ? launch_kv<128, SS_F32>(a, s, stream) : launch_kv<128, SS_BF16>(a, s, stream);
-    return a.q_dtype == SS_F32 ? launch_kv<64, SS_F32>(a, s, stream) : launch_kv<64, SS_BF16>(a, s, stream);
+    if (a.head_dim == 128) return a.q_dtype == SS_F32 ? launch_kv<128, SS_F32>(a, stream) : launch_kv<128, SS_BF16>(a, stream);
+    return a.q_dtype == SS_F32 ? launch_kv<64, SS_F32>(a, stream) : launch_kv<64, SS_BF16>(a, stream);
 }
 
 }  // namespace ss

@@ -39,22 +39,23 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a)
 {
     constexpr int QUADS = ROWS * D / 4, PARTS = QUADS / 256;
     const int part = blockIdx.x % PARTS, unit = blockIdx.x / PARTS;
-    const int g = unit % a.num_kv_heads, cut = unit / a.num_kv_heads;
-    if (cut >= a.head[0]) return;
-    const int32_t *rec = a.rec + (int64_t)cut * kChunkRecInts;
-    const int slot = rec[0], pieces = rec[1], q0 = rec[2], q_len = rec[3], row0 = rec[4];
+    const int g = unit % a.num_kv_heads, span = unit / a.num_kv_heads;
+    const int32_t *rec = a.rec + (int64_t)span * kChunkRecInts;
+    const int pieces = rec[0], q0 = rec[1], rows = rec[2], row0 = rec[3];
+    if (pieces == 0) return;
     const int j = part * 256 + threadIdx.x;
     int row, d;
     chunk_quad<RB, D>(j, row, d);
     const int G = a.num_q_heads / a.num_kv_heads, n = row0 + row;
-    if (n >= q_len * G) return;
-    const int64_t step = (int64_t)a.num_kv_heads, first = (int64_t)slot * a.num_kv_heads + g;
-    float m = kChunkNoMax;
-    for (int p = 0; p < pieces; ++p) m = fmaxf(m, a.part_ml[((first + p * step) * ROWS + row) * 2]);
+    if (n >= rows) return;
+    // the first piece is the second partial result of its span, the others the first of theirs
+    const int64_t first = (2ll * span + 1) * a.num_kv_heads + g, step = 2ll * a.num_kv_heads, back = a.num_kv_heads;
+    float m = a.part_ml[(first * ROWS + row) * 2];
+    for (int p = 1; p < pieces; ++p) m = fmaxf(m, a.part_ml[((first - back + p * step) * ROWS + row) * 2]);
     float l = 0.f;
     chunk_float4 o = {0.f, 0.f, 0.f, 0.f};
     for (int p = 0; p < pieces; ++p) {
-        const int64_t at = first + p * step;
+        const int64_t at = first + p * step - (p ? back : 0);
         const float *ml = a.part_ml + (at * ROWS + row) * 2;
         const chunk_float4 x = reinterpret_cast<const chunk_float4 *>(a.part_o)[at * QUADS + j];
         const float w = __builtin_amdgcn_exp2f(ml[0] - m);
@@ -67,18 +68,26 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a)
     if (a.lse && d == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-// After a tile's cut pieces: what the merge needs to know.  Called by every wavefront of a workgroup with its share.
-template <int ROWS>
-__device__ __forceinline__ void chunk_record(const ChunkArgs &a, const ChunkShare &s, int g)
+// What the merge needs to know of the tile that a span begins and does not end; called once for each span and KV head, with 0 pieces if there is none.
+__device__ __forceinline__ void chunk_record(const ChunkArgs &a, int span, int g, int pieces, int q0, int rows, int row0)
 {
-    if (threadIdx.x == 0 && g == 0 && s.pieces > 1 && s.piece == 0) {
-        int32_t *rec = a.rec + (int64_t)s.cut * kChunkRecInts;
-        rec[0] = s.slot;
-        rec[1] = s.pieces;
-        rec[2] = s.q0;
-        rec[3] = s.q_len;
-        rec[4] = s.tile * ROWS;
+    if (a.cap > 0 && g == 0 && threadIdx.x == 0) {
+        int32_t *rec = a.rec + (int64_t)span * kChunkRecInts;
+        rec[0] = pieces;
+        rec[1] = q0;
+        rec[2] = rows;
+        rec[3] = row0;
     }
+}
+
+// Launches the merge for what a call has cut.
+template <int ROWS, int RB, int D, int Q_DT>
+int32_t chunk_merge_launch(const ChunkArgs &a, hipStream_t stream)
+{
+    if (a.cap == 0 || a.spans < 2) return SS_OK;
+    hipLaunchKernelGGL((chunk_merge_kernel<ROWS, RB, D, Q_DT>), dim3((unsigned)(a.spans - 1) * a.num_kv_heads * (ROWS * D / 1024)), dim3(256), 0, stream, a);
+    SS_HIP_CHECK(hipGetLastError(), "launch chunk_merge_kernel");
+    return SS_OK;
 }
 
 }  // namespace ss

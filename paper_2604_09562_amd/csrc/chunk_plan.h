@@ -1,58 +1,19 @@
 // How attention of a chunk is cut into workgroups' shares, worked out by every workgroup for itself from the requests' lengths (there is no kernel in
 // front).
 //
-// A unit is a request's query rows of one KV head (row n = head n % G of the group at new token n / G); a tile is ROWS of them, a step kStepKeys
-// keys, and steps(t) what the last row of tile t sees.  A tile's time is its steps.  With W = the steps of the whole call over the workgroups that run
-// at a time, tiles of more than W steps are cut into equal pieces of at most W (all the cut tiles of a request into as many as its last tile); their
-// results are partial and merged by their log-sum-exp.  steps(t) grows with t, so the tiles that are cut are the last ones of each request.  Pieces
-// come first, then whole tiles, the longest of a request first: workgroups are started in this order, and a long share that starts last is what
-// leaves compute units without work.
+// A unit is a request's query rows of one KV head (row n = head n % G of the group at new token n / G), a tile `rows` of them, and steps(t) are the steps of
+// `keys` keys up to what the last row of tile t sees.  The tiles of all requests, end to end, are cut into spans of equal cost, a tile costing its steps and
+// kOpen more (its queries, the first keys, its results); every KV head has the same spans.  What a span's ends cut off a tile is a partial result, merged by its
+// log-sum-exp; a workgroup has at most two.  The cost in front of tile t of a request is taken as if steps(t) grew evenly from its first to its
+// last tile: workgroups need the same cuts, and cuts of nearly equal cost.
 #pragma once
 
 #include "prefill.h"
 
 namespace ss {
 
-constexpr int kStepKeys = 64;        // keys of a step
 constexpr int kMinPiece = 4;         // steps below which a piece costs more than it brings
-
-struct ChunkUnit {                   // a request, as one lane sees it
-    int q0, q_len, kv_len, tiles, last;   // last: steps of its last tile
-};
-
-template <int ROWS>
-struct ChunkCut {
-    int G;
-    __device__ int steps(const ChunkUnit &u, int t) const
-    {
-        const int tok = min((int)((((int64_t)t + 1) * ROWS - 1) / G), u.q_len - 1);
-        const int seen = u.kv_len - u.q_len + tok + 1;
-        return seen > 0 ? (int)(((unsigned)seen + kStepKeys - 1) / kStepKeys) : 0;
-    }
-    __device__ ChunkUnit unit(const ChunkArgs &a, int b) const
-    {
-        ChunkUnit u = {0, 0, 0, 0, 0};
-        if (b < a.batch) {
-            u.q0 = a.q_indptr[b];
-            u.q_len = a.q_indptr[b + 1] - u.q0;
-            u.kv_len = a.kv_len[b];
-            u.tiles = u.q_len > 0 ? (int)(((int64_t)u.q_len * G + ROWS - 1) / ROWS) : 0;
-            u.last = u.tiles ? steps(u, u.tiles - 1) : 0;
-        }
-        return u;
-    }
-    // Pieces of the tiles that are cut, and the first of these (`tiles` if there is none), for shares of at most w steps.
-    __device__ int pieces(const ChunkUnit &u, int w, int &t0) const
-    {
-        t0 = u.tiles;
-        if (u.last <= w) return 1;
-        // the first tile with steps > w: its last token sees more than w * kStepKeys keys
-        const int64_t tok = (int64_t)w * kStepKeys - (u.kv_len - u.q_len);   // at least this token
-        t0 = tok <= 0 ? 0 : (int)((tok * G + ROWS) / ROWS) - 1;
-        t0 = min(t0, u.tiles - 1);
-        return (u.last + w - 1) / w;
-    }
-};
+constexpr int kSnap = 1;             // steps of a tile that no cut is made for
 
 template <typename T>
 __device__ __forceinline__ T wave_incl_sum(T x)
@@ -65,110 +26,183 @@ __device__ __forceinline__ T wave_incl_sum(T x)
     }
     return x;
 }
-__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
+__device__ __forceinline__ double lane_value(double x, int lane)
+{
+    const uint64_t w = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)w, lane), hi = __builtin_amdgcn_readlane((uint32_t)(w >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-struct ChunkShare {
-    int b, q0, q_len, kv_len;   // the request
-    int tile, s0, s1;           // its tile, the steps of this share
-    int piece, pieces;          // pieces > 1: a partial result
-    int slot;                   // of the partial result, without the KV head
-    int cut;                    // the tile's place among those that are cut
-    int cuts;                   // tiles that are cut, over all requests
+template <int ROWS, int KEYS, int OPEN>
+struct ChunkUnit {                   // a request
+    int q0, q_len, kv_len, G;
+    int tiles, first, last;          // steps of its first and last tile
+    double slope;
+
+    __device__ __forceinline__ int steps(int t) const
+    {
+        const int tok = min((int)((((int64_t)t + 1) * ROWS - 1) / G), q_len - 1), seen = kv_len - q_len + tok + 1;
+        return seen > 0 ? (int)(((unsigned)seen + KEYS - 1) / KEYS) : 0;
+    }
+    __device__ __forceinline__ void set(int q0_, int q1, int len, int G_)
+    {
+        q0 = q0_;
+        q_len = q1 - q0_;
+        kv_len = len;
+        G = G_;
+        tiles = q_len > 0 ? (int)(((int64_t)q_len * G + ROWS - 1) / ROWS) : 0;
+        first = tiles ? steps(0) : 0;
+        last = tiles ? steps(tiles - 1) : 0;
+        slope = tiles > 1 ? (last - first) / (2.0 * (tiles - 1)) : 0.0;
+    }
+    // cost of the tiles in front of tile t
+    __device__ __forceinline__ double before(int t) const { return (double)t * (OPEN + first) + __builtin_floor(slope * t * (t - 1.0)); }
+    // the step of tile t at which a cut of this cost (counted from the request's first tile) falls: 0 and steps(t) are no cuts
+    __device__ __forceinline__ int cut(double x, int t, int n) const
+    {
+        const double off = x - before(t) - OPEN;
+        return off <= kSnap ? 0 : off >= n - kSnap ? n : (int)off;
+    }
 };
 
-template <int ROWS>
-__device__ __forceinline__ bool chunk_find(const ChunkArgs &a, int item, ChunkShare &out)
-{
-    const ChunkCut<ROWS> c = {a.num_q_heads / a.num_kv_heads};
-    const int lane = threadIdx.x & 63;
-    int64_t total = 0;
-    if (a.cap > 0) {   // (steps grow evenly over a request's tiles)
-        for (int lo = 0; lo < a.batch; lo += 64) {
-            const ChunkUnit u = c.unit(a, lo + lane);
-            if (u.tiles) total += (int64_t)u.tiles * (u.last + c.steps(u, 0) + 1) / 2;
-        }
-#pragma unroll
-        for (int off = 32; off; off >>= 1) total += __shfl_xor(total, off);
-    }
-    int64_t w64 = total * a.num_kv_heads / a.target + 1;
-    int w = a.cap > 0 ? (int)(w64 < kMinPiece ? kMinPiece : w64 > 0x3fffffff ? 0x3fffffff : w64) : 0x3fffffff;
-    // the partial results have to fit: seldom more than one round
-    int split = 0, cuts = 0;
-    for (;;) {
-        int64_t n = 0;
-        cuts = 0;
-        for (int lo = 0; lo < a.batch; lo += 64) {
-            const ChunkUnit u = c.unit(a, lo + lane);
-            int t0;
-            const int p = c.pieces(u, w, t0);
-            n += (int64_t)(u.tiles - t0) * p;
-            cuts += u.tiles - t0;
-        }
-#pragma unroll
-        for (int off = 32; off; off >>= 1) {
-            n += __shfl_xor(n, off);
-            cuts += __shfl_xor(cuts, off);
-        }
-        if (n * a.num_kv_heads <= a.cap) { split = (int)n; break; }
-        w = w > 0x1fffffff ? 0x3fffffff : 2 * w;
-    }
-    split = __builtin_amdgcn_readfirstlane(split);
-    const bool whole = item >= split;
-    int rest = whole ? item - split : item, cut_before = 0;
-    for (int lo = 0; lo < a.batch; lo += 64) {
-        const ChunkUnit u = c.unit(a, lo + lane);
-        int t0;
-        const int p = c.pieces(u, w, t0);
-        const int mine = whole ? t0 : (u.tiles - t0) * p;
-        const int incl = wave_incl_sum(mine), cut_incl = wave_incl_sum(u.tiles - t0);
-        const uint64_t here = __ballot(incl > rest);
-        if (here) {
-            const int at = __builtin_ctzll(here);
-            out.b = lo + at;
-            out.q0 = __builtin_amdgcn_readlane(u.q0, at);
-            out.q_len = __builtin_amdgcn_readlane(u.q_len, at);
-            out.kv_len = __builtin_amdgcn_readlane(u.kv_len, at);
-            const int idx = rest - __builtin_amdgcn_readlane(incl - mine, at);
-            const int n = __builtin_amdgcn_readlane(p, at), tiles = __builtin_amdgcn_readlane(u.tiles, at);
-            const int first = __builtin_amdgcn_readlane(t0, at);
-            const ChunkUnit v = {out.q0, out.q_len, out.kv_len, tiles, 0};
-            out.pieces = whole ? 1 : n;
-            out.piece = whole ? 0 : idx % n;
-            out.tile = whole ? first - 1 - idx : tiles - 1 - idx / n;
-            const int s = c.steps(v, out.tile);
-            out.s0 = (int)((int64_t)s * out.piece / out.pieces);
-            out.s1 = (int)((int64_t)s * (out.piece + 1) / out.pieces);
-            out.slot = item;
-            out.cut = cut_before + __builtin_amdgcn_readlane(cut_incl - (u.tiles - t0), at) + idx / n;
-            out.cuts = __builtin_amdgcn_readfirstlane(cuts);
-            return true;
-        }
-        rest -= last_lane(incl);
-        cut_before += last_lane(cut_incl);
-    }
-    out.cuts = __builtin_amdgcn_readfirstlane(cuts);
-    return false;
-}
+struct ChunkPos {
+    int b, t, off;   // a request's tile, the steps of it that are done
+    double base;     // cost in front of the request
+};
 
-// The share number `item`, for a whole wavefront, in scalar registers; false if there are not so many.
-template <int ROWS>
-__device__ __forceinline__ bool chunk_share(const ChunkArgs &a, int item, ChunkShare &out)
-{
-    ChunkShare s = {};
-    const bool any = chunk_find<ROWS>(a, item, s);
-    out.b = __builtin_amdgcn_readfirstlane(s.b);
-    out.q0 = __builtin_amdgcn_readfirstlane(s.q0);
-    out.q_len = __builtin_amdgcn_readfirstlane(s.q_len);
-    out.kv_len = __builtin_amdgcn_readfirstlane(s.kv_len);
-    out.tile = __builtin_amdgcn_readfirstlane(s.tile);
-    out.s0 = __builtin_amdgcn_readfirstlane(s.s0);
-    out.s1 = __builtin_amdgcn_readfirstlane(s.s1);
-    out.piece = __builtin_amdgcn_readfirstlane(s.piece);
-    out.pieces = __builtin_amdgcn_readfirstlane(s.pieces);
-    out.slot = __builtin_amdgcn_readfirstlane(s.slot);
-    out.cut = __builtin_amdgcn_readfirstlane(s.cut);
-    out.cuts = __builtin_amdgcn_readfirstlane(s.cuts);
-    return __builtin_amdgcn_readfirstlane(any);
-}
+// A workgroup's span, piece by piece; all of it uniform over a wavefront.
+template <int ROWS, int KEYS, int OPEN>
+struct ChunkWalk {
+    typedef ChunkUnit<ROWS, KEYS, OPEN> Unit;
+    // the current piece: steps s0 to before s1 of tile t of request b.  part: place of its partial result, -1 if it is the whole tile.
+    int b, t, s0, s1, part;
+    Unit u;
+    int spans;       // in use
+
+    __device__ __forceinline__ bool begin(const ChunkArgs &a, int span)
+    {
+        me = span;
+        const int lane = threadIdx.x & 63, G = a.num_q_heads / a.num_kv_heads;
+        // pass 1: the cost of everything
+        double total = 0.0, incl = 0.0;
+        Unit mine = {};
+        for (int lo = 0; lo < a.batch; lo += 64) {
+            mine = unit(a, lo + lane, G);
+            incl = wave_incl_sum(mine.before(mine.tiles));
+            total += lane_value(incl, 63);
+        }
+        const double most = total / (OPEN + kMinPiece);
+        spans = uniform(most < 1.0 ? 1 : most < a.spans ? (int)most : a.spans);
+        if (span >= spans || total == 0.0) return false;
+        share = total / spans;
+        const ChunkPos from = locate(a, __builtin_floor(share * span), mine, incl, G);
+        to.b = a.batch;
+        to.t = to.off = 0;
+        if (span + 1 < spans) to = locate(a, __builtin_floor(share * (span + 1)), mine, incl, G);
+        base = from.base;
+        b = from.b;
+        t = from.t;
+        u = request(a, b);
+        s0 = from.off;
+        if (s0 > 0 && s0 == u.steps(t)) {   // the span in front has all of this tile
+            s0 = 0;
+            ++t;
+        }
+        return settle(a);
+    }
+    __device__ __forceinline__ bool next(const ChunkArgs &a)
+    {
+        s0 = 0;
+        ++t;
+        return settle(a);
+    }
+    // pieces of the current tile, which this span begins and does not end
+    __device__ __forceinline__ int pieces() const
+    {
+        const int lane = threadIdx.x & 63, n = u.steps(t);
+        int count = 1;
+        for (int j = me + 1;; j += 64) {
+            const bool inside = j + lane < spans && u.cut(__builtin_floor(share * (j + lane)) - base, t, n) < n;
+            const uint64_t m = __ballot(inside);   // (the cuts ascend)
+            count += __popcll(m);
+            if (m != ~0ull) return uniform(count);
+        }
+    }
+
+private:
+    int me;
+    double share, base;
+    ChunkPos to;
+
+    __device__ __forceinline__ Unit unit(const ChunkArgs &a, int i, int G) const
+    {
+        Unit r = {};
+        r.G = G;
+        if (i < a.batch) r.set(a.q_indptr[i], a.q_indptr[i + 1], a.kv_len[i], G);
+        return r;
+    }
+    __device__ __forceinline__ Unit request(const ChunkArgs &a, int i) const
+    {
+        Unit r;
+        r.set(uniform(a.q_indptr[i]), uniform(a.q_indptr[i + 1]), uniform(a.kv_len[i]), a.num_q_heads / a.num_kv_heads);
+        return r;
+    }
+    // Moves on to the next tile that there is and sets the piece's end; false behind the span's end.
+    __device__ __forceinline__ bool settle(const ChunkArgs &a)
+    {
+        while (t >= u.tiles) {
+            base += u.before(u.tiles);
+            t = 0;
+            if (++b >= a.batch) return false;
+            u = request(a, b);
+        }
+        const int n = uniform(u.steps(t));
+        s1 = n;
+        if (b > to.b || (b == to.b && (t > to.t || (t == to.t && to.off == 0)))) return false;
+        if (b == to.b && t == to.t) s1 = to.off;
+        part = s0 > 0 ? 2 * me : s1 < n ? 2 * me + 1 : -1;
+        return true;
+    }
+    // Where a cost falls.  mine, incl: the units and sums of the last 64 requests.
+    __device__ __forceinline__ ChunkPos locate(const ChunkArgs &a, double x, Unit mine, double incl, int G) const
+    {
+        const int lane = threadIdx.x & 63;
+        ChunkPos p = {a.batch, 0, 0, 0.0};
+        double front = 0.0;
+        for (int lo = 0; lo < a.batch; lo += 64) {
+            if (a.batch > 64) {
+                mine = unit(a, lo + lane, G);
+                incl = wave_incl_sum(mine.before(mine.tiles));
+            }
+            const uint64_t here = __ballot(front + incl > x);
+            if (here) {
+                const int at = __builtin_ctzll(here);
+                Unit v;
+                v.G = G;
+                v.q_len = __builtin_amdgcn_readlane(mine.q_len, at);
+                v.kv_len = __builtin_amdgcn_readlane(mine.kv_len, at);
+                v.tiles = __builtin_amdgcn_readlane(mine.tiles, at);
+                v.first = __builtin_amdgcn_readlane(mine.first, at);
+                v.slope = lane_value(mine.slope, at);
+                p.b = uniform(lo + at);
+                p.base = at ? front + lane_value(incl, at - 1) : front;
+                const double y = x - p.base;
+                int t = 0, n = v.tiles;      // the last tile that begins at or in front of y
+                while (n > 1) {
+                    const int step = (n + 63) / 64, i = lane * step;
+                    const int k = __popcll(__ballot(i < n && v.before(t + i) <= y)) - 1;
+                    t += k * step;
+                    n = min(step, n - k * step);
+                }
+                p.t = uniform(t);
+                p.off = uniform(v.cut(y, p.t, v.steps(p.t)));
+                return p;
+            }
+            front += lane_value(incl, 63);
+        }
+        return p;
+    }
+};
 
 }  // namespace ss

@@ -46,28 +46,26 @@ struct ChunkArgs {
     int32_t q_dtype, num_q_heads;
     float sm_scale;
     // how the work is cut (chunk_plan.h)
-    int32_t target;               // workgroups that run at a time
-    int32_t cap;                  // partial results the workspace has room for, 0: no tile is cut
-    int32_t *head;                // [1] tiles that were cut
-    int32_t *rec;                 // [cap / 2 rounded up][kChunkRecInts] one record per tile that was cut
+    int32_t spans;                // at most, for each KV head
+    int32_t cap;                  // partial results the workspace has room for: two for each span and KV head, or none
+    int32_t *rec;                 // [spans][kChunkRecInts] the tile that a span begins and does not end
     float *part_ml, *part_o;      // [cap] partial results
 };
-constexpr int kChunkRecInts = 8;
+constexpr int kChunkRecInts = 4;
+constexpr int kChunkKeys = 32, kChunkKeysF32 = 64;   // keys of a step
 constexpr int kChunkRows = 128, kChunkRowsF32 = 64;   // query rows of a tile: bf16 matrix-core kernel (or twice as many), fp32 kernel
 
 struct ChunkShape {               // host-visible sizes a launch and its workspace follow from
     int32_t rows;                 // query rows of a tile
-    int64_t tiles;                // upper bound of the tiles of one KV head
-    int32_t target;               // workgroups that run at a time
-    int32_t cap;
+    int32_t spans, cap;
 };
 int chunk_target();
 bool chunk_mfma_supported(int head_dim, int kv_dtype, int q_dtype);
 ChunkShape chunk_shape(bool mfma, int batch, int max_blocks, int num_q_heads, int num_kv_heads, int total_rows);
 size_t chunk_workspace_bytes(const ChunkShape &s, int head_dim);
 void chunk_carve(ChunkArgs &a, const ChunkShape &s, void *workspace);
-int32_t chunk_mfma_launch(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream);
-int32_t chunk_f32_launch(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream);
+int32_t chunk_mfma_launch(const ChunkArgs &a, int rows, hipStream_t stream);   // query rows of a tile
+int32_t chunk_f32_launch(const ChunkArgs &a, hipStream_t stream);
 
 // ---- optional checks of device-resident metadata -----------------------------------------------
 int32_t validate_chunk(const int32_t *block_table, const int32_t *kv_len, const int32_t *q_indptr, int batch, int max_blocks,
