@@ -70,7 +70,7 @@ __device__ __forceinline__ void each(F &&f)
 constexpr int kKeys = kChunkKeys;   // keys that are taken at a time, two cache blocks
 // What a tile costs beside its steps, in steps.
 template <int NB>
-constexpr int kOpen = NB == 2 ? 6 : 8;
+constexpr int kOpen = NB == 2 ? 9 : 8;
 constexpr int kPairKeys = 2 * kKeys;
 
 // 64 keys or values in LDS, rows of D bf16 in pieces of 16 bytes.  Piece c of row t stands at place c ^ turn(t): 16 rows' pieces
@@ -194,22 +194,31 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
     // A step that some row of the tile does not see all of, once this wavefront's block of its values is in LDS.  What stands behind the last token is of no
     // one; a value that is not finite is taken out of the product, in which it would reach every row (0 * inf), and added to the rows that see it.
     auto clean = [&](int step, Tile<D> &tile, int pair) __attribute__((always_inline)) {
+        constexpr int N = kTile * PIECES / 64;
+        const int left = s.u.kv_len - (step * kKeys + (wave & 1) * kTile);   // tokens of the block that there are
+        u32x4 w[N];
+        uint32_t carry = 0;                                                  // the sign bits of halves whose exponent is all ones
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            w[i] = tile.w[wave * kTile + (i * 64 + lane) / PIECES][(i * 64 + lane) % PIECES];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) carry |= (w[i][j] & 0x7f807f80u) + 0x00800080u;
+        }
+        const bool found = __ballot((carry & 0x80008000u) != 0) != 0;
         bool odd = false;
+        if (found || left < kTile) {
 #pragma unroll
-        for (int i = 0; i < kTile * PIECES / 64; ++i) {
-            const int p = i * 64 + lane, t = p / PIECES;
-            u32x4 &at = tile.w[wave * kTile + t][p % PIECES];
-            u32x4 w = at;
-            const bool dead = step * kKeys + (wave & 1) * kTile + t >= s.u.kv_len;
-            bool changed = dead;
+            for (int i = 0; i < N; ++i) {
+                const int t = (i * 64 + lane) / PIECES;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t x = dead ? 0u : w[j];
-                if ((x & 0x7f80u) == 0x7f80u) { x &= 0xffff0000u; changed = odd = true; }
-                if ((x & 0x7f800000u) == 0x7f800000u) { x &= 0xffffu; changed = odd = true; }
-                w[j] = x;
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t x = t >= left ? 0u : w[i][j];
+                    if ((x & 0x7f80u) == 0x7f80u) { x &= 0xffff0000u; odd = true; }
+                    if ((x & 0x7f800000u) == 0x7f800000u) { x &= 0xffffu; odd = true; }
+                    w[i][j] = x;
+                }
+                tile.w[wave * kTile + t][(i * 64 + lane) % PIECES] = w[i];
             }
-            if (changed) at = w;
         }
         odd_flags[pair][wave] = __ballot(odd) != 0;
     };
@@ -317,10 +326,10 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
             }
         }
     };
-    auto add_odd = [&](int t) __attribute__((always_inline)) {
+    auto add_odd = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < NB; ++e)
-            for (int pos = t * kKeys; pos < min((t + 1) * kKeys, lim[e] + 1); ++pos) {
+            for (int pos = max(first, full) * kKeys; pos <= lim[e]; ++pos) {
                 const int64_t at0 = (((int64_t)table[pos / kTile] * a.num_kv_heads + g) * kTile + pos % kTile) * D + half * 4;
 #pragma unroll
                 for (int b = 0; b < DB; ++b)
@@ -343,6 +352,7 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
     // k_read: the tile of step t + 2's keys, v_read: of step t's values; k_next, v_next: those that are free after the meeting.
     bf16x8 kf[KS];
     int kid = 0, vid = 0;   // this wavefront's blocks to bring next
+    int odd_seen = 0;       // values that are not finite were taken out
     // the meeting of the wavefronts; dirty: values of theirs have to be cleaned in front of it
     auto meet = [&](bool dirty, int t, Tile<D> &v_new, int pair) __attribute__((always_inline)) {
         if constexpr (FP8) put(in_v, v_new, wave);
@@ -404,7 +414,7 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
             });
             __builtin_amdgcn_sched_barrier(0);
         });
-        if (MASKED && t >= full && (odd_flags[pair][2 * ODD] | odd_flags[pair][2 * ODD + 1])) add_odd(t);
+        if (MASKED && t >= full) odd_seen |= odd_flags[pair][2 * ODD] | odd_flags[pair][2 * ODD + 1];
 #pragma unroll
         for (int e = 0; e < NB; ++e) top[e] = whole_row(top[e]);
         follow(top);
@@ -472,6 +482,7 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
             int t = first;
             for (const int fast_end = min(full, end) - 5; t < fast_end; t += 4) four_steps(std::false_type{}, t, x, y);
             for (; t < end; t += 4) four_steps(std::true_type{}, t, x, y);
+            if (__builtin_expect(odd_seen != 0, 0)) add_odd();
         } else {
             team_barrier<false>();
             bring(k_base, block_id(first + 3, wave), k_even, wave, in_k);

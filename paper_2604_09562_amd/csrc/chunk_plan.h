@@ -3,7 +3,7 @@
 //
 // A unit is a request's query rows of one KV head (row n = head n % G of the group at new token n / G), a tile `rows` of them, and steps(t) are the steps of
 // `keys` keys up to what the last row of tile t sees.  The tiles of all requests, end to end, are cut into spans of equal cost, a tile costing its steps and
-// kOpen more (its queries, the first keys, its results); every KV head has the same spans.  What a span's ends cut off a tile is a partial result, merged by its
+// OPEN more (its queries, the first keys, its results); every KV head has the same spans.  What a span's ends cut off a tile is a partial result, merged by its
 // log-sum-exp; a workgroup has at most two.  The cost in front of tile t of a request is taken as if steps(t) grew evenly from its first to its
 // last tile: workgroups need the same cuts, and cuts of nearly equal cost.
 #pragma once
@@ -12,7 +12,8 @@
 
 namespace ss {
 
-constexpr int kMinPiece = 4;         // steps below which a piece costs more than it brings
+constexpr int kMinPiece = 3;         // steps below which a piece costs more than it brings
+constexpr int kOpenFew = 1;          // a tile's cost beside its steps where there are not spans enough for all workgroups: their openings run side by side
 constexpr int kSnap = 1;             // steps of a tile that no cut is made for
 
 template <typename T>
@@ -34,34 +35,35 @@ __device__ __forceinline__ double lane_value(double x, int lane)
 }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-template <int ROWS, int KEYS, int OPEN>
+template <int ROWS, int KEYS>
 struct ChunkUnit {                   // a request
-    int q0, q_len, kv_len, G;
+    int q0, q_len, kv_len, G, open;  // open: what a tile costs beside its steps
     int tiles, first, last;          // steps of its first and last tile
     double slope;
 
     __device__ __forceinline__ int steps(int t) const
     {
-        const int tok = min((int)((((int64_t)t + 1) * ROWS - 1) / G), q_len - 1), seen = kv_len - q_len + tok + 1;
+        const int tok = min((int)((uint32_t)((t + 1) * ROWS - 1) / (uint32_t)G), q_len - 1), seen = kv_len - q_len + tok + 1;
         return seen > 0 ? (int)(((unsigned)seen + KEYS - 1) / KEYS) : 0;
     }
-    __device__ __forceinline__ void set(int q0_, int q1, int len, int G_)
+    __device__ __forceinline__ void set(int q0_, int q1, int len, int G_, int open_)
     {
+        open = open_;
         q0 = q0_;
         q_len = q1 - q0_;
         kv_len = len;
         G = G_;
-        tiles = q_len > 0 ? (int)(((int64_t)q_len * G + ROWS - 1) / ROWS) : 0;
+        tiles = q_len > 0 ? (int)(((uint32_t)q_len * (uint32_t)G + ROWS - 1) / ROWS) : 0;
         first = tiles ? steps(0) : 0;
         last = tiles ? steps(tiles - 1) : 0;
         slope = tiles > 1 ? (last - first) / (2.0 * (tiles - 1)) : 0.0;
     }
     // cost of the tiles in front of tile t
-    __device__ __forceinline__ double before(int t) const { return (double)t * (OPEN + first) + __builtin_floor(slope * t * (t - 1.0)); }
+    __device__ __forceinline__ double before(int t) const { return (double)t * (open + first) + __builtin_floor(slope * t * (t - 1.0)); }
     // the step of tile t at which a cut of this cost (counted from the request's first tile) falls: 0 and steps(t) are no cuts
     __device__ __forceinline__ int cut(double x, int t, int n) const
     {
-        const double off = x - before(t) - OPEN;
+        const double off = x - before(t) - open;
         return off <= kSnap ? 0 : off >= n - kSnap ? n : (int)off;
     }
 };
@@ -74,7 +76,7 @@ struct ChunkPos {
 // A workgroup's span, piece by piece; all of it uniform over a wavefront.
 template <int ROWS, int KEYS, int OPEN>
 struct ChunkWalk {
-    typedef ChunkUnit<ROWS, KEYS, OPEN> Unit;
+    typedef ChunkUnit<ROWS, KEYS> Unit;
     // the current piece: steps s0 to before s1 of tile t of request b.  part: place of its partial result, -1 if it is the whole tile.
     int b, t, s0, s1, part;
     Unit u;
@@ -84,15 +86,20 @@ struct ChunkWalk {
     {
         me = span;
         const int lane = threadIdx.x & 63, G = a.num_q_heads / a.num_kv_heads;
-        // pass 1: the cost of everything
         double total = 0.0, incl = 0.0;
         Unit mine = {};
-        for (int lo = 0; lo < a.batch; lo += 64) {
-            mine = unit(a, lo + lane, G);
-            incl = wave_incl_sum(mine.before(mine.tiles));
-            total += lane_value(incl, 63);
+        open = OPEN;
+        for (;;) {   // the cost of everything
+            total = 0.0;
+            for (int lo = 0; lo < a.batch; lo += 64) {
+                mine = unit(a, lo + lane, G);
+                incl = wave_incl_sum(mine.before(mine.tiles));
+                total += lane_value(incl, 63);
+            }
+            if (open < OPEN || total >= (double)a.spans * (OPEN + kMinPiece)) break;
+            open = kOpenFew;
         }
-        const double most = total / (OPEN + kMinPiece);
+        const double most = open == OPEN ? a.spans : total / kMinPiece;
         spans = uniform(most < 1.0 ? 1 : most < a.spans ? (int)most : a.spans);
         if (span >= spans || total == 0.0) return false;
         share = total / spans;
@@ -131,7 +138,7 @@ struct ChunkWalk {
     }
 
 private:
-    int me;
+    int me, open;
     double share, base;
     ChunkPos to;
 
@@ -139,13 +146,14 @@ private:
     {
         Unit r = {};
         r.G = G;
-        if (i < a.batch) r.set(a.q_indptr[i], a.q_indptr[i + 1], a.kv_len[i], G);
+        r.open = open;
+        if (i < a.batch) r.set(a.q_indptr[i], a.q_indptr[i + 1], a.kv_len[i], G, open);
         return r;
     }
     __device__ __forceinline__ Unit request(const ChunkArgs &a, int i) const
     {
         Unit r;
-        r.set(uniform(a.q_indptr[i]), uniform(a.q_indptr[i + 1]), uniform(a.kv_len[i]), a.num_q_heads / a.num_kv_heads);
+        r.set(uniform(a.q_indptr[i]), uniform(a.q_indptr[i + 1]), uniform(a.kv_len[i]), a.num_q_heads / a.num_kv_heads, open);
         return r;
     }
     // Moves on to the next tile that there is and sets the piece's end; false behind the span's end.
@@ -180,6 +188,7 @@ private:
                 const int at = __builtin_ctzll(here);
                 Unit v;
                 v.G = G;
+                v.open = open;
                 v.q_len = __builtin_amdgcn_readlane(mine.q_len, at);
                 v.kv_len = __builtin_amdgcn_readlane(mine.kv_len, at);
                 v.tiles = __builtin_amdgcn_readlane(mine.tiles, at);
