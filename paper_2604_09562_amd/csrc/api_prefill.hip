@@ -1,5 +1,4 @@
 // C-ABI entry points of the calls that fill the paged cache: argument validation, workspace sizing, dispatch.  No arithmetic here.
-#include <stdlib.h>
 #include "chunk_plan.h"
 
 namespace ss {
@@ -67,8 +66,9 @@ ChunkShape chunk_shape(bool mfma, int batch, int max_blocks, int num_q_heads, in
 {
     ChunkShape s;
     const int64_t G = num_q_heads / num_kv_heads;
-    s.rows = mfma ? (getenv("SS_NB") ? atoi(getenv("SS_NB")) : 2) * kChunkRows : kChunkRowsF32;
-    const int64_t wgs = chunk_target() / (s.rows > kChunkRows ? 2 : 1), tiles = (int64_t)total_rows * G / s.rows + (batch < total_rows ? batch : total_rows);
+    s.rows = mfma ? kChunkRows : kChunkRowsF32;
+    // workgroups that run at a time: of the matrix-core kernel one to a compute unit, of the fp32 kernel two
+    const int64_t wgs = attn_chip_waves() / (mfma ? 4 : 2), tiles = (int64_t)total_rows * G / s.rows + (batch < total_rows ? batch : total_rows);
     // as many spans as workgroups run at a time, if there can be work enough
     const int64_t keys = mfma ? kChunkKeys : kChunkKeysF32, steps = ((int64_t)max_blocks * SS_BLOCK_SIZE + keys - 1) / keys;
     const int64_t most = tiles * ((steps + kMinPiece - 1) / kMinPiece), each = wgs > num_kv_heads ? wgs / num_kv_heads : 1;
@@ -76,9 +76,6 @@ ChunkShape chunk_shape(bool mfma, int batch, int max_blocks, int num_q_heads, in
     s.cap = s.spans > 1 ? 2 * s.spans * num_kv_heads : 0;
     return s;
 }
-
-// A wavefront is one of two on a SIMD (tiles of 128 rows, fp32), four make a workgroup.
-int chunk_target() { return attn_chip_waves() / 2; }
 
 size_t chunk_workspace_bytes(const ChunkShape &s, int head_dim)
 {
@@ -200,7 +197,7 @@ int32_t ss_chunk_attn(const ss_paged_kv *kv, const ss_batch *batch, const void *
     a.block_table = batch->block_table; a.kv_len = batch->kv_len; a.q_indptr = batch->q_indptr;
     a.q = q; a.q_stride = q_stride; a.out = out; a.lse = lse; a.q_dtype = q_dtype; a.num_q_heads = num_q_heads; a.sm_scale = sm_scale;
     chunk_carve(a, s, workspace);
-    return mfma ? chunk_mfma_launch(a, s.rows, static_cast<hipStream_t>(stream)) : chunk_f32_launch(a, static_cast<hipStream_t>(stream));
+    return mfma ? chunk_mfma_launch(a, static_cast<hipStream_t>(stream)) : chunk_f32_launch(a, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

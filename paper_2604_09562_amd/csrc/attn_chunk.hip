@@ -20,6 +20,9 @@ typedef float float2v __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4;
+constexpr int NB = 2;                                  // blocks of 32 query rows to a wavefront
+constexpr int ROWS = 32 * NB * kWaves;                // query rows of a tile
+static_assert(ROWS == kChunkRows, "what launches and workspaces are sized by");
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // How far (in powers of two) a row's scores may rise above the reference of its exponentials before the sums are rescaled.
 constexpr float kLag = 16.0f;
@@ -69,8 +72,7 @@ __device__ __forceinline__ void each(F &&f)
 
 constexpr int kKeys = kChunkKeys;   // keys that are taken at a time, two cache blocks
 // What a tile costs beside its steps, in steps.
-template <int NB>
-constexpr int kOpen = NB == 2 ? 9 : 8;
+constexpr int kOpen = 9;
 constexpr int kPairKeys = 2 * kKeys;
 
 // 64 keys or values in LDS, rows of D bf16 in pieces of 16 bytes.  Piece c of row t stands at place c ^ turn(t): 16 rows' pieces
@@ -85,19 +87,19 @@ __device__ __forceinline__ int turn(int t)
     return D == 128 ? (t & 3) << 2 | (t >> 2 & 3) : (t >> 1 & 1) << 2 | (t >> 2 & 3);
 }
 
-template <int D, bool FP8, int NB>
-__global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(ChunkArgs a, const int32_t *__restrict__ block_table,
-                                                                             const float *__restrict__ k_scale, const float *__restrict__ v_scale)
+template <int D, bool FP8>
+__global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, const int32_t *__restrict__ block_table, const float *__restrict__ k_scale,
+                                                               const float *__restrict__ v_scale)
 {
     // (table and scales come in as no-alias arguments of their own, so that they are scalar loads)
-    constexpr int ROWS = 128 * NB, KS = D / 16, DB = D / 32, PIECES = D / 8;
+    constexpr int KS = D / 16, DB = D / 32, PIECES = D / 8;
     constexpr int BLOCK_BYTES = kTile * D * (FP8 ? 1 : 2), LOADS = BLOCK_BYTES / (64 * 16);   // 16-byte loads of a lane for a cache block
     // Variables of their own: a tile's reads then do not wait for what is on its way into another one.
     __shared__ Tile<D> k_even, k_odd, v_even, v_odd;   // steps 3, 4, 7, 8, ..; 1, 2, 5, 6, ..; 0, 1, 4, 5, ..; 2, 3, 6, 7, .. (from the first)
     __shared__ int odd_flags[2][kWaves];
     const int g = blockIdx.x % a.num_kv_heads, span = blockIdx.x / a.num_kv_heads;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    ChunkWalk<ROWS, kKeys, kOpen<NB>> s;
+    ChunkWalk<ROWS, kKeys, kOpen> s;
     int begun = 0, begun_q0 = 0, begun_rows = 0, begun_row0 = 0;   // of the tile that the span begins and does not end
     for (bool any = s.begin(a, span); any; any = s.next(a)) {
     if (s.part == 2 * span + 1) {
@@ -368,12 +370,11 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
         // Both parts are as many matrix instructions and between them, in this order, what the vector unit and LDS have to do: the first EXPS of the 16 NB
         // exponentials and the values' operands (in its first half), the others, the next keys' operands (in its first half) and the largest scores.
         constexpr bool ODD = decltype(parity)::value, MASKED = decltype(masked)::value;
-        constexpr int M1 = NB * KS, M2 = NB * 2 * DB, ELS = 16 * NB, EXPS = NB == 2 ? 20 : 12, LAST = NB == 2 ? M2 * 3 / 4 : M2 / 2, FRAGS = 2 * DB;
+        constexpr int M1 = NB * KS, M2 = NB * 2 * DB, ELS = 16 * NB, EXPS = 20, LAST = M2 * 3 / 4, FRAGS = 2 * DB;
         constexpr auto least = [](int u, int v) { return u < v ? u : v; };
         constexpr auto exps_by = [](int i) { return i == 0 ? EXPS : i >= LAST ? ELS + 1 : EXPS + i * (ELS - EXPS) / LAST; };
-        // (two blocks of rows: over half of a part; one, which has fewer registers: each takes the place of one that has been used)
-        constexpr auto values_by = [least](int i) { return least(FRAGS, NB * i * FRAGS / M1); };
-        constexpr auto keys_by = [least](int i) { return least(KS, NB * i * KS / M2); };
+        constexpr auto values_by = [least](int i) { return least(FRAGS, 2 * i * FRAGS / M1); };
+        constexpr auto keys_by = [least](int i) { return least(KS, 2 * i * KS / M2); };
         constexpr auto parts_by = [](int i) { return i <= 2 ? 0 : (i - 2) * 8 * NB / (M2 - 2); };
         bf16x8 vf[2][DB], pk[NB][2];
         __builtin_amdgcn_sched_barrier(0);
@@ -530,18 +531,12 @@ __global__ __launch_bounds__(64 * kWaves, NB == 2 ? 1 : 2) void chunk_kernel(Chu
     chunk_record(a, span, g, begun, begun_q0, begun_rows, begun_row0);
 }
 
-template <int D, bool FP8, int NB>
+template <int D, bool FP8>
 int32_t launch(const ChunkArgs &a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((chunk_kernel<D, FP8, NB>), dim3((unsigned)(a.spans * a.num_kv_heads)), dim3(64 * kWaves), 0, stream, a, a.block_table, a.k_scale, a.v_scale);
+    hipLaunchKernelGGL((chunk_kernel<D, FP8>), dim3((unsigned)(a.spans * a.num_kv_heads)), dim3(64 * kWaves), 0, stream, a, a.block_table, a.k_scale, a.v_scale);
     SS_HIP_CHECK(hipGetLastError(), "launch chunk_kernel");
-    return chunk_merge_launch<128 * NB, 32, D, SS_BF16>(a, stream);
-}
-
-template <int D, bool FP8>
-int32_t launch_rows(const ChunkArgs &a, int rows, hipStream_t stream)
-{
-    return rows > kChunkRows ? launch<D, FP8, 2>(a, stream) : launch<D, FP8, 1>(a, stream);
+    return chunk_merge_launch<ROWS, 32, D, SS_BF16>(a, stream);
 }
 
 }  // namespace
@@ -551,11 +546,11 @@ bool chunk_mfma_supported(int head_dim, int kv_dtype, int q_dtype)
     return (head_dim == 64 || head_dim == 128) && q_dtype == SS_BF16 && (kv_dtype == SS_BF16 || kv_dtype == SS_FP8_E4M3);
 }
 
-int32_t chunk_mfma_launch(const ChunkArgs &a, int rows, hipStream_t stream)
+int32_t chunk_mfma_launch(const ChunkArgs &a, hipStream_t stream)
 {
     const bool fp8 = a.kv_dtype == SS_FP8_E4M3;
-    if (a.head_dim == 128) return fp8 ? launch_rows<128, true>(a, rows, stream) : launch_rows<128, false>(a, rows, stream);
-    return fp8 ? launch_rows<64, true>(a, rows, stream) : launch_rows<64, false>(a, rows, stream);
+    if (a.head_dim == 128) return fp8 ? launch<128, true>(a, stream) : launch<128, false>(a, stream);
+    return fp8 ? launch<64, true>(a, stream) : launch<64, false>(a, stream);
 }
 
 }  // namespace ss

@@ -34,38 +34,84 @@ __device__ __forceinline__ void chunk_store4(void *out, int64_t i, chunk_float4 
     }
 }
 
+// A workgroup merges 256 quads: of few pieces a wavefront 64 quads, of many (a tile of a long cache in some dozens) all four wavefronts the same 64, a quarter of
+// the pieces each.
+constexpr int kMergeWays = 4;
+
 template <int ROWS, int RB, int D, int Q_DT>
-__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a)
+__global__ __launch_bounds__(64 * kMergeWays) void chunk_merge_kernel(ChunkArgs a)
 {
-    constexpr int QUADS = ROWS * D / 4, PARTS = QUADS / 256;
+    constexpr int QUADS = ROWS * D / 4, PARTS = QUADS / (64 * kMergeWays), AHEAD = 4;
+    __shared__ chunk_float4 so[kMergeWays - 1][64];
+    __shared__ float sm[kMergeWays - 1][64], sl[kMergeWays - 1][64];
     const int part = blockIdx.x % PARTS, unit = blockIdx.x / PARTS;
     const int g = unit % a.num_kv_heads, span = unit / a.num_kv_heads;
     const int32_t *rec = a.rec + (int64_t)span * kChunkRecInts;
     const int pieces = rec[0], q0 = rec[1], rows = rec[2], row0 = rec[3];
     if (pieces == 0) return;
-    const int j = part * 256 + threadIdx.x;
-    int row, d;
-    chunk_quad<RB, D>(j, row, d);
-    const int G = a.num_q_heads / a.num_kv_heads, n = row0 + row;
-    if (n >= rows) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const bool many = pieces > 2 * kMergeWays;
+    const int way = many ? wave : 0, ways = many ? kMergeWays : 1;
+    const int G = a.num_q_heads / a.num_kv_heads;
     // the first piece is the second partial result of its span, the others the first of theirs
-    const int64_t first = (2ll * span + 1) * a.num_kv_heads + g, step = 2ll * a.num_kv_heads, back = a.num_kv_heads;
-    float m = a.part_ml[(first * ROWS + row) * 2];
-    for (int p = 1; p < pieces; ++p) m = fmaxf(m, a.part_ml[((first - back + p * step) * ROWS + row) * 2]);
-    float l = 0.f;
-    chunk_float4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < pieces; ++p) {
-        const int64_t at = first + p * step - (p ? back : 0);
-        const float *ml = a.part_ml + (at * ROWS + row) * 2;
-        const chunk_float4 x = reinterpret_cast<const chunk_float4 *>(a.part_o)[at * QUADS + j];
-        const float w = __builtin_amdgcn_exp2f(ml[0] - m);
-        l += w * ml[1];
-        o += w * x;
+    auto place = [&](int p) { return (2ll * (span + p) + (p == 0)) * a.num_kv_heads + g; };
+    for (int k = many ? 0 : wave; k < kMergeWays; k += many ? 1 : kMergeWays) {
+        const int j = (part * kMergeWays + k) * 64 + lane;
+        int row, d;
+        chunk_quad<RB, D>(j, row, d);
+        const int n = row0 + row;
+        float m = kChunkNoMax, l = 0.f;
+        chunk_float4 o = {0.f, 0.f, 0.f, 0.f};
+        if (n < rows) {
+            for (int p0 = way; p0 < pieces; p0 += ways * AHEAD) {
+                float mi[AHEAD], li[AHEAD];
+                chunk_float4 x[AHEAD];
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const int p = p0 + i * ways;
+                    mi[i] = kChunkNoMax;
+                    li[i] = 0.f;
+                    x[i] = chunk_float4{0.f, 0.f, 0.f, 0.f};
+                    if (p < pieces) {
+                        const int64_t at = place(p);
+                        const float *ml = a.part_ml + (at * ROWS + row) * 2;
+                        mi[i] = ml[0];
+                        li[i] = ml[1];
+                        x[i] = reinterpret_cast<const chunk_float4 *>(a.part_o)[at * QUADS + j];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const float up = fmaxf(m, mi[i]), down = __builtin_amdgcn_exp2f(m - up), w = __builtin_amdgcn_exp2f(mi[i] - up);
+                    m = up;
+                    l = l * down + w * li[i];
+                    o = o * down + w * x[i];
+                }
+            }
+        }
+        if (many) {
+            if (way > 0) {
+                sm[way - 1][lane] = m;
+                sl[way - 1][lane] = l;
+                so[way - 1][lane] = o;
+            }
+            __syncthreads();
+            if (way == 0)
+#pragma unroll
+                for (int i = 0; i < kMergeWays - 1; ++i) {
+                    const float up = fmaxf(m, sm[i][lane]), down = __builtin_amdgcn_exp2f(m - up), w = __builtin_amdgcn_exp2f(sm[i][lane] - up);
+                    m = up;
+                    l = l * down + w * sl[i][lane];
+                    o = o * down + w * so[i][lane];
+                }
+            __syncthreads();
+        }
+        if (way > 0 || n >= rows) continue;
+        const int64_t at = (int64_t)(q0 + n / G) * a.num_q_heads + g * G + n % G;
+        const float r = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;   // (a row that sees nothing: zeros; NaN stays)
+        chunk_store4<Q_DT>(a.out, at * D + d, o * r);
+        if (a.lse && d == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
     }
-    const int64_t at = (int64_t)(q0 + n / G) * a.num_q_heads + g * G + n % G;
-    const float r = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;   // (a row that sees nothing: zeros; NaN stays)
-    chunk_store4<Q_DT>(a.out, at * D + d, o * r);
-    if (a.lse && d == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 // What the merge needs to know of the tile that a span begins and does not end; called once for each span and KV head, with 0 pieces if there is none.
@@ -85,7 +131,8 @@ template <int ROWS, int RB, int D, int Q_DT>
 int32_t chunk_merge_launch(const ChunkArgs &a, hipStream_t stream)
 {
     if (a.cap == 0 || a.spans < 2) return SS_OK;
-    hipLaunchKernelGGL((chunk_merge_kernel<ROWS, RB, D, Q_DT>), dim3((unsigned)(a.spans - 1) * a.num_kv_heads * (ROWS * D / 1024)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((chunk_merge_kernel<ROWS, RB, D, Q_DT>), dim3((unsigned)(a.spans - 1) * a.num_kv_heads * (ROWS * D / (256 * kMergeWays))),
+                       dim3(64 * kMergeWays), 0, stream, a);
     SS_HIP_CHECK(hipGetLastError(), "launch chunk_merge_kernel");
     return SS_OK;
 }

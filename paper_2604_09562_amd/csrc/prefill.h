@@ -53,18 +53,17 @@ struct ChunkArgs {
 };
 constexpr int kChunkRecInts = 4;
 constexpr int kChunkKeys = 32, kChunkKeysF32 = 64;   // keys of a step
-constexpr int kChunkRows = 128, kChunkRowsF32 = 64;   // query rows of a tile: bf16 matrix-core kernel (or twice as many), fp32 kernel
+constexpr int kChunkRows = 256, kChunkRowsF32 = 64;   // query rows of a tile: bf16 matrix-core kernel, fp32 kernel
 
 struct ChunkShape {               // host-visible sizes a launch and its workspace follow from
     int32_t rows;                 // query rows of a tile
     int32_t spans, cap;
 };
-int chunk_target();
 bool chunk_mfma_supported(int head_dim, int kv_dtype, int q_dtype);
 ChunkShape chunk_shape(bool mfma, int batch, int max_blocks, int num_q_heads, int num_kv_heads, int total_rows);
 size_t chunk_workspace_bytes(const ChunkShape &s, int head_dim);
 void chunk_carve(ChunkArgs &a, const ChunkShape &s, void *workspace);
-int32_t chunk_mfma_launch(const ChunkArgs &a, int rows, hipStream_t stream);   // query rows of a tile
+int32_t chunk_mfma_launch(const ChunkArgs &a, hipStream_t stream);
 int32_t chunk_f32_launch(const ChunkArgs &a, hipStream_t stream);
 
 // ---- optional checks of device-resident metadata -----------------------------------------------
