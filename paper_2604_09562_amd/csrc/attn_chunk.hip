@@ -74,6 +74,7 @@ constexpr int kKeys = kChunkKeys;   // keys that are taken at a time, two cache 
 // What a tile costs beside its steps, in steps.
 constexpr int kOpen = 9;
 constexpr int kPairKeys = 2 * kKeys;
+constexpr int kFloatMax = 0x7f7fffff;   // the largest float's bits
 
 // 64 keys or values in LDS, rows of D bf16 in pieces of 16 bytes.  Piece c of row t stands at place c ^ turn(t): 16 rows' pieces
 // of equal c fill all banks (scores), and so do four rows' pieces 4 n .. 4 n + 3 (transposing reads of values).
@@ -137,9 +138,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
     }
 
     typedef const __attribute__((address_space(4))) int32_t *scalar_ints;       // (read with scalar loads, whatever else is written meanwhile)
-    typedef const __attribute__((address_space(4))) float *scalar_floats;
     const scalar_ints table = (scalar_ints)(uintptr_t)(block_table + (int64_t)s.b * a.max_blocks);
-    const scalar_floats k_scales = (scalar_floats)(uintptr_t)k_scale, v_scales = (scalar_floats)(uintptr_t)v_scale;
+    const scalar_ints k_scales = (scalar_ints)(uintptr_t)k_scale, v_scales = (scalar_ints)(uintptr_t)v_scale;
     const int last_block = (int)(((unsigned)s.u.kv_len + kTile - 1) / kTile) - 1;
     // block j of a step (the last block again where there is none: what stands there is masked)
     auto block_id = [&](int step, int j) __attribute__((always_inline)) { return table[min(step * 2 + j, last_block)]; };
@@ -148,7 +148,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
 
     // ---- a cache block into a quarter of a tile ----
     // bf16: straight into LDS, where a lane's 16 bytes stand behind those of the lane in front of it: the lanes read the pieces in the order of their places.
-    // e4m3: through registers, turned into bf16.
+    // e4m3: through registers, turned into bf16, with the sign of their scale; NaN all of them if it is not finite.
     uint32_t piece_at[FP8 ? 1 : LOADS];
     if constexpr (!FP8)
 #pragma unroll
@@ -176,8 +176,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) bring_part(block, i, tile, quarter, in);
     };
-    auto put = [&](const u32x4 (&in)[FP8 ? LOADS : 1], Tile<D> &tile, int quarter) __attribute__((always_inline)) {
-        if constexpr (FP8)
+    auto put = [&](const u32x4 (&in)[FP8 ? LOADS : 1], Tile<D> &tile, int quarter, int scale) __attribute__((always_inline)) {
+        if constexpr (FP8) {
+            const uint32_t sign = (uint32_t)(scale >> 31) & 0x80808080u, nan = (scale & 0x7fffffff) > kFloatMax ? 0x7f7f7f7fu : 0u;
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
                 const int el = (i * 64 + lane) * 16, t = el / D, col = el % D / 8;   // first element: row, piece
@@ -186,12 +187,14 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
                     u32x4 w;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        w[2 * j] = fp8x2_to_bf16x2<false>(in[i][2 * p + j]);
-                        w[2 * j + 1] = fp8x2_to_bf16x2<true>(in[i][2 * p + j]);
+                        const uint32_t four = (in[i][2 * p + j] ^ sign) | nan;
+                        w[2 * j] = fp8x2_to_bf16x2<false>(four);
+                        w[2 * j + 1] = fp8x2_to_bf16x2<true>(four);
                     }
                     tile.w[quarter * kTile + t][(col + p) ^ turn<D>(t)] = w;
                 }
             }
+        }
     };
     // A step that some row of the tile does not see all of, once this wavefront's block of its values is in LDS.  What stands behind the last token is of no
     // one; a value that is not finite is taken out of the product, in which it would reach every row (0 * inf), and added to the rows that see it.
@@ -264,33 +267,63 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
             for (int e = 0; e < NB; ++e) x[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], q[e][k], x[e], 0, 0, 0);
     };
     // What scores need before their exponentials: scales (one to 16 keys: they are in eight accumulators), mask, the largest of each row, and a reference that
-    // follows it when it has risen by kLag.
-    float vs[2] = {1.f, 1.f}, vs_next[2] = {1.f, 1.f}, ks_next[2] = {1.f, 1.f};   // of this step's values, of the next step's values and keys
-    int sid[2] = {0, 0};                                                           // blocks of the step whose scales are read next
-    auto scales = [&](int step) __attribute__((always_inline)) {
+    // follows it when it has risen by kLag.  Scales count by their magnitudes here, of keys never quite zero (a masked score stays minus infinity), and never
+    // infinite or NaN (a weight of zero stays zero): the rest of them is in what LDS holds.
+    // (Their bits are compared and cut as integers, which scalar instructions do.)
+    float ks[2] = {c, c}, ks_next[2] = {c, c};                       // this step's, the next step's
+    float vl[2] = {}, vl_next[2] = {}, vr[2] = {}, vr_next[2] = {};   // the scale of values: its logarithm, its inverse
+    int k_raw[2] = {}, v_raw[2] = {};                                // and, as bits, those of the step behind it
+    int sid[2] = {0, 0};                                             // and the blocks of the one behind that
+    auto scale_of = [&](scalar_ints scales, int id) __attribute__((always_inline)) { return scales[(int64_t)id * a.num_kv_heads + g]; };
+    auto ask_scales = [&]() __attribute__((always_inline)) {
         if constexpr (FP8)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int64_t tile = (int64_t)sid[j] * a.num_kv_heads + g;
-                ks_next[j] = k_scales[tile] * c;
-                vs_next[j] = v_scales[tile];
-                sid[j] = block_id(step + 1, j);
+                k_raw[j] = scale_of(k_scales, sid[j]);
+                v_raw[j] = scale_of(v_scales, sid[j]);
             }
     };
-    // The largest of a row's 16 scores in the lane, in eight parts; the scores are scaled and masked on the way.
-    auto largest = [&](auto masked, int step, int e, float16v &x, int part, float top) __attribute__((always_inline)) {
-        const int lo = part ? 2 * part + 1 : 0, hi = part < 7 ? 2 * part + 3 : 16;
-        const int seen = lim[e] - step * kKeys - 4 * half;    // keys up to this one, counted from the lane's first
+    auto ask_blocks = [&](int step) __attribute__((always_inline)) {
+        if constexpr (FP8) {
+            sid[0] = block_id(step, 0);
+            sid[1] = block_id(step, 1);
+        }
+    };
+    auto take_scales = [&]() __attribute__((always_inline)) {
+        if constexpr (FP8)
 #pragma unroll
-        for (int i = lo; i < hi; ++i) {
-            if constexpr (FP8) x[i] *= ks_next[i / 8];
-            if constexpr (decltype(masked)::value)
+            for (int j = 0; j < 2; ++j) {
+                ks_next[j] = __int_as_float(uniform(__float_as_int(__int_as_float(min(max(k_raw[j] & 0x7fffffff, 0x0da24260 /* 1e-30 */), kFloatMax)) * c)));
+                const float v = __int_as_float(min(max(v_raw[j] & 0x7fffffff, 0x0da24260), kFloatMax));
+                vl_next[j] = __int_as_float(uniform(__float_as_int(__builtin_amdgcn_logf(v))));
+                vr_next[j] = __int_as_float(uniform(__float_as_int(__builtin_amdgcn_rcpf(v))));
+            }
+    };
+    auto step_scales = [&]() __attribute__((always_inline)) {
+        if constexpr (FP8)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                ks[j] = ks_next[j];
+                vl[j] = vl_next[j];
+                vr[j] = vr_next[j];
+            }
+    };
+    // The largest of a row's 16 scores in the lane, in four parts for either eight; the scores are masked on the way.
+    auto largest = [&](auto masked, int step, int e, float16v &x, int part, float (&top)[2]) __attribute__((always_inline)) {
+        const int group = part / 4, lo = group * 8 + (part % 4 ? 2 * (part % 4) + 1 : 0), hi = group * 8 + (part % 4 < 3 ? 2 * (part % 4) + 3 : 8);
+        if constexpr (decltype(masked)::value) {
+            const int seen = lim[e] - step * kKeys - 4 * half;    // keys up to this one, counted from the lane's first
+#pragma unroll
+            for (int i = lo; i < hi; ++i)
                 if (i / 4 * 8 + i % 4 > seen) x[i] = -__builtin_inff();
         }
-        if (part == 0) return max3(x[0], x[1], x[2]);
-        return part < 7 ? max3(top, x[lo], x[lo + 1]) : __builtin_elementwise_maximum(top, x[15]);
+        if (part % 4 == 0) top[group] = max3(x[lo], x[lo + 1], x[lo + 2]);
+        else top[group] = part % 4 < 3 ? max3(top[group], x[lo], x[lo + 1]) : __builtin_elementwise_maximum(top[group], x[lo]);
     };
-    auto whole_row = [&](float top) __attribute__((always_inline)) { return FP8 ? max_of_halves(top) : max_of_halves(top) * c; };
+    auto whole_row = [&](const float (&top)[2]) __attribute__((always_inline)) {
+        if constexpr (FP8) return max_of_halves(__builtin_elementwise_maximum(top[0] * ks_next[0], top[1] * ks_next[1]));
+        else return max_of_halves(__builtin_elementwise_maximum(top[0], top[1])) * c;
+    };
     auto follow = [&](const float (&top)[NB]) __attribute__((always_inline)) {
         bool rise = false;
 #pragma unroll
@@ -309,18 +342,27 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
         }
     };
     // Score j of the lane's 16 NB on its way to a weight: the exponents of the next one, its exponential, the sum and the rounding of those in front of it.
+    float ref = 0.f, part_sum = 0.f;
     auto advance = [&](float16v (&x)[NB], int j, bf16x8 (&pk)[NB][2]) __attribute__((always_inline)) {
         auto exponent = [&](int i) __attribute__((always_inline)) {
-            const float v = x[i / 16][i % 16];
-            x[i / 16][i % 16] = FP8 ? v - m[i / 16] : __builtin_fmaf(v, c, -m[i / 16]);
+            if constexpr (FP8) {
+                if (i % 8 == 0) ref = m[i / 16] - vl[i % 16 / 8];
+                x[i / 16][i % 16] = __builtin_fmaf(x[i / 16][i % 16], ks[i % 16 / 8], -ref);
+            } else {
+                x[i / 16][i % 16] = __builtin_fmaf(x[i / 16][i % 16], c, -m[i / 16]);
+            }
         };
         if (j == 0) exponent(0);
         if (j + 1 < 16 * NB) exponent(j + 1);
         if (j < 16 * NB) x[j / 16][j % 16] = __builtin_amdgcn_exp2f(x[j / 16][j % 16]);
         if (j > 0) {
             const int i = j - 1;
-            l[i / 16] += x[i / 16][i % 16];
-            if constexpr (FP8) x[i / 16][i % 16] *= vs[i % 16 / 8];
+            if constexpr (FP8) {
+                part_sum = i % 8 ? part_sum + x[i / 16][i % 16] : x[i / 16][i % 16];
+                if (i % 8 == 7) l[i / 16] = __builtin_fmaf(part_sum, vr[i % 16 / 8], l[i / 16]);
+            } else {
+                l[i / 16] += x[i / 16][i % 16];
+            }
             if (i % 2) {
                 u32x4 w = __builtin_bit_cast(u32x4, pk[i / 16][i % 16 / 8]);
                 w[i % 8 / 2] = pack_bf16(x[i / 16][i % 16 - 1], x[i / 16][i % 16]);
@@ -332,7 +374,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
 #pragma unroll
         for (int e = 0; e < NB; ++e)
             for (int pos = max(first, full) * kKeys; pos <= lim[e]; ++pos) {
-                const int64_t at0 = (((int64_t)table[pos / kTile] * a.num_kv_heads + g) * kTile + pos % kTile) * D + half * 4;
+                const int64_t block = (int64_t)block_table[(int64_t)s.b * a.max_blocks + pos / kTile] * a.num_kv_heads + g, at0 = (block * kTile + pos % kTile) * D + half * 4;
+                const float scale = FP8 ? v_scale[block] : 1.f;
 #pragma unroll
                 for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -341,6 +384,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
                         float v;
                         if constexpr (FP8) v = __builtin_amdgcn_cvt_f32_fp8((int)static_cast<const uint8_t *>(a.v)[at], 0);
                         else v = __uint_as_float((uint32_t) static_cast<const uint16_t *>(a.v)[at] << 16);
+                        if constexpr (FP8) v *= scale;
                         if (!__builtin_isfinite(v)) o[e][b][i] += v;
                     }
             }
@@ -354,10 +398,11 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
     // k_read: the tile of step t + 2's keys, v_read: of step t's values; k_next, v_next: those that are free after the meeting.
     bf16x8 kf[KS];
     int kid = 0, vid = 0;   // this wavefront's blocks to bring next
+    int k_put = 0, v_put = 0, v_put_next = 0;   // the scales of the blocks that are on their way
     int odd_seen = 0;       // values that are not finite were taken out
     // the meeting of the wavefronts; dirty: values of theirs have to be cleaned in front of it
     auto meet = [&](bool dirty, int t, Tile<D> &v_new, int pair) __attribute__((always_inline)) {
-        if constexpr (FP8) put(in_v, v_new, wave);
+        if constexpr (FP8) put(in_v, v_new, wave, v_put);
         const int vstep = t + 1 + (wave >> 1);   // of the values that this wavefront has brought
         if (dirty && vstep >= full) {
             if constexpr (!FP8) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
@@ -390,15 +435,21 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
                 if constexpr (!ODD) {
                     kid = block_id(t + 5, wave);
                     vid = block_id(t + 4, wave);
+                } else if constexpr (FP8) {
+                    k_put = scale_of(k_scales, kid);
+                    v_put_next = scale_of(v_scales, vid);
                 }
-                scales(t + 1);
+                take_scales();
+                ask_scales();
+                ask_blocks(t + 3);
             }
             __builtin_amdgcn_sched_barrier(0);
         });
         if constexpr (ODD) meet(MASKED, t, v_new, pair ^ 1);
-        else put(in_k, k_new, wave);
+        else put(in_k, k_new, wave, k_put);
         const char *k_block = block_at(k_base, kid), *v_block = block_at(v_base, vid);
-        float top[NB];
+        if constexpr (ODD) v_put = v_put_next;
+        float top[NB][2];
         __builtin_amdgcn_sched_barrier(0);
         each<0, M2>([&](auto number) __attribute__((always_inline)) {
             constexpr int I = decltype(number)::value, E = I / FRAGS, F = I % FRAGS;
@@ -411,25 +462,29 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
                     else bring_part(v_block, i - LOADS, v_next, wave, in_v);
                 });
             each<parts_by(I), parts_by(I + 1)>([&](auto part) __attribute__((always_inline)) {
-                top[part / 8] = largest(masked, t + 1, part / 8, y[part / 8], part % 8, top[part / 8]);
+                largest(masked, t + 1, part / 8, y[part / 8], part % 8, top[part / 8]);
             });
             __builtin_amdgcn_sched_barrier(0);
         });
         if (MASKED && t >= full) odd_seen |= odd_flags[pair][2 * ODD] | odd_flags[pair][2 * ODD + 1];
+        float row_top[NB];
 #pragma unroll
-        for (int e = 0; e < NB; ++e) top[e] = whole_row(top[e]);
-        follow(top);
-        vs[0] = vs_next[0];
-        vs[1] = vs_next[1];
+        for (int e = 0; e < NB; ++e) row_top[e] = whole_row(top[e]);
+        follow(row_top);
+        step_scales();
     };
     // a wavefront without rows
     auto idle_step = [&](auto parity, int t, Tile<D> &k_new, Tile<D> &v_new, Tile<D> &k_next, Tile<D> &v_next, int pair) __attribute__((always_inline)) {
         if constexpr (decltype(parity)::value) {
             meet(true, t, v_new, pair ^ 1);
             bring(k_base, kid, k_next, wave, in_k);
+            if constexpr (FP8) {
+                k_put = scale_of(k_scales, kid);
+                v_put = scale_of(v_scales, vid);
+            }
             bring(v_base, vid, v_next, wave, in_v);
         } else {
-            put(in_k, k_new, wave);
+            put(in_k, k_new, wave, k_put);
             kid = block_id(t + 5, wave);
             vid = block_id(t + 4, wave);
         }
@@ -445,12 +500,17 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
     if (first < end) {
         // keys of the first three steps, values of the first two
         u32x4 in_0[FP8 ? LOADS : 1];
-        if (wave < 2) bring(k_base, block_id(first, wave), k_even, 2 + wave, in_0);
-        bring(k_base, block_id(first + 1, wave), k_odd, wave, in_k);
-        bring(v_base, block_id(first, wave), v_even, wave, in_v);
-        if (wave < 2) put(in_0, k_even, 2 + wave);
-        put(in_k, k_odd, wave);
-        put(in_v, v_even, wave);
+        const int id_0 = block_id(first, wave), id_1 = block_id(first + 1, wave), id_2 = block_id(first + 2, wave), id_3 = block_id(first + 3, wave);
+        if (wave < 2) bring(k_base, id_0, k_even, 2 + wave, in_0);
+        bring(k_base, id_1, k_odd, wave, in_k);
+        bring(v_base, id_0, v_even, wave, in_v);
+        if constexpr (FP8) {
+            if (wave < 2) put(in_0, k_even, 2 + wave, scale_of(k_scales, id_0));
+            put(in_k, k_odd, wave, scale_of(k_scales, id_1));
+            put(in_v, v_even, wave, scale_of(v_scales, id_0));
+            k_put = scale_of(k_scales, id_3);
+            v_put = scale_of(v_scales, id_2);
+        }
         if (first + (wave >> 1) >= full) {
             if constexpr (!FP8) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
             clean(first + (wave >> 1), v_even, 0);
@@ -460,34 +520,34 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
             float16v x[NB], y[NB];
 #pragma unroll
             for (int k = 0; k < KS; ++k) kf[k] = read_keys(k_even, 1, k);
-            if constexpr (FP8) {
-                sid[0] = block_id(first, 0);
-                sid[1] = block_id(first, 1);
-            }
-            scales(first);
+            ask_blocks(first);
+            ask_scales();
+            take_scales();
+            ask_blocks(first + 1);
+            ask_scales();
+            ask_blocks(first + 2);
             scores(kf, x);
-            float top[NB];
+            float top[NB][2], row_top[NB];
 #pragma unroll
             for (int e = 0; e < NB; ++e) {
-                each<0, 8>([&](auto part) __attribute__((always_inline)) { top[e] = largest(std::true_type{}, first, e, x[e], part, top[e]); });
-                top[e] = whole_row(top[e]);
+                each<0, 8>([&](auto part) __attribute__((always_inline)) { largest(std::true_type{}, first, e, x[e], part, top[e]); });
+                row_top[e] = whole_row(top[e]);
             }
-            follow(top);
-            vs[0] = vs_next[0];
-            vs[1] = vs_next[1];
+            follow(row_top);
+            step_scales();
 #pragma unroll
             for (int k = 0; k < KS; ++k) kf[k] = read_keys(k_odd, 0, k);
             team_barrier<false>();   // (new keys come to where these were)
-            bring(k_base, block_id(first + 3, wave), k_even, wave, in_k);
-            bring(v_base, block_id(first + 2, wave), v_odd, wave, in_v);
+            bring(k_base, id_3, k_even, wave, in_k);
+            bring(v_base, id_2, v_odd, wave, in_v);
             int t = first;
             for (const int fast_end = min(full, end) - 5; t < fast_end; t += 4) four_steps(std::false_type{}, t, x, y);
             for (; t < end; t += 4) four_steps(std::true_type{}, t, x, y);
             if (__builtin_expect(odd_seen != 0, 0)) add_odd();
         } else {
             team_barrier<false>();
-            bring(k_base, block_id(first + 3, wave), k_even, wave, in_k);
-            bring(v_base, block_id(first + 2, wave), v_odd, wave, in_v);
+            bring(k_base, id_3, k_even, wave, in_k);
+            bring(v_base, id_2, v_odd, wave, in_v);
             for (int t = first; t < end; t += 4) {
                 idle_step(std::false_type{}, t, k_even, v_odd, k_odd, v_even, 0);
                 if (t + 1 < end) idle_step(std::true_type{}, t + 1, k_even, v_odd, k_odd, v_even, 0);
