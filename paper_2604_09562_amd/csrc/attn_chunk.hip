@@ -176,25 +176,23 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) bring_part(block, i, tile, quarter, in);
     };
-    auto put = [&](const u32x4 (&in)[FP8 ? LOADS : 1], Tile<D> &tile, int quarter, int scale) __attribute__((always_inline)) {
-        if constexpr (FP8) {
-            const uint32_t sign = (uint32_t)(scale >> 31) & 0x80808080u, nan = (scale & 0x7fffffff) > kFloatMax ? 0x7f7f7f7fu : 0u;
+    // part i of 2 LOADS
+    auto put_part = [&](const u32x4 (&in)[FP8 ? LOADS : 1], int i, Tile<D> &tile, int quarter, int scale) __attribute__((always_inline)) {
+        const uint32_t sign = (uint32_t)(scale >> 31) & 0x80808080u, nan = (scale & 0x7fffffff) > kFloatMax ? 0x7f7f7f7fu : 0u;
+        const int el = (i / 2 * 64 + lane) * 16, t = el / D, col = el % D / 8;   // first element: row, piece
+        u32x4 w;
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int el = (i * 64 + lane) * 16, t = el / D, col = el % D / 8;   // first element: row, piece
-#pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    u32x4 w;
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const uint32_t four = (in[i][2 * p + j] ^ sign) | nan;
-                        w[2 * j] = fp8x2_to_bf16x2<false>(four);
-                        w[2 * j + 1] = fp8x2_to_bf16x2<true>(four);
-                    }
-                    tile.w[quarter * kTile + t][(col + p) ^ turn<D>(t)] = w;
-                }
-            }
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t four = (in[i / 2][2 * (i % 2) + j] ^ sign) | nan;
+            w[2 * j] = fp8x2_to_bf16x2<false>(four);
+            w[2 * j + 1] = fp8x2_to_bf16x2<true>(four);
         }
+        tile.w[quarter * kTile + t][(col + i % 2) ^ turn<D>(t)] = w;
+    };
+    auto put = [&](const u32x4 (&in)[FP8 ? LOADS : 1], Tile<D> &tile, int quarter, int scale) __attribute__((always_inline)) {
+        if constexpr (FP8)
+#pragma unroll
+            for (int i = 0; i < 2 * LOADS; ++i) put_part(in, i, tile, quarter, scale);
     };
     // A step that some row of the tile does not see all of, once this wavefront's block of its values is in LDS.  What stands behind the last token is of no
     // one; a value that is not finite is taken out of the product, in which it would reach every row (0 * inf), and added to the rows that see it.
@@ -275,6 +273,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
     int k_raw[2] = {}, v_raw[2] = {};                                // and, as bits, those of the step behind it
     int sid[2] = {0, 0};                                             // and the blocks of the one behind that
     auto scale_of = [&](scalar_ints scales, int id) __attribute__((always_inline)) { return scales[(int64_t)id * a.num_kv_heads + g]; };
+    auto magnitude = [&](int scale) __attribute__((always_inline)) { return __int_as_float(min(max(scale & 0x7fffffff, 0x0da24260 /* 1e-30 */), kFloatMax)); };
     auto ask_scales = [&]() __attribute__((always_inline)) {
         if constexpr (FP8)
 #pragma unroll
@@ -289,14 +288,18 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
             sid[1] = block_id(step, 1);
         }
     };
-    auto take_scales = [&]() __attribute__((always_inline)) {
+    auto take_key_scales = [&]() __attribute__((always_inline)) {
+        if constexpr (FP8)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                ks_next[j] = __int_as_float(uniform(__float_as_int(magnitude(k_raw[j]) * c)));
+    };
+    auto take_value_scales = [&]() __attribute__((always_inline)) {
         if constexpr (FP8)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                ks_next[j] = __int_as_float(uniform(__float_as_int(__int_as_float(min(max(k_raw[j] & 0x7fffffff, 0x0da24260 /* 1e-30 */), kFloatMax)) * c)));
-                const float v = __int_as_float(min(max(v_raw[j] & 0x7fffffff, 0x0da24260), kFloatMax));
-                vl_next[j] = __int_as_float(uniform(__float_as_int(__builtin_amdgcn_logf(v))));
-                vr_next[j] = __int_as_float(uniform(__float_as_int(__builtin_amdgcn_rcpf(v))));
+                vl_next[j] = __int_as_float(uniform(__float_as_int(__builtin_amdgcn_logf(magnitude(v_raw[j])))));
+                vr_next[j] = __int_as_float(uniform(__float_as_int(__builtin_amdgcn_rcpf(magnitude(v_raw[j])))));
             }
     };
     auto step_scales = [&]() __attribute__((always_inline)) {
@@ -402,7 +405,6 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
     int odd_seen = 0;       // values that are not finite were taken out
     // the meeting of the wavefronts; dirty: values of theirs have to be cleaned in front of it
     auto meet = [&](bool dirty, int t, Tile<D> &v_new, int pair) __attribute__((always_inline)) {
-        if constexpr (FP8) put(in_v, v_new, wave, v_put);
         const int vstep = t + 1 + (wave >> 1);   // of the values that this wavefront has brought
         if (dirty && vstep >= full) {
             if constexpr (!FP8) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
@@ -431,22 +433,26 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
             y[E] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[K], q[E][K], y[E], 0, 0, 0);
             each<values_by(I), values_by(I + 1)>([&](auto f) __attribute__((always_inline)) { vf[f / DB][f % DB] = read_values(v_read, ODD, f / DB, f % DB); });
             each<I * EXPS / M1, (I + 1) * EXPS / M1>([&](auto j) __attribute__((always_inline)) { advance(x, j, pk); });
-            if constexpr (I == M1 / 2) {   // (scalar loads, which whoever waits for LDS waits for: where nothing is waited for until the second part)
-                if constexpr (!ODD) {
-                    kid = block_id(t + 5, wave);
-                    vid = block_id(t + 4, wave);
-                } else if constexpr (FP8) {
-                    k_put = scale_of(k_scales, kid);
-                    v_put_next = scale_of(v_scales, vid);
-                }
-                take_scales();
+            // (scalar loads, which whoever waits for LDS waits for: where nothing is waited for until the second part)
+            constexpr int J = I - M1 / 2;
+            if constexpr (J == 0 && !ODD) {
+                kid = block_id(t + 5, wave);
+                vid = block_id(t + 4, wave);
+            }
+            if constexpr (J == 0 && ODD && FP8) {
+                k_put = scale_of(k_scales, kid);
+                v_put_next = scale_of(v_scales, vid);
+            }
+            if constexpr (J == 1) take_key_scales();
+            if constexpr (J == 2) take_value_scales();
+            if constexpr (J == 3) {
                 ask_scales();
                 ask_blocks(t + 3);
             }
+            if constexpr (FP8 && I >= M1 - 2 * LOADS) put_part(ODD ? in_v : in_k, I - (M1 - 2 * LOADS), ODD ? v_new : k_new, wave, ODD ? v_put : k_put);
             __builtin_amdgcn_sched_barrier(0);
         });
         if constexpr (ODD) meet(MASKED, t, v_new, pair ^ 1);
-        else put(in_k, k_new, wave, k_put);
         const char *k_block = block_at(k_base, kid), *v_block = block_at(v_base, vid);
         if constexpr (ODD) v_put = v_put_next;
         float top[NB][2];
@@ -476,6 +482,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
     // a wavefront without rows
     auto idle_step = [&](auto parity, int t, Tile<D> &k_new, Tile<D> &v_new, Tile<D> &k_next, Tile<D> &v_next, int pair) __attribute__((always_inline)) {
         if constexpr (decltype(parity)::value) {
+            put(in_v, v_new, wave, v_put);
             meet(true, t, v_new, pair ^ 1);
             bring(k_base, kid, k_next, wave, in_k);
             if constexpr (FP8) {
@@ -522,7 +529,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
             for (int k = 0; k < KS; ++k) kf[k] = read_keys(k_even, 1, k);
             ask_blocks(first);
             ask_scales();
-            take_scales();
+            take_key_scales();
+            take_value_scales();
             ask_blocks(first + 1);
             ask_scales();
             ask_blocks(first + 2);
