@@ -6,6 +6,8 @@
 // e4m3 caches: the rows of a block stand as far apart in the call as their slots (a run); a wavefront takes a run's keys or values of one
 // head, has the largest magnitude of all of them in registers before it rounds the first, and writes each row's codes.  One read of the values
 // instead of the two that a row by itself needs.
+#include <type_traits>
+
 #include "prefill.h"
 
 namespace ss {
@@ -85,13 +87,35 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvWriteArgs a, uint32_t p
     store_eight<KV_DT, NEW_DT>(a.v, to, v);
 }
 
-__device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d, float scale)
+// The code of x / scale, the quotient rounded once to fp32 (as one IEEE division gives it) and cut at the largest code.
+//
+// Within 2^-60 .. 2^60 a quotient is the product with the rounded inverse, corrected twice by what it leaves of x: the product is at most two steps off and the
+// first correction leaves less than one, from where the second one, with an inverse that is off by at most half a step, gives the nearest number (Markstein's
+// theorem).  Remainders are exact but for x so small that the code is zero anyway, and x is cut first, so that nothing overflows: 448 scale may be rounded up,
+// by less than the 16 that a quotient may be above 448 and still round to it.  Seven instructions instead of a division's 15: 15.8 us instead of 21.6 where
+// 43 MB of bf16 become 21 MB of codes.
+struct Divisor {
+    float scale, inverse, limit;
+    bool near_one;
+    __device__ explicit Divisor(float s) : scale(s), inverse(1.0f / s), limit(kFp8Max * fabsf(s)), near_one(fabsf(s) >= 0x1p-60f && fabsf(s) <= 0x1p60f) {}
+    template <bool NEAR_ONE>
+    __device__ float operator()(float x) const
+    {
+        // (saturated: the cache never holds the NaN byte for finite input)
+        if constexpr (!NEAR_ONE) return fminf(fmaxf(x / scale, -kFp8Max), kFp8Max);
+        x = __builtin_amdgcn_fmed3f(x, -limit, limit);
+        const float product = x * inverse;
+        float q = product;
+        q = __builtin_fmaf(__builtin_fmaf(-q, scale, x), inverse, q);
+        q = __builtin_fmaf(__builtin_fmaf(-q, scale, x), inverse, q);
+        return __builtin_copysignf(q, product);   // (corrections of minus zero are plus zero)
+    }
+};
+template <bool NEAR_ONE, typename EIGHT>
+__device__ __forceinline__ uint32_t four_codes(const EIGHT &x, int e, const Divisor &by)
 {
-    // one IEEE division each, saturated: the cache never holds the NaN byte for finite input
-    const float x0 = fminf(fmaxf(a / scale, -kFp8Max), kFp8Max), x1 = fminf(fmaxf(b / scale, -kFp8Max), kFp8Max);
-    const float x2 = fminf(fmaxf(c / scale, -kFp8Max), kFp8Max), x3 = fminf(fmaxf(d / scale, -kFp8Max), kFp8Max);
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(x0, x1, 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(x2, x3, w, true);
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(by.operator()<NEAR_ONE>(x.value(e)), by.operator()<NEAR_ONE>(x.value(e + 1)), 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(by.operator()<NEAR_ONE>(x.value(e + 2)), by.operator()<NEAR_ONE>(x.value(e + 3)), w, true);
     return (uint32_t)w;
 }
 
@@ -147,14 +171,17 @@ __global__ __launch_bounds__(256) void kv_write_e4m3_kernel(KvWriteArgs a, int w
             scale = top > 0.f ? top / kFp8Max : 1.0f;
             if (lane == 0) scales[tile] = scale;
         }
+        const Divisor by(scale);
+        auto write = [&](auto near_one) __attribute__((always_inline)) {
+            constexpr bool NEAR_ONE = decltype(near_one)::value;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (run >> (i * ROWS + sub) & 1) {
-                u32x2 w;
-                w.x = four_codes(x[i].value(0), x[i].value(1), x[i].value(2), x[i].value(3), scale);
-                w.y = four_codes(x[i].value(4), x[i].value(5), x[i].value(6), x[i].value(7), scale);
-                *reinterpret_cast<u32x2 *>(cache + (tile * kTile + place + i * ROWS + sub) * D + col) = w;
-            }
+            for (int i = 0; i < N; ++i)
+                if (run >> (i * ROWS + sub) & 1)
+                    *reinterpret_cast<u32x2 *>(cache + (tile * kTile + place + i * ROWS + sub) * D + col) =
+                        u32x2{four_codes<NEAR_ONE>(x[i], 0, by), four_codes<NEAR_ONE>(x[i], 4, by)};
+        };
+        if (by.near_one) write(std::true_type{});   // (one scale to the wavefront)
+        else write(std::false_type{});
     }
 }
 

@@ -160,3 +160,34 @@ def test_option_validate_names_the_row():
         run(c)
     finally:
         binding.ss_set_option("validate", 0)
+
+
+@pytest.mark.parametrize("new", ["f32", "bf16"])
+def test_e4m3_codes_at_and_beside_ties(new):
+    """Rows that go on blocks whose scales stand: values at the middles between codes times a scale, the numbers beside them, what is cut, and zeros of both signs,
+    for ordinary scales, both signs, powers of two, mantissas of ones, and those so large or small that their inverses or the products overflow."""
+    codes = torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).float()
+    points = torch.cat([codes, (codes[1:] + codes[:-1]) / 2, torch.tensor([449.0, 463.9, 464.0, 480.0, 1e4, 1e30, 3e38])])
+    scales = [1.0, 0.0123, 1 / 3, 2.0**-7, 1.9999999, 1.0000001, -0.7, 3.0e-5, 2.0**-60, 2.0**-61, 2.0**60, 2.0**61, 1.1e-30, 3.0e30, 1.0e-38, 1.0e-42]
+    c = batch([(1, 2)] * len(scales), 2, 64, "fp8", new, seed=5)
+    blocks = torch.randperm(len(scales) * 4, generator=torch.Generator().manual_seed(3))[:len(scales) * 2].tolist()
+    total = len(scales) * 4
+    gen = torch.Generator().manual_seed(6)
+    k, ks = ref.cache_values((total, 2, 16, 64), "fp8", gen, "cpu")
+    v, vs = ref.cache_values((total, 2, 16, 64), "fp8", gen, "cpu")
+    slots, wide = [], []
+    for i, s in enumerate(scales):
+        s = torch.tensor(s, dtype=torch.float32)
+        x = points * s
+        for _ in range(2):
+            x = torch.cat([x, torch.nextafter(x, torch.tensor(float("inf"))), torch.nextafter(x, torch.tensor(-float("inf")))])
+        x = x[x.isfinite()]
+        x = torch.cat([x, -x])
+        x = x[torch.randint(len(x), (15 * 256,), generator=gen)].reshape(15, 256)
+        for side, block in enumerate(blocks[2 * i:2 * i + 2]):
+            ks[block], vs[block] = s, s
+            slots += [block * 16 + p for p in range(1, 16)]
+            wide.append(x if side == 0 else x.flip(0))
+    c.update(num_blocks=total, k_cache=k, v_cache=v, k_scale=ks, v_scale=vs, wide=torch.cat(wide).to(ref.TORCH[new]), total_rows=len(slots),
+             slots=torch.tensor(slots, dtype=torch.int32))
+    run(c)
