@@ -32,11 +32,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y)
     const float2v v = {x, y};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
-template <bool HI>
-__device__ __forceinline__ uint32_t fp8x2_to_bf16x2(uint32_t w)   // exact
-{
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
-}
 // The largest of three, or NaN (the other kind of maximum costs an instruction more for each operand that may be a signalling NaN).
 __device__ __forceinline__ float max3(float x, float y, float z) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x, y), z); }
 // What the lane of the row's other keys has, joined.
@@ -74,7 +69,7 @@ constexpr int kKeys = kChunkKeys;   // keys that are taken at a time, two cache 
 // What a tile costs beside its steps, in steps.
 constexpr int kOpen = 9;
 constexpr int kPairKeys = 2 * kKeys;
-constexpr int kFloatMax = 0x7f7fffff;   // the largest float's bits
+constexpr int kInfinity = 0x7f800000;   // its bits, those of an exponent too
 
 // 64 keys or values in LDS, rows of D bf16 in pieces of 16 bytes.  Piece c of row t stands at place c ^ turn(t): 16 rows' pieces
 // of equal c fill all banks (scores), and so do four rows' pieces 4 n .. 4 n + 3 (transposing reads of values).
@@ -119,7 +114,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
     // In steps of 32 keys: the share's, and up to where all rows of the tile see everything
     const int first = s.s0, end = s.s1;
     const int full = max((ctx + s.t * ROWS / G + 1) / kKeys, 0);
-    const float c = a.sm_scale * kLog2e;
+    const float c = fmaxf(a.sm_scale * kLog2e, 0x1p-126f);
 #pragma unroll
     for (int e = 0; e < NB; ++e) lim[e] = min(lim[e], end * kKeys - 1);   // (what a step reads behind the share is another one's)
 
@@ -148,7 +143,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
 
     // ---- a cache block into a quarter of a tile ----
     // bf16: straight into LDS, where a lane's 16 bytes stand behind those of the lane in front of it: the lanes read the pieces in the order of their places.
-    // e4m3: through registers, turned into bf16, with the sign of their scale; NaN all of them if it is not finite.
+    // e4m3: through registers, turned into bf16, with the sign and the power of two of their scale, which bf16 holds exactly; NaN
+    // all of them if it is not finite.
     uint32_t piece_at[FP8 ? 1 : LOADS];
     if constexpr (!FP8)
 #pragma unroll
@@ -178,14 +174,15 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
     };
     // part i of 2 LOADS
     auto put_part = [&](const u32x4 (&in)[FP8 ? LOADS : 1], int i, Tile<D> &tile, int quarter, int scale) __attribute__((always_inline)) {
-        const uint32_t sign = (uint32_t)(scale >> 31) & 0x80808080u, nan = (scale & 0x7fffffff) > kFloatMax ? 0x7f7f7f7fu : 0u;
+        const uint32_t sign = (uint32_t)(scale >> 31) & 0x80808080u, nan = (scale & 0x7fffffff) >= kInfinity ? 0x7f7f7f7fu : 0u;
+        const float power = __int_as_float(scale & kInfinity);
         const int el = (i / 2 * 64 + lane) * 16, t = el / D, col = el % D / 8;   // first element: row, piece
         u32x4 w;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const uint32_t four = (in[i / 2][2 * (i % 2) + j] ^ sign) | nan;
-            w[2 * j] = fp8x2_to_bf16x2<false>(four);
-            w[2 * j + 1] = fp8x2_to_bf16x2<true>(four);
+            w[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, power, false));
+            w[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, power, true));
         }
         tile.w[quarter * kTile + t][(col + i % 2) ^ turn<D>(t)] = w;
     };
@@ -265,15 +262,16 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
             for (int e = 0; e < NB; ++e) x[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], q[e][k], x[e], 0, 0, 0);
     };
     // What scores need before their exponentials: scales (one to 16 keys: they are in eight accumulators), mask, the largest of each row, and a reference that
-    // follows it when it has risen by kLag.  Scales count by their magnitudes here, of keys never quite zero (a masked score stays minus infinity), and never
-    // infinite or NaN (a weight of zero stays zero): the rest of them is in what LDS holds.
-    // (Their bits are compared and cut as integers, which scalar instructions do.)
+    // follows it when it has risen by kLag.  Scales count by their fractions here, from one to two: a masked score stays minus infinity, a weight of zero zero, and
+    // no weight leaves the range of floats.  The rest of a scale is in what LDS holds.
+    // The scale of values goes into the exponent: 2^(x - m) vs = 2^(x - (m - log2 vs)), and the sum over the values' block is divided by vs again.  That is two
+    // instructions for eight weights instead of eight (336 -> 298 us for four requests of 1024 tokens with the rest in LDS and scales asked for two steps ahead).
     float ks[2] = {c, c}, ks_next[2] = {c, c};                       // this step's, the next step's
     float vl[2] = {}, vl_next[2] = {}, vr[2] = {}, vr_next[2] = {};   // the scale of values: its logarithm, its inverse
     int k_raw[2] = {}, v_raw[2] = {};                                // and, as bits, those of the step behind it
     int sid[2] = {0, 0};                                             // and the blocks of the one behind that
     auto scale_of = [&](scalar_ints scales, int id) __attribute__((always_inline)) { return scales[(int64_t)id * a.num_kv_heads + g]; };
-    auto magnitude = [&](int scale) __attribute__((always_inline)) { return __int_as_float(min(max(scale & 0x7fffffff, 0x0da24260 /* 1e-30 */), kFloatMax)); };
+    auto fraction = [&](int scale) __attribute__((always_inline)) { return __int_as_float((scale & 0x7fffff) | 0x3f800000); };
     auto ask_scales = [&]() __attribute__((always_inline)) {
         if constexpr (FP8)
 #pragma unroll
@@ -292,14 +290,14 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
         if constexpr (FP8)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                ks_next[j] = __int_as_float(uniform(__float_as_int(magnitude(k_raw[j]) * c)));
+                ks_next[j] = __int_as_float(uniform(__float_as_int(fraction(k_raw[j]) * c)));
     };
     auto take_value_scales = [&]() __attribute__((always_inline)) {
         if constexpr (FP8)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                vl_next[j] = __int_as_float(uniform(__float_as_int(__builtin_amdgcn_logf(magnitude(v_raw[j])))));
-                vr_next[j] = __int_as_float(uniform(__float_as_int(__builtin_amdgcn_rcpf(magnitude(v_raw[j])))));
+                vl_next[j] = __int_as_float(uniform(__float_as_int(__builtin_amdgcn_logf(fraction(v_raw[j])))));
+                vr_next[j] = __int_as_float(uniform(__float_as_int(__builtin_amdgcn_rcpf(fraction(v_raw[j])))));
             }
     };
     auto step_scales = [&]() __attribute__((always_inline)) {

@@ -146,7 +146,8 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
                 const int64_t tile = (int64_t)table[pos / kTile] * a.num_kv_heads + g, from = (tile * kTile + pos % kTile) * D + 4 * jq;
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
-                    const float4v v = load4<KV>(a.v, from + 16 * c);
+                    float4v v = load4<KV>(a.v, from + 16 * c);
+                    if constexpr (KV == SS_FP8_E4M3) v *= a.v_scale[tile];
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (!__builtin_isfinite(v[i])) o[c][i] += v[i];

@@ -202,3 +202,37 @@ def test_option_validate_names_the_request():
             binding.ss_chunk_attn(good, *binding.alloc_chunk_outputs(good), max_q_len=19)
     finally:
         binding.ss_set_option("validate", 0)
+
+
+@pytest.mark.parametrize("q", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_scales_that_are_not_finite(q, value):
+    """They reach the rows that see their block and no other."""
+    inp = ref.chunk_batch([(150, 200)], 4, 1, 128, "fp8", q, seed=3)
+    blk = int(inp["block_table"][0, 7])                  # seen from position 112 on, row 62
+    out, z, ws = binding.alloc_chunk_outputs(inp)
+    binding.ss_chunk_attn(inp, out, z, ws)
+    for name in ("k_scale", "v_scale"):
+        odd = dict(inp, **{name: inp[name].clone()})
+        odd[name][blk] = value
+        got, zg, _ = binding.alloc_chunk_outputs(odd)
+        binding.ss_chunk_attn(odd, got, zg, ws)
+        torch.cuda.synchronize()
+        assert torch.equal(got[:62], out[:62]) and torch.equal(zg[:62], z[:62])
+        x = got[62:] if q == "f32" else got[62:].view(torch.bfloat16).float()
+        assert not torch.isfinite(x).any(-1).any()
+
+
+@pytest.mark.parametrize("q", ["bf16", "f32"])
+def test_scales_far_from_one(q):
+    inp = ref.chunk_batch([(70, 300), (1, 40), (33, 90)], 8, 2, 128, "fp8", q, seed=13)
+    for b, (of_keys, of_values) in enumerate(((1e-33, 1e33), (1.0, 1e-33), (1e-42, 1e30))):
+        ids = inp["block_table"][b, :ref.blocks(int(inp["kv_len"][b]))].long()
+        inp["k_scale"][ids] *= of_keys
+        inp["v_scale"][ids] *= of_values
+    run(inp)
+
+
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32")])
+def test_a_scale_of_scores_near_zero(q, kv):
+    run(dict(ref.chunk_batch([(70, 300), (1, 40)], 8, 2, 64, kv, q, seed=14), sm_scale=1e-44))
