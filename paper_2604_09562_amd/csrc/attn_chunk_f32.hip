@@ -46,135 +46,135 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
     ChunkWalk<kRows, kStepKeys, kOpen> s;
     int begun = 0, begun_q0 = 0, begun_rows = 0, begun_row0 = 0;
     for (bool any = s.begin(a, span); any; any = s.next(a)) {
-    if (s.part == 2 * span + 1) {
-        begun = s.pieces();
-        begun_q0 = s.u.q0;
-        begun_rows = s.u.q_len * s.u.G;
-        begun_row0 = s.t * kRows;
-    }
-    const int n16 = lane & 15, jq = lane >> 4;
-    const int G = a.num_q_heads / a.num_kv_heads;
-    const int rows = s.u.q_len * G, n = s.t * kRows + wave * 16 + n16;
-    const int qi = min(n, rows - 1) / G, hh = n % G;
-    const int lim = s.u.kv_len - s.u.q_len + qi;                     // the last position this lane's row sees
-    const int64_t at = (int64_t)(s.u.q0 + qi) * a.num_q_heads + g * G + hh;
-    float4v q[D / 16];   // B operand: d = 16 c + 4 jq ..
+        if (s.part == 2 * span + 1) {
+            begun = s.pieces();
+            begun_q0 = s.u.q0;
+            begun_rows = s.u.q_len * s.u.G;
+            begun_row0 = s.t * kRows;
+        }
+        const int n16 = lane & 15, jq = lane >> 4;
+        const int G = a.num_q_heads / a.num_kv_heads;
+        const int rows = s.u.q_len * G, n = s.t * kRows + wave * 16 + n16;
+        const int qi = min(n, rows - 1) / G, hh = n % G;
+        const int lim = s.u.kv_len - s.u.q_len + qi;                     // the last position this lane's row sees
+        const int64_t at = (int64_t)(s.u.q0 + qi) * a.num_q_heads + g * G + hh;
+        float4v q[D / 16];   // B operand: d = 16 c + 4 jq ..
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) {
-        q[c] = float4v{0.f, 0.f, 0.f, 0.f};
-        if (n < rows) q[c] = load4<QDT>(a.q, (int64_t)(s.u.q0 + qi) * a.q_stride + (int64_t)(g * G + hh) * D + 16 * c + 4 * jq);
-    }
-    // scores are taken to powers of two; the factor in two parts, since fp32 holds it to 2^-24 of a score's size only
-    const double c64 = (double)a.sm_scale * 1.4426950408889634;
-    const float c_hi = (float)c64, c_lo = (float)(c64 - (double)c_hi);
-    const int32_t *table = a.block_table + (int64_t)s.b * a.max_blocks;
-    float m = kChunkNoMax, l = 0.f;
-    float4v o[D / 16];
+        for (int c = 0; c < D / 16; ++c) {
+            q[c] = float4v{0.f, 0.f, 0.f, 0.f};
+            if (n < rows) q[c] = load4<QDT>(a.q, (int64_t)(s.u.q0 + qi) * a.q_stride + (int64_t)(g * G + hh) * D + 16 * c + 4 * jq);
+        }
+        // scores are taken to powers of two; the factor in two parts, since fp32 holds it to 2^-24 of a score's size only
+        const double c64 = (double)a.sm_scale * 1.4426950408889634;
+        const float c_hi = (float)c64, c_lo = (float)(c64 - (double)c_hi);
+        const int32_t *table = a.block_table + (int64_t)s.b * a.max_blocks;
+        float m = kChunkNoMax, l = 0.f;
+        float4v o[D / 16];
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) o[c] = float4v{0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < D / 16; ++c) o[c] = float4v{0.f, 0.f, 0.f, 0.f};
 
-    // Steps from `full` on hold keys that some row of the tile does not see.  There a value that is not finite is taken out of the product, in
-    // which it would reach every row (0 * inf), and added to the rows that see it.
-    const int full = max((s.u.kv_len - s.u.q_len + s.t * kRows / G + 1) / kStepKeys, 0);
-    for (int step = s.s0; step < s.s1; ++step) {
-        bool odd = false;
-        __syncthreads();
+        // Steps from `full` on hold keys that some row of the tile does not see.  There a value that is not finite is taken out of the product, in
+        // which it would reach every row (0 * inf), and added to the rows that see it.
+        const int full = max((s.u.kv_len - s.u.q_len + s.t * kRows / G + 1) / kStepKeys, 0);
+        for (int step = s.s0; step < s.s1; ++step) {
+            bool odd = false;
+            __syncthreads();
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            const int e = i * 64 * kWaves + tid, t = e / (D / 4), d = e % (D / 4) * 4;
-            const int pos = step * kStepKeys + t;
-            float4v k = {0.f, 0.f, 0.f, 0.f}, v = k;
-            if (pos < s.u.kv_len) {   // what stands behind the last token is of no one
-                const int64_t tile = (int64_t)table[pos / kTile] * a.num_kv_heads + g, from = (tile * kTile + pos % kTile) * D + d;
-                k = load4<KV>(a.k, from);
-                v = load4<KV>(a.v, from);
-                if constexpr (KV == SS_FP8_E4M3) { k *= a.k_scale[tile]; v *= a.v_scale[tile]; }
+            for (int i = 0; i < PIECES; ++i) {
+                const int e = i * 64 * kWaves + tid, t = e / (D / 4), d = e % (D / 4) * 4;
+                const int pos = step * kStepKeys + t;
+                float4v k = {0.f, 0.f, 0.f, 0.f}, v = k;
+                if (pos < s.u.kv_len) {   // what stands behind the last token is of no one
+                    const int64_t tile = (int64_t)table[pos / kTile] * a.num_kv_heads + g, from = (tile * kTile + pos % kTile) * D + d;
+                    k = load4<KV>(a.k, from);
+                    v = load4<KV>(a.v, from);
+                    if constexpr (KV == SS_FP8_E4M3) { k *= a.k_scale[tile]; v *= a.v_scale[tile]; }
+                }
+                if (step >= full) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (!__builtin_isfinite(v[c])) { v[c] = 0.f; odd = true; }
+                }
+                *reinterpret_cast<float4v *>(&ks[t][d]) = k;
+                *reinterpret_cast<float4v *>(&vs[t][d]) = v;
             }
-            if (step >= full) {
+            const int any_odd = __syncthreads_or(odd);
+            float4v x[4];
+            float top = kChunkNoMax;
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (!__builtin_isfinite(v[c])) { v[c] = 0.f; odd = true; }
-            }
-            *reinterpret_cast<float4v *>(&ks[t][d]) = k;
-            *reinterpret_cast<float4v *>(&vs[t][d]) = v;
-        }
-        const int any_odd = __syncthreads_or(odd);
-        float4v x[4];
-        float top = kChunkNoMax;
-#pragma unroll
-        for (int tb = 0; tb < 4; ++tb) {
-            float4v acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < D / 16; ++c) {
-                const float4v k = *reinterpret_cast<const float4v *>(&ks[tb * 16 + n16][16 * c + 4 * jq]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i], q[c][i], acc, 0, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (step * kStepKeys + tb * 16 + jq * 4 + i > lim) acc[i] = -__builtin_inff();
-                top = fmaxf(top, acc[i] * c_hi);
-            }
-            x[tb] = acc;
-        }
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float m_new = fmaxf(m, top), down = __builtin_amdgcn_exp2f(m - m_new);
-        m = m_new;
-        l *= down;
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) o[c] *= down;
-#pragma unroll
-        for (int tb = 0; tb < 4; ++tb) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float y = x[tb][i];
-                const float p = y == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(y, c_hi, __builtin_fmaf(y, c_lo, -m)));
-                x[tb][i] = p;
-                l += p;
-            }
-        }
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c)
-#pragma unroll
-            for (int tb = 0; tb < 4; ++tb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vs[tb * 16 + jq * 4 + i][16 * c + n16], x[tb][i], o[c], 0, 0, 0);
-        if (any_odd) {
-            for (int pos = step * kStepKeys; pos < min((step + 1) * kStepKeys, lim + 1); ++pos) {
-                const int64_t tile = (int64_t)table[pos / kTile] * a.num_kv_heads + g, from = (tile * kTile + pos % kTile) * D + 4 * jq;
+            for (int tb = 0; tb < 4; ++tb) {
+                float4v acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
-                    float4v v = load4<KV>(a.v, from + 16 * c);
-                    if constexpr (KV == SS_FP8_E4M3) v *= a.v_scale[tile];
+                    const float4v k = *reinterpret_cast<const float4v *>(&ks[tb * 16 + n16][16 * c + 4 * jq]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i], q[c][i], acc, 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (step * kStepKeys + tb * 16 + jq * 4 + i > lim) acc[i] = -__builtin_inff();
+                    top = fmaxf(top, acc[i] * c_hi);
+                }
+                x[tb] = acc;
+            }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float m_new = fmaxf(m, top), down = __builtin_amdgcn_exp2f(m - m_new);
+            m = m_new;
+            l *= down;
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) o[c] *= down;
+#pragma unroll
+            for (int tb = 0; tb < 4; ++tb) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float y = x[tb][i];
+                    const float p = y == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(y, c_hi, __builtin_fmaf(y, c_lo, -m)));
+                    x[tb][i] = p;
+                    l += p;
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+                for (int tb = 0; tb < 4; ++tb)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (!__builtin_isfinite(v[i])) o[c][i] += v[i];
+                        o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vs[tb * 16 + jq * 4 + i][16 * c + n16], x[tb][i], o[c], 0, 0, 0);
+            if (any_odd) {
+                for (int pos = step * kStepKeys; pos < min((step + 1) * kStepKeys, lim + 1); ++pos) {
+                    const int64_t tile = (int64_t)table[pos / kTile] * a.num_kv_heads + g, from = (tile * kTile + pos % kTile) * D + 4 * jq;
+#pragma unroll
+                    for (int c = 0; c < D / 16; ++c) {
+                        float4v v = load4<KV>(a.v, from + 16 * c);
+                        if constexpr (KV == SS_FP8_E4M3) v *= a.v_scale[tile];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (!__builtin_isfinite(v[i])) o[c][i] += v[i];
+                    }
                 }
             }
         }
-    }
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (s.part >= 0) {
-        const int64_t part = (int64_t)s.part * a.num_kv_heads + g;
-        float4v *po = reinterpret_cast<float4v *>(a.part_o) + part * (kRows * D / 4) + wave * (16 * D / 4) + lane;
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (s.part >= 0) {
+            const int64_t part = (int64_t)s.part * a.num_kv_heads + g;
+            float4v *po = reinterpret_cast<float4v *>(a.part_o) + part * (kRows * D / 4) + wave * (16 * D / 4) + lane;
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) po[c * 64] = o[c];
-        if (jq == 0) {
-            float *ml = a.part_ml + (part * kRows + wave * 16 + n16) * 2;
-            ml[0] = m;
-            ml[1] = l;
+            for (int c = 0; c < D / 16; ++c) po[c * 64] = o[c];
+            if (jq == 0) {
+                float *ml = a.part_ml + (part * kRows + wave * 16 + n16) * 2;
+                ml[0] = m;
+                ml[1] = l;
+            }
+            continue;
         }
-        continue;
-    }
-    if (n < rows) {   // (the walk takes whole wavefronts)
-        const float r = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
+        if (n < rows) {   // (the walk takes whole wavefronts)
+            const float r = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) chunk_store4<QDT>(a.out, at * D + 16 * c + 4 * jq, o[c] * r);
-        if (a.lse && jq == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-    }
+            for (int c = 0; c < D / 16; ++c) chunk_store4<QDT>(a.out, at * D + 16 * c + 4 * jq, o[c] * r);
+            if (a.lse && jq == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+        }
     }
     chunk_record(a, span, g, begun, begun_q0, begun_rows, begun_row0);
 }

@@ -43,7 +43,7 @@ struct ChunkUnit {                   // a request
 
     __device__ __forceinline__ int steps(int t) const
     {
-        const int tok = min((int)((uint32_t)((t + 1) * ROWS - 1) / (uint32_t)G), q_len - 1), seen = kv_len - q_len + tok + 1;
+        const int tok = min((int)(((uint32_t)(t + 1) * ROWS - 1) / (uint32_t)G), q_len - 1), seen = kv_len - q_len + tok + 1;
         return seen > 0 ? (int)(((unsigned)seen + KEYS - 1) / KEYS) : 0;
     }
     __device__ __forceinline__ void set(int q0_, int q1, int len, int G_, int open_)

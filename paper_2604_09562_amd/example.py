@@ -1,12 +1,19 @@
 """A decode lane driven end to end through the library, on synthetic model outputs.
 
-    python -m paper_2604_09562_amd.example [--steps N] [--batch B] [--layers L] [--tree]
+    python -m paper_2604_09562_amd.example [--steps N] [--batch B] [--layers L] [--tree] [--chunk C]
 
-Each step does what a decode worker does around its model (whose projections and logits are stood in
+First the prompts are put into the empty cache, C new tokens of every request at a time:
+
+  blocks      blocks for the new tokens, and where each goes                  ss_block_map
+  write       their keys and values, once per layer                           ss_kv_write
+  attention   over what is in the cache, once per layer                       ss_chunk_attn
+
+Then each step does what a decode worker does around its model (whose projections and logits are stood in
 for by seeded random tensors, there being no weights here):
 
   router      pick the worker for a new request from reported metrics         ss_route_select
   controller  per request, the next draft depth from its last acceptance     ss_depth_update
+  blocks      blocks for the k+1 new tokens, those of rejected ones back      ss_block_map
   append      write the k+1 new tokens' keys/values into the paged cache      ss_kv_append
   attention   verify attention, once per layer; layers after the first        ss_spec_verify_attn
               reuse the first one's plan                                      (SS_BATCH_REUSE_PLAN)
@@ -29,7 +36,7 @@ from . import binding, synth
 
 
 def run(steps: int = 6, batch: int = 8, layers: int = 4, tree: bool = False, vocab: int = 32000, seed: int = 0,
-        verbose: bool = True, sample: bool = False) -> dict:
+        verbose: bool = True, sample: bool = False, chunk: int = 512) -> dict:
     dev = "cuda:0"
     torch.cuda.set_device(0)
     cfg = synth.CONFIGS[1].scaled(batch=batch, vocab=vocab, ctx=("uniform", 200, 1500))
@@ -51,6 +58,45 @@ def run(steps: int = 6, batch: int = 8, layers: int = 4, tree: bool = False, voc
     depth = np.full(batch, 4, dtype=np.int32)
     emitted, t_dev = 0, 0.0
     start_len = cur.copy()
+    sm_scale = cache["sm_scale"]
+
+    # the cache's blocks, all free, and what the requests hold of them
+    i32 = lambda x: binding.to_device(np.asarray(x, dtype=np.int32), dev)  # noqa: E731
+    cache.update(free_ids=i32(np.arange(cache["num_blocks"])), free_count=i32([cache["num_blocks"]]), held=i32(np.zeros(batch)),
+                 block_table=torch.zeros_like(cache["block_table"]))
+    status, ws_b = i32([0]), binding.alloc_block_map_workspace(cache, dev)
+
+    def blocks(d, rows):
+        slots = torch.empty(rows, dtype=torch.int32, device=dev)
+        binding.ss_block_map(d, slots, None, status, ws_b)
+        return slots
+
+    # ---- the prompts
+    prompt_rng = np.random.default_rng(seed + 1)
+    done, chunks, t_prompt = np.zeros_like(cur), 0, 0.0
+    while (done < cur).any():
+        new = np.minimum(cur - done, chunk)
+        done += new
+        q_indptr = np.concatenate([[0], np.cumsum(new)])
+        R = int(q_indptr[-1])
+        d = dict(cache, total_rows=R, q_dtype="bf16", new_dtype="bf16", sm_scale=sm_scale, kv_len=i32(done), q_indptr=i32(q_indptr))
+        # queries, keys and values of a layer are parts of one product's rows
+        wide = torch.from_numpy(prompt_rng.standard_normal((R, (Hq + 2 * Hkv) * D), dtype=np.float32)).to(dev, torch.bfloat16)
+        d["q"], d["k_new"], d["v_new"] = (x.unflatten(1, (-1, D)) for x in wide.split([Hq * D, Hkv * D, Hkv * D], 1))
+        out, lse, ws_c = binding.alloc_chunk_outputs(d, dev)
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        slots = blocks(d, R)
+        for _ in range(layers):
+            binding.ss_kv_write(d, slots)
+            binding.ss_chunk_attn(d, out, lse, ws_c)
+        torch.cuda.synchronize()
+        t_prompt += time.perf_counter() - t0
+        chunks += 1
+        if int(status):
+            raise RuntimeError(f"ss_block_map: status {int(status)}")
+    if verbose:
+        print(f"{int(cur.sum())} prompt tokens in {chunks} chunks, {1e3 * t_prompt / max(chunks, 1):.3f} ms of device work per chunk ({layers} layers)")
 
     for step in range(steps):
         # ---- what the models would hand over: draft tokens/logits, queries and new keys/values per layer
@@ -78,6 +124,7 @@ def run(steps: int = 6, batch: int = 8, layers: int = 4, tree: bool = False, voc
         # ---- the device side of the step
         torch.cuda.synchronize()
         t0 = time.perf_counter()
+        blocks(dict(d, tree_mask=None), R)
         binding.ss_kv_append(d, max_q_len=mq)
         for layer in range(layers):   # one cache stands in for every layer's; the batch metadata is shared
             binding.ss_spec_verify_attn(d, out, lse, ws, max_q_len=mq, reuse_plan=layer > 0)
@@ -94,6 +141,8 @@ def run(steps: int = 6, batch: int = 8, layers: int = 4, tree: bool = False, voc
         t_dev += time.perf_counter() - t0
 
         # ---- feedback: the controller turns each request's acceptance into its next depth
+        if int(status):
+            raise RuntimeError(f"ss_block_map: status {int(status)}")
         n = n_acc.cpu().numpy()
         cur = d["kv_len"].cpu().numpy()
         load, tput = 0.3, 300.0
@@ -115,9 +164,10 @@ def main() -> None:
     ap.add_argument("--batch", type=int, default=8)
     ap.add_argument("--layers", type=int, default=4)
     ap.add_argument("--tree", action="store_true", help="tree-shaped drafts (greedy acceptance unless --sample)")
+    ap.add_argument("--chunk", type=int, default=512, help="new tokens of a request's prompt at a time")
     ap.add_argument("--sample", action="store_true", help="with --tree: the sampled acceptance walk")
     a = ap.parse_args()
-    run(a.steps, a.batch, a.layers, a.tree, sample=a.sample)
+    run(a.steps, a.batch, a.layers, a.tree, sample=a.sample, chunk=a.chunk)
 
 
 if __name__ == "__main__":

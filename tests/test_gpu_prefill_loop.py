@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2604_09562_amd import binding
+from paper_2604_09562_amd import binding, example
 from tests import prefill_ref as ref
 
 pytestmark = pytest.mark.gpu
@@ -196,3 +196,9 @@ def test_captured_steps(kv, q):
         torch.cuda.synchronize()
         for i, (t, w) in enumerate(zip(results, want)):
             assert torch.equal(t.contiguous().view(torch.uint8), w.contiguous().view(torch.uint8)), f"replay {replay}: result {i}"
+
+
+@pytest.mark.parametrize("chunk", [64, 2000])
+def test_the_example_with_prompts_in_chunks(chunk):
+    r = example.run(steps=2, batch=4, layers=2, vocab=4096, seed=1, verbose=False, chunk=chunk)
+    assert int((r["kv_len"] - r["start_len"]).sum()) == r["emitted"]
