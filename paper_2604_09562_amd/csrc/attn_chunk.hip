@@ -5,13 +5,13 @@
 //   S^T[key][row]  = K[key][:] . Q[row][:]       v_mfma_f32_32x32x16_bf16, queries in registers
 //   O^T[d][row]   += V^T[d][key] P^T[key][row]    the same shape; P is taken straight from the accumulators of S^T, V^T by transposing LDS reads
 // so that a lane holds one row: maximum, sum and rescaling of the softmax need no exchange but with the lane that has the row's other keys.  Weights are rounded
-// to bf16, half a step (2^-9) at most; scores, sums and outputs are fp32.
+// to bf16 for the second product, by half a step (2^-8) at most, about as much as the outputs are; scores, sums and outputs are fp32.
 //
 // What bounds it: one wavefront to a SIMD, so every instruction beside the matrix instructions (1024 of a step's cycles) takes issue slots of its own.  A step of
-// a wavefront is 32 matrix instructions, 64 x 32 / 64 exponentials (two slots each), and as many multiply-adds and additions: about 1650 cycles.  Therefore
-// - two blocks of rows to a wavefront: keys and values are read from LDS once for 64 rows (one block: 913 -> 1100 TFLOP/s on 4096 tokens behind 12288);
-// - the next step's scores are made between this step's exponentials, all in a fixed order (-> 1140 TFLOP/s);
-// - bf16 keys and values come into LDS without registers, one meeting of the wavefronts for 64 keys;
+// a wavefront is 32 matrix instructions, 32 exponentials (two slots each), and as many multiply-adds and additions: about 1650 cycles.  Therefore
+// - the next step's scores are made between this step's exponentials (913 -> 1020 TFLOP/s on 4096 tokens behind 12288), all in a fixed order (1100 -> 1140);
+// - two blocks of rows to a wavefront, so that keys and values are read from LDS once for 64 rows, bf16 ones brought there without registers, and one meeting of
+//   the wavefronts for 64 keys (1020 -> 1100);
 // - sums follow a rising maximum only when it has risen by 2^kLag: weights up to 2^16 are exact enough in bf16 and far from fp32's end.
 // 862 us there, 1.12 PFLOP/s, where a large bf16 product of the library reaches 1.27 .. 1.36; 61 us for a prompt of 2048 tokens (32 heads over 8); e4m3 caches:
 // 288 us, 820 TFLOP/s, for four requests of 200 .. 1000 tokens behind 1000 .. 6000 (64 heads over 8), their codes turned to bf16 on the way into LDS.
