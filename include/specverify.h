@@ -476,7 +476,7 @@ int32_t ss_route_select(const ss_worker_metrics *workers, int32_t n, const doubl
  *                   measured by row blocks and cache type above that.  Not used where every unit is a partition (few short units)
  *   "validate"      1 = before launching, ss_spec_verify_attn, ss_chunk_attn, ss_kv_append, ss_kv_write and ss_spec_accept check the
  *                   device-resident metadata with a small kernel (row offsets, lengths against block counts,
- *                   block ids, slots, draft tokens, temperatures, uniforms), synchronise the stream and return
+ *                   block ids, slots (given twice: by rows up to 32768 apart), draft tokens, temperatures, uniforms), synchronise the stream and return
  *                   SS_ERR_INVALID_ARG naming the first inconsistency; 0 (default) = contents are trusted
  * Returns SS_ERR_INVALID_ARG for an unknown name or value.
  */

@@ -105,7 +105,7 @@ __device__ Head sum_requests(const BlockMapArgs &a, SumLds &lds, int32_t *held, 
     __syncthreads();
     Head head = {count, before_t, before_g, 0};
     if (lds.bad != 0x7fffffff) head.status = -1 - lds.bad;
-    else if (count < 0 || (int64_t)count + before_g - before_t > a.num_blocks) head.status = -1 - a.batch;
+    else if (count < 0 || count > a.num_blocks || (int64_t)count + before_g - before_t > a.num_blocks) head.status = -1 - a.batch;
     else if ((int64_t)count + before_g < before_t) head.status = before_t - before_g - count;
     if (tid == 0) {
         taken[a.batch] = before_t;
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(kFillThreads) void block_fill_kernel(BlockMapArgs a
     const int first = blockIdx.x * kFillThreads + threadIdx.x, threads = gridDim.x * kFillThreads;
     if constexpr (LDS) {
         constexpr int N = kLdsRequests + 1;
-        for (int b = threadIdx.x; b <= a.batch; b += kFillThreads) {
+        for (int b = threadIdx.x; b <= a.batch && a.batch > 0; b += kFillThreads) {   // (no requests: there may be no arrays)
             buf[N + b] = taken[b];
             buf[2 * N + b] = given[b];
             buf[3 * N + b] = a.q_indptr[b];

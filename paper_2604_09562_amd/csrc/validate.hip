@@ -156,7 +156,8 @@ __global__ __launch_bounds__(256) void validate_chunk_kernel(const int32_t *bloc
     __threadfence_system();
 }
 
-// Slots inside the cache, each named once; where a block's rows have to be a run, one run.
+// Slots inside the cache, each named once (among so many rows, or the check takes long); where a block's rows have to be a run, one run.
+constexpr int kSlotsBack = 32768;
 __global__ __launch_bounds__(1024) void validate_slots_kernel(const int32_t *slot_map, int total_rows, long long slots, int runs, CheckRecord *out)
 {
     __shared__ int range, twice, run;
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(1024) void validate_slots_kernel(const int32_t *slo
         const int x = slot_map[r];
         if (x < 0) continue;
         if (x >= slots) atomicMin(&range, r);
-        for (int i = 0; i < r; ++i) {
+        for (int i = max(0, r - kSlotsBack); i < r; ++i) {
             const int y = slot_map[i];
             if (y == x) atomicMin(&twice, r);
             else if (runs && y >= 0 && y / kTile == x / kTile && x - y != r - i) atomicMin(&run, r);

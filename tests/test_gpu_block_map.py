@@ -175,3 +175,29 @@ def test_captured_and_replayed():
             x.fill_(-3)
         graph.replay()
         check(c, d, outs)
+
+
+@pytest.mark.parametrize("rows", [0, 9, 5000])
+def test_no_requests_and_no_arrays_of_theirs(rows):
+    c = ref.map_batch([], [], spare_rows=rows)
+    c["q_indptr"] = np.zeros(1, np.int32)
+    d, outs, ws = on_gpu(c)
+    for name in ("q_indptr", "kv_len", "held", "block_table"):
+        d[name] = torch.empty(0, dtype=torch.int32, device="cuda")
+    assert d["q_indptr"].data_ptr() == 0
+    binding.ss_block_map(d, outs[0], outs[1], outs[2], ws)
+    torch.cuda.synchronize()
+    assert int(outs[2]) == 0 and (outs[0] == -1).all() and (outs[1] == -1).all() and int(d["free_count"]) == c["count"]
+
+
+@pytest.mark.parametrize("rows", [12, 5000])
+def test_a_free_list_longer_than_the_cache(rows):
+    """Also where the step takes what is too much of it."""
+    c = ref.map_batch([(12, 40), (rows - 12, rows)], [0, 0])
+    d, outs, ws = on_gpu(c)
+    d["free_count"].fill_(c["num_blocks"] + 2)
+    before = [t.clone() for t in (d["block_table"], d["held"], d["free_ids"], d["free_count"])]
+    binding.ss_block_map(d, outs[0], outs[1], outs[2], ws)
+    torch.cuda.synchronize()
+    assert int(outs[2]) == -3 and (outs[0] == -1).all()
+    assert all(torch.equal(a, b) for a, b in zip(before, (d["block_table"], d["held"], d["free_ids"], d["free_count"])))
