@@ -202,3 +202,60 @@ def test_captured_steps(kv, q):
 def test_the_example_with_prompts_in_chunks(chunk):
     r = example.run(steps=2, batch=4, layers=2, vocab=4096, seed=1, verbose=False, chunk=chunk)
     assert int((r["kv_len"] - r["start_len"]).sum()) == r["emitted"]
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+def test_blocks_behind_four_gigabytes(kv):
+    """Offsets into a long cache pass 32 bits: blocks at its end, written and attended."""
+    num_blocks, hkv, d = 300000, 8, 128
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(3)
+    lengths = [(70, 70), (20, 20)]
+    ids = torch.arange(num_blocks - 8, num_blocks, dtype=torch.int32, device=DEV).flip(0)
+    table = torch.zeros((2, 5), dtype=torch.int32, device=DEV)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    free = torch.empty(num_blocks, dtype=torch.int32, device=DEV)
+    free[:8] = ids
+    b = dict(batch=2, num_q_heads=16, num_kv_heads=hkv, head_dim=d, block_size=16, num_blocks=num_blocks, max_blocks_per_seq=5, total_rows=90, kv_dtype=kv,
+             q_dtype="bf16", new_dtype="bf16", sm_scale=d ** -0.5, block_table=table, held=i32([0, 0]), free_ids=free, free_count=i32([8]), kv_len=i32([70, 20]),
+             q_indptr=i32([0, 70, 90]))
+    for name in ("k", "v"):
+        b[name + "_cache"] = torch.empty((num_blocks, hkv, 16, d), dtype=ref.TORCH[kv], device=DEV)
+        b[name + "_scale"] = torch.empty((num_blocks, hkv), device=DEV) if kv == "fp8" else None
+        b[name + "_new"] = torch.randn((90, hkv, d), generator=gen, device=DEV).to(torch.bfloat16)
+    assert b["k_cache"].nbytes > 4 << 30
+    b["q"] = torch.randn((90, 16, d), generator=gen, device=DEV).to(torch.bfloat16)
+    slots, status = torch.empty(90, dtype=torch.int32, device=DEV), i32([1])
+    binding.ss_block_map(b, slots, None, status, binding.alloc_block_map_workspace(b))
+    binding.ss_kv_write(b, slots)
+    out, lse, ws = binding.alloc_chunk_outputs(b)
+    binding.ss_chunk_attn(b, out, lse, ws)
+    torch.cuda.synchronize()
+    assert int(status) == 0 and int(slots.min()) >= 16 * (num_blocks - 8)
+    place = slots.long()
+    for name in ("k", "v"):
+        got = b[name + "_cache"].view(torch.uint8) if kv == "fp8" else b[name + "_cache"]
+        got = got[place // 16, :, place % 16]
+        new = b[name + "_new"]
+        if kv == "fp8":
+            new = (new.float() / b[name + "_scale"][place // 16][..., None]).clamp(-448.0, 448.0).to(torch.float8_e4m3fn).view(torch.uint8)
+        assert torch.equal(got, new)
+    ref.check_chunk(b, out, lse, kv)
+
+
+def test_two_workers_at_once():
+    """Two batches with caches, pools and workspaces of their own on two streams give what each gives alone."""
+    lanes = [Lane(5, 80, 33, 1, 8, 2, 128, "bf16", "bf16", seed=21 + i) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in lanes]
+    work = []
+    for lane, lengths in zip(lanes, (STEPS[0], STEPS[0][::-1])):
+        b, wide, slot_map, positions = lane.batch_of(lengths)
+        work.append((b, wide, slot_map, positions, [binding.alloc_chunk_outputs(lane.layer(b, wide, 0))]))
+        lane.ws = binding.alloc_block_map_workspace(b)
+    torch.cuda.synchronize()
+    for lane, w, stream in zip(lanes, work, streams):
+        with torch.cuda.stream(stream):
+            lane.enqueue(*w)
+    torch.cuda.synchronize()
+    for lane, w in zip(lanes, work):
+        lane.check(*w, "two at once")
