@@ -103,14 +103,14 @@ struct ChunkWalk {
         spans = uniform(most < 1.0 ? 1 : most < a.spans ? (int)most : a.spans);
         if (span >= spans || total == 0.0) return false;
         share = total / spans;
-        const ChunkPos from = locate(a, __builtin_floor(share * span), mine, incl, G);
+        Unit unused;
+        const ChunkPos from = locate(a, __builtin_floor(share * span), mine, incl, G, u);
         to.b = a.batch;
         to.t = to.off = 0;
-        if (span + 1 < spans) to = locate(a, __builtin_floor(share * (span + 1)), mine, incl, G);
+        if (span + 1 < spans) to = locate(a, __builtin_floor(share * (span + 1)), mine, incl, G, unused);
         base = from.base;
         b = from.b;
         t = from.t;
-        u = request(a, b);
         s0 = from.off;
         if (s0 > 0 && s0 == u.steps(t)) {   // the span in front has all of this tile
             s0 = 0;
@@ -172,8 +172,8 @@ private:
         part = s0 > 0 ? 2 * me : s1 < n ? 2 * me + 1 : -1;
         return true;
     }
-    // Where a cost falls.  mine, incl: the units and sums of the last 64 requests.
-    __device__ __forceinline__ ChunkPos locate(const ChunkArgs &a, double x, Unit mine, double incl, int G) const
+    // Where a cost falls, and in which request.  mine, incl: the units and sums of the last 64 requests.
+    __device__ __forceinline__ ChunkPos locate(const ChunkArgs &a, double x, Unit mine, double incl, int G, Unit &v) const
     {
         const int lane = threadIdx.x & 63;
         ChunkPos p = {a.batch, 0, 0, 0.0};
@@ -186,9 +186,9 @@ private:
             const uint64_t here = __ballot(front + incl > x);
             if (here) {
                 const int at = __builtin_ctzll(here);
-                Unit v;
                 v.G = G;
                 v.open = open;
+                v.q0 = __builtin_amdgcn_readlane(mine.q0, at);
                 v.q_len = __builtin_amdgcn_readlane(mine.q_len, at);
                 v.kv_len = __builtin_amdgcn_readlane(mine.kv_len, at);
                 v.tiles = __builtin_amdgcn_readlane(mine.tiles, at);
