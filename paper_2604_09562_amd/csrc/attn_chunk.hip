@@ -8,13 +8,17 @@
 // to bf16 for the second product, by half a step (2^-8) at most, about as much as the outputs are; scores, sums and outputs are fp32.
 //
 // What bounds it: one wavefront to a SIMD, so every instruction beside the matrix instructions (1024 of a step's cycles) takes issue slots of its own.  A step of
-// a wavefront is 32 matrix instructions, 32 exponentials (two slots each), and as many multiply-adds and additions: about 1650 cycles.  Therefore
+// a wavefront is 32 matrix instructions, 32 exponentials (two slots each), as many multiply-adds and additions, and half as many roundings and sums of them:
+// about 1750 cycles.  Therefore
 // - the next step's scores are made between this step's exponentials (913 -> 1020 TFLOP/s on 4096 tokens behind 12288), all in a fixed order (1100 -> 1140);
 // - two blocks of rows to a wavefront, so that keys and values are read from LDS once for 64 rows, bf16 ones brought there without registers, and one meeting of
 //   the wavefronts for 64 keys (1020 -> 1100);
 // - sums follow a rising maximum only when it has risen by 2^kLag: weights up to 2^16 are exact enough in bf16 and far from fp32's end.
-// 862 us there, 1.12 PFLOP/s, where a large bf16 product of the library reaches 1.27 .. 1.36; 61 us for a prompt of 2048 tokens (32 heads over 8); e4m3 caches:
-// 288 us, 820 TFLOP/s, for four requests of 200 .. 1000 tokens behind 1000 .. 6000 (64 heads over 8), their codes turned to bf16 on the way into LDS.
+// Outputs are divided by the sum of the weights as rounded, a sum of its own (5 %): where a few weights are most of it their roundings cancel, and the error
+// against 64 bits is 1.2 of what rounding the outputs costs instead of 1.4 (scores that spread by 1 to 4).  The log-sum-exp takes the sum of the weights
+// themselves; calls that do not ask for it have a form without that sum (3 % faster).
+// 903 us there, 1.07 PFLOP/s, where a large bf16 product of the library reaches 1.27 .. 1.36; 62 us for a prompt of 2048 tokens (32 heads over 8); e4m3 caches:
+// 307 us, 773 TFLOP/s, for four requests of 200 .. 1000 tokens behind 1000 .. 6000 (64 heads over 8), their codes turned to bf16 on the way into LDS.
 #include <type_traits>
 
 #include "chunk_merge.h"
@@ -42,6 +46,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y)
 {
     const float2v v = {x, y};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+// x and the two of a pair of bf16, added
+__device__ __forceinline__ float pair_sum(uint32_t pair, float x)
+{
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3f803f80u), x, false);
 }
 // The largest of three, or NaN (the other kind of maximum costs an instruction more for each operand that may be a signalling NaN).
 __device__ __forceinline__ float max3(float x, float y, float z) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x, y), z); }
@@ -94,7 +103,7 @@ __device__ __forceinline__ int turn(int t)
     return D == 128 ? (t & 3) << 2 | (t >> 2 & 3) : (t >> 1 & 1) << 2 | (t >> 2 & 3);
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, bool LSE>
 __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, const int32_t *__restrict__ block_table, const float *__restrict__ k_scale,
                                                                const float *__restrict__ v_scale)
 {
@@ -234,12 +243,12 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
             odd_flags[pair][wave] = __ballot(odd) != 0;
         };
 
-        float m[NB], l[NB];
+        float m[NB], l[NB], l_used[NB];   // reference, sum of the weights, sum of the weights as rounded
         float16v o[NB][DB];
 #pragma unroll
         for (int e = 0; e < NB; ++e) {
             m[e] = kChunkNoMax;
-            l[e] = 0.f;
+            l[e] = l_used[e] = 0.f;
 #pragma unroll
             for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -346,6 +355,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
                     const float up = fmaxf(m[e], top[e]), down = __builtin_amdgcn_exp2f(m[e] - up);
                     m[e] = up;
                     l[e] *= down;
+                    l_used[e] *= down;
 #pragma unroll
                     for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -354,7 +364,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
             }
         };
         // Score j of the lane's 16 NB on its way to a weight: the exponents of the next one, its exponential, the sum and the rounding of those in front of it.
-        float ref = 0.f, part_sum = 0.f;
+        float ref = 0.f, part_sum = 0.f, part_used = 0.f;
         auto advance = [&](float16v (&x)[NB], int j, bf16x8 (&pk)[NB][2]) __attribute__((always_inline)) {
             auto exponent = [&](int i) __attribute__((always_inline)) {
                 if constexpr (FP8) {
@@ -369,7 +379,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
             if (j < 16 * NB) x[j / 16][j % 16] = __builtin_amdgcn_exp2f(x[j / 16][j % 16]);
             if (j > 0) {
                 const int i = j - 1;
-                if constexpr (FP8) {
+                if constexpr (!LSE) {
+                } else if constexpr (FP8) {
                     part_sum = i % 8 ? part_sum + x[i / 16][i % 16] : x[i / 16][i % 16];
                     if (i % 8 == 7) l[i / 16] = __builtin_fmaf(part_sum, vr[i % 16 / 8], l[i / 16]);
                 } else {
@@ -378,6 +389,12 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
                 if (i % 2) {
                     u32x4 w = __builtin_bit_cast(u32x4, pk[i / 16][i % 16 / 8]);
                     w[i % 8 / 2] = pack_bf16(x[i / 16][i % 16 - 1], x[i / 16][i % 16]);
+                    if constexpr (FP8) {
+                        part_used = pair_sum(w[i % 8 / 2], i % 8 == 1 ? 0.f : part_used);
+                        if (i % 8 == 7) l_used[i / 16] = __builtin_fmaf(part_used, vr[i % 16 / 8], l_used[i / 16]);
+                    } else {
+                        l_used[i / 16] = pair_sum(w[i % 8 / 2], l_used[i / 16]);
+                    }
                     pk[i / 16][i % 16 / 8] = __builtin_bit_cast(bf16x8, w);
                 }
             }
@@ -578,14 +595,15 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
 #pragma unroll
         for (int e = 0; e < NB; ++e) {
             const int n = n_first + e * 32 + r32;
-            const float sum = sum_of_halves(l[e]);
+            const float used = sum_of_halves(l_used[e]), sum = LSE ? sum_of_halves(l[e]) : used;
             if (s.part >= 0) {
                 const int64_t part = (int64_t)s.part * a.num_kv_heads + g;
+                const float level = used > 0.f ? sum / used : 1.0f;   // (the merge divides by the sum of the weights)
                 float4v *po = reinterpret_cast<float4v *>(a.part_o) + part * (ROWS * D / 4) + (wave * NB + e) * (32 * D / 4) + lane;
 #pragma unroll
                 for (int b = 0; b < DB; ++b)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) po[(b * 4 + j) * 64] = float4v{o[e][b][4 * j], o[e][b][4 * j + 1], o[e][b][4 * j + 2], o[e][b][4 * j + 3]};
+                    for (int j = 0; j < 4; ++j) po[(b * 4 + j) * 64] = float4v{o[e][b][4 * j], o[e][b][4 * j + 1], o[e][b][4 * j + 2], o[e][b][4 * j + 3]} * level;
                 if (half == 0) {
                     float *ml = a.part_ml + (part * ROWS + (wave * NB + e) * 32 + r32) * 2;
                     ml[0] = m[e];
@@ -593,14 +611,14 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
                 }
             } else if (n < rows) {
                 const int64_t at = (int64_t)(s.u.q0 + n / G) * a.num_q_heads + g * G + n % G;
-                const float r = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;   // (a row that sees nothing: zeros; NaN stays)
+                const float r = used > 0.f ? 1.0f / used : used == 0.f ? 0.f : used;   // (a row that sees nothing: zeros; NaN stays)
 #pragma unroll
                 for (int b = 0; b < DB; ++b)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         chunk_store4<SS_BF16>(a.out, at * D + b * 32 + j * 8 + half * 4,
                                               float4v{o[e][b][4 * j], o[e][b][4 * j + 1], o[e][b][4 * j + 2], o[e][b][4 * j + 3]} * r);
-                if (a.lse && half == 0) a.lse[at] = sum == 0.f ? -__builtin_inff() : (m[e] + __builtin_amdgcn_logf(sum)) * kLn2;
+                if (LSE && half == 0) a.lse[at] = sum == 0.f ? -__builtin_inff() : (m[e] + __builtin_amdgcn_logf(sum)) * kLn2;
             }
         }
         team_barrier<false>();   // (the next tile's keys come to where the others may still read)
@@ -608,10 +626,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
     chunk_record(a, span, g, begun, begun_q0, begun_rows, begun_row0);
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, bool LSE>
 int32_t launch(const ChunkArgs &a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((chunk_kernel<D, FP8>), dim3((unsigned)(a.spans * a.num_kv_heads)), dim3(64 * kWaves), 0, stream, a, a.block_table, a.k_scale, a.v_scale);
+    hipLaunchKernelGGL((chunk_kernel<D, FP8, LSE>), dim3((unsigned)(a.spans * a.num_kv_heads)), dim3(64 * kWaves), 0, stream, a, a.block_table, a.k_scale, a.v_scale);
     SS_HIP_CHECK(hipGetLastError(), "launch chunk_kernel");
     return chunk_merge_launch<ROWS, 32, D, SS_BF16>(a, stream);
 }
@@ -626,8 +644,12 @@ bool chunk_mfma_supported(int head_dim, int kv_dtype, int q_dtype)
 int32_t chunk_mfma_launch(const ChunkArgs &a, hipStream_t stream)
 {
     const bool fp8 = a.kv_dtype == SS_FP8_E4M3;
-    if (a.head_dim == 128) return fp8 ? launch<128, true>(a, stream) : launch<128, false>(a, stream);
-    return fp8 ? launch<64, true>(a, stream) : launch<64, false>(a, stream);
+    if (a.lse) {
+        if (a.head_dim == 128) return fp8 ? launch<128, true, true>(a, stream) : launch<128, false, true>(a, stream);
+        return fp8 ? launch<64, true, true>(a, stream) : launch<64, false, true>(a, stream);
+    }
+    if (a.head_dim == 128) return fp8 ? launch<128, true, false>(a, stream) : launch<128, false, false>(a, stream);
+    return fp8 ? launch<64, true, false>(a, stream) : launch<64, false, false>(a, stream);
 }
 
 }  // namespace ss

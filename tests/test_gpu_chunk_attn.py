@@ -236,3 +236,36 @@ def test_scales_far_from_one(q):
 @pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32")])
 def test_a_scale_of_scores_near_zero(q, kv):
     run(dict(ref.chunk_batch([(70, 300), (1, 40)], 8, 2, 64, kv, q, seed=14), sm_scale=1e-44))
+
+
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32")])
+@pytest.mark.parametrize("d", [64, 128])
+def test_without_lse(q, kv, d):
+    """A form of its own, with whole tiles, merged ones, and rows that see nothing."""
+    run(ref.chunk_batch([(200, 200), (64, 5000), (1, 1), (30, 10), (1, 700)], 8, 2, d, kv, q, seed=d + 1, spare_rows=2), lse=False)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+def test_rows_with_one_weight(kv):
+    """All weight on one key, far from the first ones: the output is its value, to the rounding of the output.
+
+    The sum that divides is that of the weights as rounded, so the weight's own rounding (up to 2^-8) is not in the result; what is left are the other
+    weights, below 2^-12 in all, and half a step of bf16.
+    """
+    n, d = 900, 128
+    inp = ref.chunk_batch([(40, n)], 4, 1, d, kv, seed=15)
+    blk, place = int(inp["block_table"][0, 500 // 16]), 500 % 16
+    direction = torch.randn(d, generator=torch.Generator().manual_seed(1)).sign()
+    key = (direction * 2.0).cuda()
+    k = inp["k_cache"].float()
+    k[:, 0] *= 0.125                                   # other scores: small
+    k[blk, 0, place] = key / (inp["k_scale"][blk, 0] if kv == "fp8" else 1.0)
+    inp["k_cache"] = k.clamp(-448.0, 448.0).to(inp["k_cache"].dtype)
+    inp["q"] = (direction.cuda() * torch.linspace(1.1, 1.4, 40 * 4, device="cuda").view(40, 4, 1)).to(torch.bfloat16)
+    out, _ = run(inp)
+    value = inp["v_cache"][blk, 0, place].float() * (inp["v_scale"][blk, 0] if kv == "fp8" else 1.0)
+    got = out.view(torch.bfloat16).float()
+    x = (inp["q"].float() * key).sum(-1) / d ** 0.5     # its score: 24 and more
+    assert float(x.min()) > 20.0
+    size = ref.chunk_reference(inp)[2].float().amax(-1, keepdim=True) + value.abs().max()
+    assert ((got - value).abs() <= value.abs() * 2.0 ** -8 + size * 2.0 ** -12 + n * torch.exp(-x.min() + 8.0) * 6.0).all()
