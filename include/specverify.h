@@ -409,9 +409,10 @@ int32_t ss_kv_write(const ss_paged_kv *kv, const int32_t *slot_map, const void *
  *              Rows from q_indptr[batch] on keep what they hold
  *   workspace  device, >= ss_chunk_attn_workspace(...) bytes, 256-byte aligned; contents are scratch.  It follows from the
  *              host-visible arguments and is largest for a few hundred rows against a wide table (up to 69 MB)
- * bf16 queries over bf16 or e4m3 caches take bf16 matrix instructions with fp32 scores, sums and outputs, the probabilities
- * rounded to bf16 for the product with the values; fp32 queries or caches are computed in fp32 throughout.  Up to 16 query
- * heads per KV head.  Batches with nothing but 1..21 new tokens per request are what ss_spec_verify_attn is for.
+ * bf16 queries over bf16 or e4m3 caches take bf16 matrix instructions with fp32 scores, sums and outputs: the probabilities are
+ * rounded to bf16 for the product with the values, and outputs divided by the sum of what they were rounded to (lse takes the sum of
+ * the probabilities themselves).  fp32 queries or caches are computed in fp32 throughout.  Up to 16 query heads per KV head.
+ * Batches with nothing but 1..21 new tokens per request are what ss_spec_verify_attn is for.
  */
 size_t ss_chunk_attn_workspace(const ss_paged_kv *kv, const ss_batch *batch, int32_t q_dtype, int32_t num_q_heads, int32_t total_rows);
 int32_t ss_chunk_attn(const ss_paged_kv *kv, const ss_batch *batch, const void *q, int64_t q_stride, int32_t q_dtype, int32_t num_q_heads,
