@@ -86,8 +86,6 @@ __device__ __forceinline__ void each(F &&f)
 }
 
 constexpr int kKeys = kChunkKeys;   // keys that are taken at a time, two cache blocks
-// What a tile costs beside its steps, in steps.
-constexpr int kOpen = 9;
 constexpr int kPairKeys = 2 * kKeys;
 constexpr int kInfinity = 0x7f800000;   // its bits, those of an exponent too
 
@@ -115,7 +113,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
     __shared__ int odd_flags[2][kWaves];
     const int g = blockIdx.x % a.num_kv_heads, span = blockIdx.x / a.num_kv_heads;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    ChunkWalk<ROWS, kKeys, kOpen> s;
+    ChunkWalk<ROWS, kKeys, kChunkOpen> s;
     int begun = 0, begun_q0 = 0, begun_rows = 0, begun_row0 = 0;   // of the tile that the span begins and does not end
     for (bool any = s.begin(a, span); any; any = s.next(a)) {
         if (s.part == 2 * span + 1) {

@@ -17,7 +17,7 @@ typedef float float2v __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kRows = kChunkRowsF32, kWaves = 4, kStepKeys = kChunkKeysF32, kOpen = 3;
+constexpr int kRows = kChunkRowsF32, kWaves = 4, kStepKeys = kChunkKeysF32;
 
 // four consecutive elements (from a multiple of four) as fp32
 template <int DT>
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
     __shared__ float vs[kStepKeys][PAD];
     const int g = blockIdx.x % a.num_kv_heads, span = blockIdx.x / a.num_kv_heads;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    ChunkWalk<kRows, kStepKeys, kOpen> s;
+    ChunkWalk<kRows, kStepKeys, kChunkOpenF32> s;
     int begun = 0, begun_q0 = 0, begun_rows = 0, begun_row0 = 0;
     for (bool any = s.begin(a, span); any; any = s.next(a)) {
         if (s.part == 2 * span + 1) {

@@ -124,13 +124,16 @@ struct ChunkWalk {
         ++t;
         return settle(a);
     }
-    // pieces of the current tile, which this span begins and does not end
+    // pieces of the current tile, which this span begins and does not end: one more than the cuts that fall into it, as locate() assigns them (a cut is
+    // the last tile's that begins at or in front of it, whatever is left of the tile's steps there: costs are interpolated, steps are not)
     __device__ __forceinline__ int pieces() const
     {
         const int lane = threadIdx.x & 63, n = u.steps(t);
+        const double behind = u.before(t + 1);
         int count = 1;
         for (int j = me + 1;; j += 64) {
-            const bool inside = j + lane < spans && u.cut(__builtin_floor(share * (j + lane)) - base, t, n) < n;
+            const double x = __builtin_floor(share * (j + lane)) - base;
+            const bool inside = j + lane < spans && x < behind && u.cut(x, t, n) < n;
             const uint64_t m = __ballot(inside);   // (the cuts ascend)
             count += __popcll(m);
             if (m != ~0ull) return uniform(count);

@@ -54,6 +54,7 @@ struct ChunkArgs {
 constexpr int kChunkRecInts = 4;
 constexpr int kChunkKeys = 32, kChunkKeysF32 = 64;   // keys of a step
 constexpr int kChunkRows = 256, kChunkRowsF32 = 64;   // query rows of a tile: bf16 matrix-core kernel, fp32 kernel
+constexpr int kChunkOpen = 9, kChunkOpenF32 = 3;      // what a tile costs beside its steps, in steps
 
 struct ChunkShape {               // host-visible sizes a launch and its workspace follow from
     int32_t rows;                 // query rows of a tile

@@ -269,3 +269,18 @@ def test_rows_with_one_weight(kv):
     assert float(x.min()) > 20.0
     size = ref.chunk_reference(inp)[2].float().amax(-1, keepdim=True) + value.abs().max()
     assert ((got - value).abs() <= value.abs() * 2.0 ** -8 + size * 2.0 ** -12 + n * torch.exp(-x.min() + 8.0) * 6.0).all()
+
+
+@pytest.mark.parametrize("lse", [True, False])
+@pytest.mark.parametrize("kv,d", [("bf16", 128), ("fp8", 128), ("bf16", 64), ("fp8", 64)])
+@pytest.mark.parametrize("lengths,hq,hkv", [([(389, 489)], 32, 8), ([(385, 485)], 32, 8), ([(519, 519)], 8, 8), ([(521, 521)], 8, 8), ([(259, 259)], 16, 8), ([(1031, 1031)], 8, 8),
+                                            ([(700, 1500), (300, 333), (513, 513)], 8, 4)])
+def test_last_tiles_that_are_not_full(lengths, hq, hkv, kv, d, lse):
+    """Requests of three tiles and more whose last one is short: what is merged is what was written (the workspace holds NaN before)."""
+    run(ref.chunk_batch(lengths, hq, hkv, d, kv, seed=hq, spare_rows=2), lse=lse)
+
+
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (4, 4), (4, 2), (5, 1), (14, 2), (16, 1)])
+def test_groupings_of_several_tiles(q, kv, hq, hkv):
+    run(ref.chunk_batch([(1100, 1500), (333, 800), (1, 90), (600, 600)], hq, hkv, 64, kv, q, seed=hq))
