@@ -110,7 +110,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
     constexpr int BLOCK_BYTES = kTile * D * (FP8 ? 1 : 2), LOADS = BLOCK_BYTES / (64 * 16);   // 16-byte loads of a lane for a cache block
     // Variables of their own: a tile's reads then do not wait for what is on its way into another one.
     __shared__ Tile<D> k_even, k_odd, v_even, v_odd;   // steps 3, 4, 7, 8, ..; 1, 2, 5, 6, ..; 0, 1, 4, 5, ..; 2, 3, 6, 7, .. (from the first)
-    __shared__ int odd_flags[2][kWaves];
+    __shared__ int odd_flags[2][kWaves];               // of two steps' values each: whether a wavefront's block of them had values that are not finite
     const int g = blockIdx.x % a.num_kv_heads, span = blockIdx.x / a.num_kv_heads;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     ChunkWalk<ROWS, kKeys, kChunkOpen> s;
@@ -496,7 +496,11 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
                 });
                 __builtin_amdgcn_sched_barrier(0);
             });
-            if (MASKED && t >= full) odd_seen |= odd_flags[pair][2 * ODD] | odd_flags[pair][2 * ODD + 1];
+            // (This step's flags and the next one's, which the same meeting has made known.  Behind the meeting in the next step the others may write them again.)
+            if (MASKED && !ODD) {
+                if (t >= full) odd_seen |= odd_flags[pair][0] | odd_flags[pair][1];
+                if (t + 1 >= full) odd_seen |= odd_flags[pair][2] | odd_flags[pair][3];
+            }
             float row_top[NB];
 #pragma unroll
             for (int e = 0; e < NB; ++e) row_top[e] = whole_row(top[e]);

@@ -284,3 +284,31 @@ def test_last_tiles_that_are_not_full(lengths, hq, hkv, kv, d, lse):
 @pytest.mark.parametrize("hq,hkv", [(1, 1), (4, 4), (4, 2), (5, 1), (14, 2), (16, 1)])
 def test_groupings_of_several_tiles(q, kv, hq, hkv):
     run(ref.chunk_batch([(1100, 1500), (333, 800), (1, 90), (600, 600)], hq, hkv, 64, kv, q, seed=hq))
+
+
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32"), ("f32", "fp8")])
+@pytest.mark.parametrize("hq,d,chunk,n", [(4, 128, 150, 200), (2, 128, 300, 700), (2, 64, 300, 700), (16, 128, 40, 333), (2, 128, 128, 128)])
+def test_values_that_are_not_finite(q, kv, hq, d, chunk, n):
+    """A value that is not finite reaches its column of the rows that see it, whichever step it is in, and nothing else changes by a bit.
+
+    Two KV heads; the last tiles leave wavefronts without rows.
+    """
+    inp = ref.chunk_batch([(chunk, n), (1, 40)], hq, 2, d, kv, q, seed=3)
+    G = hq // 2
+    want, zw = run(inp)
+    bits = lambda x: x.contiguous().view(torch.uint8)  # noqa: E731
+    _, _, ws = binding.alloc_chunk_outputs(inp)
+    for i, pos in enumerate(sorted({0, n - chunk, n - chunk // 2} | set(range(n - 1, max(n - 140, -1), -16)))):
+        blk, place = int(inp["block_table"][0, pos // 16]), pos % 16
+        odd = dict(inp, v_cache=inp["v_cache"].clone())
+        raw = odd["v_cache"].view(torch.uint8) if kv == "fp8" else odd["v_cache"]
+        raw[blk, 0, place, 5] = (0x7F, 0xFF)[i % 2] if kv == "fp8" else (float("inf"), float("nan"), -float("inf"))[i % 3]
+        got, zg, _ = binding.alloc_chunk_outputs(inp)
+        ws.fill_(0xFF)
+        binding.ss_chunk_attn(odd, got, zg, ws)
+        torch.cuda.synchronize()
+        row = max(pos - (n - chunk), 0)                  # the first one that sees it
+        hit = (got if q == "f32" else got.view(torch.bfloat16))[row:chunk, :G, 5]
+        assert not torch.isfinite(hit).any(), f"position {pos}: {int(torch.isfinite(hit).sum())} of {hit.numel()} rows do not have it"
+        got[row:chunk, :G, 5] = want[row:chunk, :G, 5]
+        assert torch.equal(bits(got), bits(want)) and torch.equal(zg, zw), f"position {pos}"
