@@ -41,12 +41,18 @@ static_assert(ROWS == kChunkRows, "what launches and workspaces are sized by");
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // How far (in powers of two) a row's scores may rise above the reference of its exponentials before the sums are rescaled.
 constexpr float kLag = 16.0f;
+// References beyond this (in powers of two) are taken care of apart: from 2^31 on the rounded reference and the scale's product with the largest score
+// may be further apart than an exponential's range.
+constexpr float kFar = 0x1p28f;
+constexpr int kOddValues = 1;   // values that are not finite were taken out
+constexpr int kFarRows = 2;     // a row's reference was beyond kFar
 
 __device__ __forceinline__ uint32_t pack_bf16(float x, float y)
 {
     const float2v v = {x, y};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
+__device__ __forceinline__ float bf16_value(const void *base, int64_t i) { return __uint_as_float((uint32_t) static_cast<const uint16_t *>(base)[i] << 16); }
 // x and the two of a pair of bf16, added
 __device__ __forceinline__ float pair_sum(uint32_t pair, float x)
 {
@@ -238,9 +244,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
                     tile.w[wave * kTile + t][(i * 64 + lane) % PIECES] = w[i];
                 }
             }
-            odd_flags[pair][wave] = __ballot(odd) != 0;
+            odd_flags[pair][wave] = __ballot(odd) ? kOddValues : 0;
         };
 
+        int special = 0;                  // what the steps leave for their end: kOddValues, kFarRows
         float m[NB], l[NB], l_used[NB];   // reference, sum of the weights, sum of the weights as rounded
         float16v o[NB][DB];
 #pragma unroll
@@ -343,14 +350,20 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
             if constexpr (FP8) return max_of_halves(__builtin_elementwise_maximum(top[0] * ks_next[0], top[1] * ks_next[1]));
             else return max_of_halves(__builtin_elementwise_maximum(top[0], top[1])) * c;
         };
+        auto element = [&](const void *cache, int64_t i) __attribute__((always_inline)) {
+            if constexpr (FP8) return __builtin_amdgcn_cvt_f32_fp8((int)static_cast<const uint8_t *>(cache)[i], 0);
+            else return bf16_value(cache, i);
+        };
         auto follow = [&](const float (&top)[NB]) __attribute__((always_inline)) {
             bool rise = false;
 #pragma unroll
             for (int e = 0; e < NB; ++e) rise = rise || top[e] > m[e] + kLag;
             if (__builtin_expect(__ballot(rise) != 0, 0)) {
+                bool beyond = false;
 #pragma unroll
                 for (int e = 0; e < NB; ++e) {
                     const float up = fmaxf(m[e], top[e]), down = __builtin_amdgcn_exp2f(m[e] - up);
+                    beyond = beyond || (up > m[e] && fabsf(up) > kFar && fabsf(up) < __builtin_inff());
                     m[e] = up;
                     l[e] *= down;
                     l_used[e] *= down;
@@ -359,6 +372,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
 #pragma unroll
                         for (int i = 0; i < 16; ++i) o[e][b][i] *= down;
                 }
+                if (__ballot(beyond)) special |= kFarRows;
             }
         };
         // Score j of the lane's 16 NB on its way to a weight: the exponents of the next one, its exponential, the sum and the rounding of those in front of it.
@@ -407,10 +421,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
                     for (int b = 0; b < DB; ++b)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const int64_t at = at0 + b * 32 + i / 4 * 8 + i % 4;
-                            float v;
-                            if constexpr (FP8) v = __builtin_amdgcn_cvt_f32_fp8((int)static_cast<const uint8_t *>(a.v)[at], 0);
-                            else v = __uint_as_float((uint32_t) static_cast<const uint16_t *>(a.v)[at] << 16);
+                            float v = element(a.v, at0 + b * 32 + i / 4 * 8 + i % 4);
                             if constexpr (FP8) v *= scale;
                             if (!__builtin_isfinite(v)) o[e][b][i] += v;
                         }
@@ -426,7 +437,6 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
         bf16x8 kf[KS];
         int kid = 0, vid = 0;   // this wavefront's blocks to bring next
         int k_put = 0, v_put = 0, v_put_next = 0;   // the scales of the blocks that are on their way
-        int odd_seen = 0;       // values that are not finite were taken out
         // the meeting of the wavefronts; dirty: values of theirs have to be cleaned in front of it
         auto meet = [&](bool dirty, int t, Tile<D> &v_new, int pair) __attribute__((always_inline)) {
             const int vstep = t + 1 + (wave >> 1);   // of the values that this wavefront has brought
@@ -498,8 +508,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
             });
             // (This step's flags and the next one's, which the same meeting has made known.  Behind the meeting in the next step the others may write them again.)
             if (MASKED && !ODD) {
-                if (t >= full) odd_seen |= odd_flags[pair][0] | odd_flags[pair][1];
-                if (t + 1 >= full) odd_seen |= odd_flags[pair][2] | odd_flags[pair][3];
+                if (t >= full) special |= odd_flags[pair][0] | odd_flags[pair][1];
+                if (t + 1 >= full) special |= odd_flags[pair][2] | odd_flags[pair][3];
             }
             float row_top[NB];
 #pragma unroll
@@ -579,7 +589,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
                 int t = first;
                 for (const int fast_end = min(full, end) - 5; t < fast_end; t += 4) four_steps(std::false_type{}, t, x, y);
                 for (; t < end; t += 4) four_steps(std::true_type{}, t, x, y);
-                if (__builtin_expect(odd_seen != 0, 0)) add_odd();
+                if (__builtin_expect((special & kOddValues) != 0, 0)) add_odd();
             } else {
                 team_barrier<false>();
                 bring(k_base, id_3, k_even, wave, in_k);
@@ -594,10 +604,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
             if constexpr (!FP8) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): nothing is on its way into LDS when the workgroup ends
         }
 
-#pragma unroll
-        for (int e = 0; e < NB; ++e) {
+        // A block of rows: the weighted values, the reference, the sums of the weights (as rounded, and themselves)
+        auto store = [&](int e, const float16v (&x)[DB], float ref, float used, float sum) __attribute__((always_inline)) {
             const int n = n_first + e * 32 + r32;
-            const float used = sum_of_halves(l_used[e]), sum = LSE ? sum_of_halves(l[e]) : used;
             if (s.part >= 0) {
                 const int64_t part = (int64_t)s.part * a.num_kv_heads + g;
                 const float level = used > 0.f ? sum / used : 1.0f;   // (the merge divides by the sum of the weights)
@@ -605,10 +614,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
 #pragma unroll
                 for (int b = 0; b < DB; ++b)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) po[(b * 4 + j) * 64] = float4v{o[e][b][4 * j], o[e][b][4 * j + 1], o[e][b][4 * j + 2], o[e][b][4 * j + 3]} * level;
+                    for (int j = 0; j < 4; ++j) po[(b * 4 + j) * 64] = float4v{x[b][4 * j], x[b][4 * j + 1], x[b][4 * j + 2], x[b][4 * j + 3]} * level;
                 if (half == 0) {
                     float *ml = a.part_ml + (part * ROWS + (wave * NB + e) * 32 + r32) * 2;
-                    ml[0] = m[e];
+                    ml[0] = ref;
                     ml[1] = sum;
                 }
             } else if (n < rows) {
@@ -618,9 +627,45 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
                 for (int b = 0; b < DB; ++b)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        chunk_store4<SS_BF16>(a.out, at * D + b * 32 + j * 8 + half * 4,
-                                              float4v{o[e][b][4 * j], o[e][b][4 * j + 1], o[e][b][4 * j + 2], o[e][b][4 * j + 3]} * r);
-                if (LSE && half == 0) a.lse[at] = sum == 0.f ? -__builtin_inff() : (m[e] + __builtin_amdgcn_logf(sum)) * kLn2;
+                        chunk_store4<SS_BF16>(a.out, at * D + b * 32 + j * 8 + half * 4, float4v{x[b][4 * j], x[b][4 * j + 1], x[b][4 * j + 2], x[b][4 * j + 3]} * r);
+                if (LSE && half == 0) a.lse[at] = sum == 0.f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+            }
+        };
+#pragma unroll
+        for (int e = 0; e < NB; ++e) {
+            const float used = sum_of_halves(l_used[e]);
+            store(e, o[e], m[e], used, LSE ? sum_of_halves(l[e]) : used);
+        }
+        // The wavefront's rows again, a key at a time in fp32, the scale applied before the reference is taken off: the largest score's weight is one whatever
+        // its size.  (By itself, so that the steps need no register for it; some 2 us a key.)
+        if (__builtin_expect((uniform(special) & kFarRows) != 0, 0)) {
+#pragma unroll 1
+            for (int e = 0; e < NB; ++e) {
+                const int n = min(n_first + e * 32 + r32, rows - 1), last = min(ctx + n / G, end * kKeys - 1);
+                const int64_t q_at = (int64_t)(s.u.q0 + n / G) * a.q_stride + (int64_t)(g * G + n % G) * D + half * (D / 2);
+                float ref = kChunkNoMax, sum = 0.f;
+                float16v x[DB] = {};
+#pragma unroll 1
+                for (int pos = first * kKeys; pos < min(end * kKeys, s.u.kv_len); ++pos) {
+#pragma clang fp contract(off)   // (a score is rounded before the reference, which is one of them, is taken off)
+                    const int64_t block = (int64_t)block_table[(int64_t)s.b * a.max_blocks + pos / kTile] * a.num_kv_heads + g, at = (block * kTile + pos % kTile) * D;
+                    float y = 0.f;
+#pragma unroll 4
+                    for (int i = 0; i < D / 2; ++i) y = __builtin_fmaf(element(a.k, at + half * (D / 2) + i), bf16_value(a.q, q_at + i), y);
+                    y = (FP8 ? sum_of_halves(y) * k_scale[block] : sum_of_halves(y)) * c;
+                    if (pos > last) continue;
+                    const float up = fmaxf(ref, y), down = __builtin_amdgcn_exp2f(ref - up), w = __builtin_amdgcn_exp2f(y - up);
+                    ref = up;
+                    sum = sum * down + w;
+#pragma unroll
+                    for (int b = 0; b < DB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float v = element(a.v, at + half * 4 + b * 32 + i / 4 * 8 + i % 4);
+                            x[b][i] = x[b][i] * down + w * (FP8 ? v * v_scale[block] : v);
+                        }
+                }
+                store(e, x, ref, sum, sum);
             }
         }
         team_barrier<false>();   // (the next tile's keys come to where the others may still read)

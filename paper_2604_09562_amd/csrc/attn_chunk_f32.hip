@@ -64,11 +64,12 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
             q[c] = float4v{0.f, 0.f, 0.f, 0.f};
             if (n < rows) q[c] = load4<QDT>(a.q, (int64_t)(s.u.q0 + qi) * a.q_stride + (int64_t)(g * G + hh) * D + 16 * c + 4 * jq);
         }
-        // scores are taken to powers of two; the factor in two parts, since fp32 holds it to 2^-24 of a score's size only
+        // Weights are powers of two of scores' differences to the largest, which is subtracted before the scale is applied: the largest score's weight is one
+        // whatever its size.  The factor in two parts, for the reference in powers of two (fp32 holds it to 2^-24 of a score's size only).
         const double c64 = (double)a.sm_scale * 1.4426950408889634;
         const float c_hi = (float)c64, c_lo = (float)(c64 - (double)c_hi);
         const int32_t *table = a.block_table + (int64_t)s.b * a.max_blocks;
-        float m = kChunkNoMax, l = 0.f;
+        float m = kChunkNoMax, l = 0.f;   // (m: in scores before the scale)
         float4v o[D / 16];
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) o[c] = float4v{0.f, 0.f, 0.f, 0.f};
@@ -113,13 +114,13 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (step * kStepKeys + tb * 16 + jq * 4 + i > lim) acc[i] = -__builtin_inff();
-                    top = fmaxf(top, acc[i] * c_hi);
+                    top = fmaxf(top, acc[i]);
                 }
                 x[tb] = acc;
             }
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float m_new = fmaxf(m, top), down = __builtin_amdgcn_exp2f(m - m_new);
+            const float m_new = fmaxf(m, top), down = __builtin_amdgcn_exp2f((m - m_new) * c_hi);
             m = m_new;
             l *= down;
 #pragma unroll
@@ -129,7 +130,7 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float y = x[tb][i];
-                    const float p = y == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(y, c_hi, __builtin_fmaf(y, c_lo, -m)));
+                    const float p = y == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((y - m) * c_hi);
                     x[tb][i] = p;
                     l += p;
                 }
@@ -157,15 +158,18 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
         }
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
+        // the reference in powers of two, and what its rounding leaves (of references so large that this is no factor, nothing: it is within the scores' own rounding)
+        const float ref = l == 0.f ? kChunkNoMax : fmaxf(m * c_hi, kChunkNoMax);
+        const float rest = fabsf(ref) < 0x1p20f ? __builtin_amdgcn_exp2f(__builtin_fmaf(m, c_hi, __builtin_fmaf(m, c_lo, -ref))) : 1.0f;
         if (s.part >= 0) {
             const int64_t part = (int64_t)s.part * a.num_kv_heads + g;
             float4v *po = reinterpret_cast<float4v *>(a.part_o) + part * (kRows * D / 4) + wave * (16 * D / 4) + lane;
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c) po[c * 64] = o[c];
+            for (int c = 0; c < D / 16; ++c) po[c * 64] = o[c] * rest;
             if (jq == 0) {
                 float *ml = a.part_ml + (part * kRows + wave * 16 + n16) * 2;
-                ml[0] = m;
-                ml[1] = l;
+                ml[0] = ref;
+                ml[1] = l * rest;
             }
             continue;
         }
@@ -173,7 +177,7 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
             const float r = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) chunk_store4<QDT>(a.out, at * D + 16 * c + 4 * jq, o[c] * r);
-            if (a.lse && jq == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+            if (a.lse && jq == 0) a.lse[at] = l == 0.f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(l * rest)) * 0.6931471805599453f;
         }
     }
     chunk_record(a, span, g, begun, begun_q0, begun_rows, begun_row0);

@@ -10,7 +10,7 @@
 
 namespace ss {
 
-constexpr float kChunkNoMax = -1.0e30f;   // reference of a row that has seen nothing
+constexpr float kChunkNoMax = -3.4028234663852886e38f;   // reference of a row that has seen nothing: no finite score lies below it
 
 typedef float chunk_float4 __attribute__((ext_vector_type(4)));
 

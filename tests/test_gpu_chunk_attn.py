@@ -312,3 +312,104 @@ def test_values_that_are_not_finite(q, kv, hq, d, chunk, n):
         assert not torch.isfinite(hit).any(), f"position {pos}: {int(torch.isfinite(hit).sum())} of {hit.numel()} rows do not have it"
         got[row:chunk, :G, 5] = want[row:chunk, :G, 5]
         assert torch.equal(bits(got), bits(want)) and torch.equal(zg, zw), f"position {pos}"
+
+
+@pytest.mark.parametrize("lse", [True, False])
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+@pytest.mark.parametrize("q,kv,d", [("bf16", "bf16", 128), ("bf16", "fp8", 128), ("bf16", "bf16", 64), ("bf16", "fp8", 64), ("f32", "f32", 128), ("f32", "bf16", 64), ("f32", "fp8", 64)])
+def test_scores_of_the_whole_fp32_range(q, kv, d, sign, lse):
+    """Scores of every second head from +-1e32 to +-2e37, products to 1.6e38: the largest takes all of the weight, whatever its sign.  The other heads' are ordinary.
+
+    One product to a score, no two the same: a score is off by three roundings at most (product, scale, factor of powers of two), the next one by 2^-7 of it or, in
+    e4m3 blocks, 2^-17 by their scales.  The weight of the largest is one and the others' zero, so the output is its value, rounded once if to bf16 (the sum
+    that divides is one), and the log-sum-exp the score, to the score's roundings and three more.
+    """
+    lengths = [(3, 3), (70, 200), (64, 1100), (1, 40), (300, 500)]
+    inp = ref.chunk_batch(lengths, 8, 2, d, kv, q, seed=3)
+    rng = np.random.default_rng(5)
+    shape = inp["k_cache"].shape
+    bits = lambda x: int(np.float32(x).view(np.uint32)) >> 16  # noqa: E731
+    if kv == "fp8":                                      # codes 2^-6 .. 448 of blocks whose scales all differ
+        codes = rng.integers(8, 127, shape[:3]).astype(np.uint8)
+        for row in codes.reshape(-1, 16):
+            row[:] = rng.choice(np.arange(8, 127), 16, replace=False)
+        steps = rng.permutation(shape[0] * shape[1]).reshape(shape[:2])
+        inp["k_scale"] = torch.from_numpy((sign * 10.0 ** (15.8 + 0.2 * (steps + rng.random(shape[:2]) * 0.5) / steps.size)).astype(np.float32)).cuda()
+        k = torch.zeros(shape, dtype=torch.uint8)
+        k[..., 5] = torch.from_numpy(codes)
+        inp["k_cache"] = k.cuda().view(torch.float8_e4m3fn)
+    else:                                                # every bf16 number at most once to a head
+        sizes = np.stack([rng.permutation(np.arange(bits(1e14), bits(1e19)))[:shape[0] * 16] for _ in range(shape[1])], 1)
+        sizes = (sizes.astype(np.uint32) << 16).view(np.float32).reshape(shape[0], 16, shape[1]).transpose(0, 2, 1)
+        k = torch.zeros(shape)
+        k[..., 5] = torch.from_numpy(sign * sizes.copy())
+        inp["k_cache"] = k.cuda().to(inp["k_cache"].dtype)
+    query = torch.zeros_like(inp["q"])
+    query[:, 0::2, 5] = 1.6e19
+    query[:, 1::2, 5] = 1.0e-17
+    inp["q"] = query
+    out, z, ws = binding.alloc_chunk_outputs(inp)
+    ws.fill_(0xFF)
+    binding.ss_chunk_attn(inp, out, z if lse else None, ws)
+    torch.cuda.synchronize()
+    got = (out if q == "f32" else out.view(torch.bfloat16)).double()
+    want, zw, size, mag = ref.chunk_reference(inp)
+    tol, ltol = ref.chunk_tolerances(inp, want, zw, size, mag)
+    assert ((got - want).abs() <= tol)[:, 1::2].all(), "ordinary heads"
+    assert not lse or ((z.double() - zw).abs() <= ltol)[:, 1::2].all()
+    row = 0
+    for b, (chunk, n) in enumerate(lengths):
+        ids = inp["block_table"][b, :ref.blocks(n)].long()
+        for h in range(2):
+            part = lambda c, sc: (c.view(torch.uint8)[:, h][ids].view(c.dtype) if kv == "fp8" else c[:, h][ids]).double() * (1.0 if sc is None else sc[ids, h].double()[:, None, None])  # noqa: E731
+            keys, values = part(inp["k_cache"], inp["k_scale"]).reshape(-1, d)[:n, 5], part(inp["v_cache"], inp["v_scale"]).reshape(-1, d)[:n]
+            for head in (4 * h, 4 * h + 2):
+                x = inp["q"][row:row + chunk, head, 5].double()[:, None] * keys * inp["sm_scale"]
+                last = torch.arange(chunk, device="cuda") + n - chunk
+                x = torch.where(torch.arange(n, device="cuda") <= last[:, None], x, -float("inf"))
+                top, at = x.topk(min(2, n), -1)
+                assert n == 1 or (top[:, 0] - top[:, 1] > top[:, 0].abs() * 2.0 ** -20)[last > 0].all()
+                o = got[row:row + chunk, head]
+                # (a scale of values in the chunk's bf16 form: its fraction goes through a logarithm and an exponential of about 2^-22 each)
+                bound = values[at[:, 0]].abs() * ((2.0 ** -8 if q == "bf16" else 0.0) + 2.0 ** -20) + 1e-30
+                assert ((o - values[at[:, 0]]).abs() <= bound).all(), f"request {b}, head {head}"
+                if lse:
+                    assert ((z[row:row + chunk, head].double() - top[:, 0]).abs() <= top[:, 0].abs() * 2.0 ** -21).all(), f"request {b}, head {head}"
+        row += chunk
+
+
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32")])
+def test_references_that_rise_from_far_below(q, kv):
+    """Scores of a row go from -1e33 at its first keys to ordinary ones, and from ordinary ones to 1e33: what came before has no weight left."""
+    n, d = 800, 128
+    for first, sign in ((400, -1.0), (400, 1.0)):
+        inp = ref.chunk_batch([(100, n)], 4, 1, d, kv, q, seed=8, sharp=1.0)
+        ids = inp["block_table"][0].long()
+        k = torch.zeros(inp["k_cache"].shape, dtype=torch.float32, device="cuda")
+        k[ids, 0] = torch.randn((ids.numel(), 16, d), device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+        big = (torch.arange(ids.numel() * 16, device="cuda") < first) if sign < 0 else (torch.arange(ids.numel() * 16, device="cuda") == first)
+        k[ids, 0, :, 7] = torch.where(big, sign * 1.0e15, 0.0).view(-1, 16)
+        if kv == "fp8":                                  # (a block's own scale is 1e13 where it holds what is large)
+            rows = ids[big.view(-1, 16).any(-1)]
+            inp["k_scale"].fill_(0.05)
+            inp["k_scale"][rows] = 1.0e13
+            k = (k / inp["k_scale"][..., None, None]).clamp(-448.0, 448.0)
+        inp["k_cache"] = k.to(inp["k_cache"].dtype)
+        query = inp["q"].clone()
+        query[..., 7] = 1.0e19
+        inp["q"] = query
+        out, z, ws = binding.alloc_chunk_outputs(inp)
+        ws.fill_(0xFF)
+        binding.ss_chunk_attn(inp, out, z, ws)
+        torch.cuda.synchronize()
+        got = (out if q == "f32" else out.view(torch.bfloat16)).double()
+        if sign < 0:                                     # the rows as if the first keys were not there
+            want, zw, size, mag = ref.chunk_reference(inp)
+            ordinary = dict(inp, q=query.clone())
+            ordinary["q"][..., 7] = 0.0                  # (the magnitudes of the scores that count)
+            tol, ltol = ref.chunk_tolerances(inp, want, zw, size, ref.chunk_reference(ordinary)[3])
+            assert ((got - want).abs() <= tol).all() and ((z.double() - zw).abs() <= ltol).all()
+        else:
+            blk, place = int(ids[first // 16]), first % 16
+            value = inp["v_cache"][blk, 0, place].double() * (inp["v_scale"][blk, 0].double() if kv == "fp8" else 1.0)
+            assert ((got - value).abs() <= value.abs() * ((2.0 ** -8 if q == "bf16" else 0.0) + 2.0 ** -20)).all()
