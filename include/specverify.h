@@ -376,7 +376,8 @@ typedef struct ss_block_pool {
  *   status      device int32 [1]: 0, or why nothing was done: s > 0: s blocks are missing; s < 0: request -1-s has impossible
  *               lengths (kv_len below its rows, rows outside [0, total_rows], more blocks than the table has columns), s = -1-batch:
  *               the free list's length has.  Then table, held and free list are as they were and every slot is -1, so that
- *               ss_kv_write writes nothing.
+ *               ss_kv_write writes nothing; ss_chunk_attn behind it stays inside its arrays, but what it puts out is of no use.  Calls
+ *               that follow the table without bounds (ss_kv_append, ss_spec_verify_attn) must not be made before status is known to be 0.
  *   workspace   device, >= ss_block_map_workspace(batch) bytes, 256-byte aligned; contents are scratch
  * One call at a time for one pool; a block belongs to one request only (shared prefixes are the caller's).
  */
@@ -402,7 +403,9 @@ int32_t ss_kv_write(const ss_paged_kv *kv, const int32_t *slot_map, const void *
  * Attention of a chunk of new tokens over the paged cache, in which their keys and values already are: the formulas of
  * ss_spec_verify_attn for chains, without its bound on the new tokens.  Row i of request b is at position
  * kv_len_b - q_len_b + i and attends positions 0 up to its own.  A row whose position is negative (kv_len below the
- * request's rows) attends nothing: zeros, and lse minus infinity.
+ * request's rows) attends nothing: zeros, and lse minus infinity.  A request whose rows lie outside [0, total_rows] or whose kv_len
+ * passes its row of the table is left out (its rows keep what they hold), and a block id outside the cache is read as its last
+ * block: nothing outside the arrays is read or written, whatever lengths and table hold.
  *   q          device, rows of [num_q_heads][head_dim] in q_dtype (SS_F32 or SS_BF16), q_stride elements apart (>= num_q_heads *
  *              head_dim); rows start 16-byte aligned
  *   out        device, dense [total_rows][num_q_heads][head_dim] in q_dtype; lse device float [total_rows][num_q_heads] or NULL.

@@ -193,7 +193,7 @@ int32_t ss_chunk_attn(const ss_paged_kv *kv, const ss_batch *batch, const void *
     ChunkArgs a{};
     a.k = kv->k; a.v = kv->v; a.k_scale = kv->k_scale; a.v_scale = kv->v_scale;
     a.num_kv_heads = kv->num_kv_heads; a.head_dim = kv->head_dim; a.kv_dtype = kv->dtype;
-    a.batch = batch->batch; a.max_blocks = batch->max_blocks_per_seq;
+    a.batch = batch->batch; a.max_blocks = batch->max_blocks_per_seq; a.num_blocks = kv->num_blocks; a.total_rows = total_rows;
     a.block_table = batch->block_table; a.kv_len = batch->kv_len; a.q_indptr = batch->q_indptr;
     a.q = q; a.q_stride = q_stride; a.out = out; a.lse = lse; a.q_dtype = q_dtype; a.num_q_heads = num_q_heads; a.sm_scale = sm_scale;
     chunk_carve(a, s, workspace);

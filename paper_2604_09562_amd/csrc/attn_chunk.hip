@@ -161,7 +161,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
         const scalar_ints k_scales = (scalar_ints)(uintptr_t)k_scale, v_scales = (scalar_ints)(uintptr_t)v_scale;
         const int last_block = (int)(((unsigned)s.u.kv_len + kTile - 1) / kTile) - 1;
         // block j of a step (the last block again where there is none: what stands there is masked)
-        auto block_id = [&](int step, int j) __attribute__((always_inline)) { return table[min(step * 2 + j, last_block)]; };
+        auto block_id = [&](int step, int j) __attribute__((always_inline)) { return chunk_block(a, table[min(step * 2 + j, last_block)]); };
         const uint32_t block_stride = (uint32_t)a.num_kv_heads * BLOCK_BYTES;
         const char *k_base = static_cast<const char *>(a.k) + (int64_t)g * BLOCK_BYTES, *v_base = static_cast<const char *>(a.v) + (int64_t)g * BLOCK_BYTES;
 
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
 #pragma unroll
             for (int e = 0; e < NB; ++e)
                 for (int pos = max(first, full) * kKeys; pos <= lim[e]; ++pos) {
-                    const int64_t block = (int64_t)block_table[(int64_t)s.b * a.max_blocks + pos / kTile] * a.num_kv_heads + g, at0 = (block * kTile + pos % kTile) * D + half * 4;
+                    const int64_t block = (int64_t)chunk_block(a, block_table[(int64_t)s.b * a.max_blocks + pos / kTile]) * a.num_kv_heads + g, at0 = (block * kTile + pos % kTile) * D + half * 4;
                     const float scale = FP8 ? v_scale[block] : 1.f;
 #pragma unroll
                     for (int b = 0; b < DB; ++b)
@@ -648,7 +648,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
 #pragma unroll 1
                 for (int pos = first * kKeys; pos < min(end * kKeys, s.u.kv_len); ++pos) {
 #pragma clang fp contract(off)   // (a score is rounded before the reference, which is one of them, is taken off)
-                    const int64_t block = (int64_t)block_table[(int64_t)s.b * a.max_blocks + pos / kTile] * a.num_kv_heads + g, at = (block * kTile + pos % kTile) * D;
+                    const int64_t block = (int64_t)chunk_block(a, block_table[(int64_t)s.b * a.max_blocks + pos / kTile]) * a.num_kv_heads + g, at = (block * kTile + pos % kTile) * D;
                     float y = 0.f;
 #pragma unroll 4
                     for (int i = 0; i < D / 2; ++i) y = __builtin_fmaf(element(a.k, at + half * (D / 2) + i), bf16_value(a.q, q_at + i), y);

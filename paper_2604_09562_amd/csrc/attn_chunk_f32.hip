@@ -86,7 +86,7 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
                 const int pos = step * kStepKeys + t;
                 float4v k = {0.f, 0.f, 0.f, 0.f}, v = k;
                 if (pos < s.u.kv_len) {   // what stands behind the last token is of no one
-                    const int64_t tile = (int64_t)table[pos / kTile] * a.num_kv_heads + g, from = (tile * kTile + pos % kTile) * D + d;
+                    const int64_t tile = (int64_t)chunk_block(a, table[pos / kTile]) * a.num_kv_heads + g, from = (tile * kTile + pos % kTile) * D + d;
                     k = load4<KV>(a.k, from);
                     v = load4<KV>(a.v, from);
                     if constexpr (KV == SS_FP8_E4M3) { k *= a.k_scale[tile]; v *= a.v_scale[tile]; }
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
                         o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vs[tb * 16 + jq * 4 + i][16 * c + n16], x[tb][i], o[c], 0, 0, 0);
             if (any_odd) {
                 for (int pos = step * kStepKeys; pos < min((step + 1) * kStepKeys, lim + 1); ++pos) {
-                    const int64_t tile = (int64_t)table[pos / kTile] * a.num_kv_heads + g, from = (tile * kTile + pos % kTile) * D + 4 * jq;
+                    const int64_t tile = (int64_t)chunk_block(a, table[pos / kTile]) * a.num_kv_heads + g, from = (tile * kTile + pos % kTile) * D + 4 * jq;
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) {
                         float4v v = load4<KV>(a.v, from + 16 * c);

@@ -46,13 +46,15 @@ struct ChunkUnit {                   // a request
         const int tok = min((int)(((uint32_t)(t + 1) * ROWS - 1) / (uint32_t)G), q_len - 1), seen = kv_len - q_len + tok + 1;
         return seen > 0 ? (int)(((unsigned)seen + KEYS - 1) / KEYS) : 0;
     }
-    __device__ __forceinline__ void set(int q0_, int q1, int len, int G_, int open_)
+    // A request.  One whose rows are outside of the call's or whose cache is longer than its row of the table has no tiles: nothing of it is read or written.
+    __device__ __forceinline__ void set(const ChunkArgs &a, int q0_, int q1, int len, int open_)
     {
         open = open_;
         q0 = q0_;
-        q_len = q1 - q0_;
-        kv_len = len;
-        G = G_;
+        const bool fits = q0_ >= 0 && q1 >= q0_ && q1 <= a.total_rows && len <= (a.num_blocks > 0 ? a.max_blocks * kTile : 0);
+        q_len = fits ? q1 - q0_ : 0;
+        kv_len = max(len, 0);
+        G = a.num_q_heads / a.num_kv_heads;
         tiles = q_len > 0 ? (int)(((uint32_t)q_len * (uint32_t)G + ROWS - 1) / ROWS) : 0;
         first = tiles ? steps(0) : 0;
         last = tiles ? steps(tiles - 1) : 0;
@@ -150,13 +152,13 @@ private:
         Unit r = {};
         r.G = G;
         r.open = open;
-        if (i < a.batch) r.set(a.q_indptr[i], a.q_indptr[i + 1], a.kv_len[i], G, open);
+        if (i < a.batch) r.set(a, a.q_indptr[i], a.q_indptr[i + 1], a.kv_len[i], open);
         return r;
     }
     __device__ __forceinline__ Unit request(const ChunkArgs &a, int i) const
     {
         Unit r;
-        r.set(uniform(a.q_indptr[i]), uniform(a.q_indptr[i + 1]), uniform(a.kv_len[i]), a.num_q_heads / a.num_kv_heads, open);
+        r.set(a, uniform(a.q_indptr[i]), uniform(a.q_indptr[i + 1]), uniform(a.kv_len[i]), open);
         return r;
     }
     // Moves on to the next tile that there is and sets the piece's end; false behind the span's end.

@@ -38,6 +38,7 @@ struct ChunkArgs {
     const float *k_scale, *v_scale;
     int32_t num_kv_heads, head_dim, kv_dtype;
     int32_t batch, max_blocks;
+    int32_t num_blocks, total_rows;   // bounds of what the table and q_indptr say
     const int32_t *block_table, *kv_len, *q_indptr;
     const void *q;
     int64_t q_stride;             // elements from one row to the next
@@ -51,6 +52,12 @@ struct ChunkArgs {
     int32_t *rec;                 // [spans][kChunkRecInts] the tile that a span begins and does not end
     float *part_ml, *part_o;      // [cap] partial results
 };
+// A block id of the table as it is followed: one that is no block's, as behind a block map that lacked blocks, as the last block's.
+__device__ __forceinline__ int chunk_block(const ChunkArgs &a, int id)
+{
+    const uint32_t last = (uint32_t)a.num_blocks - 1u;   // (requests with keys have a cache)
+    return (int)((uint32_t)id < last ? (uint32_t)id : last);
+}
 constexpr int kChunkRecInts = 4;
 constexpr int kChunkKeys = 32, kChunkKeysF32 = 64;   // keys of a step
 constexpr int kChunkRows = 256, kChunkRowsF32 = 64;   // query rows of a tile: bf16 matrix-core kernel, fp32 kernel

@@ -69,6 +69,8 @@ def run(steps: int = 6, batch: int = 8, layers: int = 4, tree: bool = False, voc
     def blocks(d, rows):
         slots = torch.empty(rows, dtype=torch.int32, device=dev)
         binding.ss_block_map(d, slots, None, status, ws_b)
+        if int(status):      # (known before anything follows the table)
+            raise RuntimeError(f"ss_block_map: status {int(status)}")
         return slots
 
     # ---- the prompts
@@ -93,8 +95,6 @@ def run(steps: int = 6, batch: int = 8, layers: int = 4, tree: bool = False, voc
         torch.cuda.synchronize()
         t_prompt += time.perf_counter() - t0
         chunks += 1
-        if int(status):
-            raise RuntimeError(f"ss_block_map: status {int(status)}")
     if verbose:
         print(f"{int(cur.sum())} prompt tokens in {chunks} chunks, {1e3 * t_prompt / max(chunks, 1):.3f} ms of device work per chunk ({layers} layers)")
 
@@ -141,8 +141,6 @@ def run(steps: int = 6, batch: int = 8, layers: int = 4, tree: bool = False, voc
         t_dev += time.perf_counter() - t0
 
         # ---- feedback: the controller turns each request's acceptance into its next depth
-        if int(status):
-            raise RuntimeError(f"ss_block_map: status {int(status)}")
         n = n_acc.cpu().numpy()
         cur = d["kv_len"].cpu().numpy()
         load, tput = 0.3, 300.0

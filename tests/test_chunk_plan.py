@@ -141,6 +141,8 @@ extern "C" const int32_t *plan(int f32, int batch, int max_blocks, int num_block
     args = ss::ChunkArgs{};
     args.batch = batch;
     args.max_blocks = max_blocks;
+    args.num_blocks = num_blocks;
+    args.total_rows = total_rows;
     args.num_q_heads = hq;
     args.num_kv_heads = hkv;
     args.spans = spans;
@@ -225,3 +227,28 @@ def test_random_batches(shim, f32, G):
             lengths.append((q, n))
         spans = int(rng.choice([1, 2, 7, 256 // hkv, 256 // hkv, 512 // hkv]))
         check(shim, f32, lengths, hkv * G, hkv, spans)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+def test_requests_whose_lengths_are_impossible_have_no_tiles(shim, f32):
+    """Rows outside the call's or a cache longer than the table's row: no piece.  The others are cut as if those had no new tokens."""
+    lengths = [(300, 700), (64, 64), (200, 900), (5, 90)]
+    spans, big = 32, 2 ** 31 - 1
+    for change in (lambda q, n: n.__setitem__(1, 16 * 57 + 1), lambda q, n: n.__setitem__(1, big), lambda q, n: q.__setitem__(slice(1, 3), [300, 299]),
+                   lambda q, n: q.__setitem__(slice(1, 3), [-5, -2]), lambda q, n: q.__setitem__(slice(1, 3), [-big - 1, 5]),
+                   lambda q, n: q.__setitem__(slice(1, 3), [5, -big]), lambda q, n: q.__setitem__(slice(2, 5), [570, 571, big])):
+        indptr, kv = [0, 300, 364, 564, 569], [n for _, n in lengths]
+        change(indptr, kv)
+        got = walked(shim, f32, [(0, n) for n in kv], 8, 2, spans, q_indptr=indptr, max_blocks=57, total_rows=569)
+        fits = [0 <= a <= b <= 569 and n <= 57 * 16 for a, b, n in zip(indptr, indptr[1:], kv)]
+        assert not all(fits) and {b for _, b, *_ in got} <= {b for b in range(4) if fits[b] and indptr[b + 1] > indptr[b]}
+        steps = {}
+        for _, b, t, s0, s1, _, _ in got:
+            steps[b, t] = steps.get((b, t), 0) + s1 - s0
+        for (b, t), n in steps.items():
+            rows, keys = (64, 64) if f32 else (256, 32)
+            chunk = indptr[b + 1] - indptr[b]
+            last = min(((t + 1) * rows - 1) // 4, chunk - 1)
+            assert n == -(-(kv[b] - chunk + last + 1) // keys)
+    assert walked(shim, f32, lengths, 8, 2, spans, num_blocks=0) == []           # no cache, no keys
+    assert [p[3:6] for p in walked(shim, f32, [(3, -5), (2, -big - 1)], 8, 2, 1)] == [(0, 0, -1)] * 2   # (rows in front of the cache: nothing to see)

@@ -413,3 +413,57 @@ def test_references_that_rise_from_far_below(q, kv):
             blk, place = int(ids[first // 16]), first % 16
             value = inp["v_cache"][blk, 0, place].double() * (inp["v_scale"][blk, 0].double() if kv == "fp8" else 1.0)
             assert ((got - value).abs() <= value.abs() * ((2.0 ** -8 if q == "bf16" else 0.0) + 2.0 ** -20)).all()
+
+
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32"), ("f32", "fp8")])
+def test_requests_with_impossible_lengths_or_blocks(q, kv):
+    """They are left out or read what is in the cache; nothing outside the arrays is touched, and the other requests' rows are what they were."""
+    lengths = [(90, 333), (130, 400), (5, 900), (200, 200)]
+    inp = ref.chunk_batch(lengths, 8, 2, 128, kv, q, seed=4, spare_rows=7)
+    want, zw = run(inp)
+    starts = inp["q_indptr"].tolist()
+    big = 2 ** 31 - 1
+
+    def call(**change):
+        d = dict(inp, **{k: inp[k].clone() for k in ("kv_len", "q_indptr", "block_table")})
+        for name, (at, value) in change.items():
+            d[name][at] = torch.tensor(value, dtype=torch.int32, device="cuda")
+        out, z, ws = binding.alloc_chunk_outputs(d)
+        out.view(torch.uint8).fill_(0x5A)
+        z.fill_(123.0)
+        ws.fill_(0xFF)
+        binding.ss_chunk_attn(d, out, z, ws)
+        torch.cuda.synchronize()
+        return out, z
+
+    bits = lambda x: x.contiguous().view(torch.uint8)  # noqa: E731
+
+    def same(got, requests):
+        for b in requests:
+            rows = slice(starts[b], starts[b + 1])
+            ref.check_chunk(dict(inp, batch=1, block_table=inp["block_table"][b:b + 1], kv_len=inp["kv_len"][b:b + 1], q=inp["q"][rows],
+                                 q_indptr=torch.tensor([0, lengths[b][0]], dtype=torch.int32, device="cuda"), total_rows=lengths[b][0]), got[0][rows], got[1][rows])
+
+    for ids in (-1, big, -big - 1, inp["num_blocks"]):                      # (as many steps as before: the same cuts, the same bits)
+        got = call(block_table=((1, slice(3, None)), ids))
+        for b in (0, 2, 3):
+            rows = slice(starts[b], starts[b + 1])
+            assert torch.equal(bits(got[0][rows]), bits(want[rows])) and torch.equal(got[1][rows], zw[rows])
+        assert (got[0].view(torch.uint8)[starts[-1]:] == 0x5A).all() and (got[1][starts[-1]:] == 123.0).all()
+    for n in (inp["max_blocks_per_seq"] * 16 + 1, big):                     # a request that is left out
+        got = call(kv_len=(1, n))
+        same(got, (0, 2, 3))
+        left = slice(starts[1], starts[2])
+        assert (got[0].view(torch.uint8)[left] == 0x5A).all() and (got[1][left] == 123.0).all()
+    for end in (inp["total_rows"] + 1, big, starts[3] - 1, -3):             # the last one's rows end outside the call's, or in front of where they begin
+        got = call(q_indptr=(4, end))
+        same(got, (0, 1, 2))
+        assert (got[0].view(torch.uint8)[starts[3]:] == 0x5A).all() and (got[1][starts[3]:] == 123.0).all()
+    got = call(kv_len=(1, -big - 1))
+    same(got, (0, 2, 3))
+    assert (bits(got[0][starts[1]:starts[2]]) == 0).all() and torch.isinf(got[1][starts[1]:starts[2]]).all()
+    out, z, ws = binding.alloc_chunk_outputs(inp)
+    out.view(torch.uint8).fill_(0x5A)
+    binding.ss_chunk_attn(dict(inp, num_blocks=0), out, z, ws)              # no block at all
+    torch.cuda.synchronize()
+    assert (out.view(torch.uint8) == 0x5A).all()

@@ -259,3 +259,42 @@ def test_two_workers_at_once():
     torch.cuda.synchronize()
     for lane, w in zip(lanes, work):
         lane.check(*w, "two at once")
+
+
+@pytest.mark.parametrize("kv,q", [("bf16", "bf16"), ("fp8", "bf16"), ("f32", "f32")])
+def test_the_whole_of_a_step_that_lacks_blocks(kv, q):
+    """All three calls are enqueued before anyone knows the status: the cache stays as it was, and the step is made again."""
+    lane = Lane(2, 10, 33, 1, 4, 2, 64, kv, q, seed=1)
+    lane.table.fill_(-7)
+    lane.mirror["table"][:] = -7
+    steps = [[(100, 100), (40, 40)], [(300, 400), (1, 41)], [(20, 120), (1, 41)]]     # 7 + 3 blocks; 25 + 3; 8 + 3: one is missing; then a request leaves
+    for i, lengths in enumerate(steps + [[(20, 120), (0, 0)]]):
+        b, wide, slot_map, positions = lane.batch_of(lengths)
+        outs = [binding.alloc_chunk_outputs(lane.layer(b, wide, 0))]
+        before = [t.clone() for t in lane.caches[0] if t is not None] + [lane.table.clone(), lane.held.clone()]
+        lane.enqueue(b, wide, slot_map, positions, outs)
+        torch.cuda.synchronize()
+        if i in (1, 2):
+            assert int(lane.status) == (18, 1)[i - 1] and (slot_map == -1).all()
+            after = [t for t in lane.caches[0] if t is not None] + [lane.table, lane.held]
+            assert all(torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8)) for x, y in zip(before, after))
+            continue
+        lane.check(b, wide, slot_map, positions, outs, str(lengths))
+
+
+def test_the_example_stops_where_blocks_are_missing(monkeypatch):
+    """Nothing that follows the table is enqueued behind a block map that has not been made."""
+    real, calls, steps = binding.ss_block_map, [], [0]
+
+    def lacking(d, slots, positions, status, ws):
+        real(d, slots, positions, status, ws)
+        steps[0] += 1
+        if steps[0] == 2:                                # (the prompts in one chunk, then the first decode step)
+            status.fill_(4)
+
+    monkeypatch.setattr(binding, "ss_block_map", lacking)
+    for name in ("ss_kv_append", "ss_spec_verify_attn"):
+        monkeypatch.setattr(binding, name, lambda *a, **k: calls.append(1))
+    with pytest.raises(RuntimeError, match="status 4"):
+        example.run(steps=2, batch=4, layers=1, vocab=4096, seed=1, verbose=False, chunk=4000)
+    assert steps[0] == 2 and not calls
