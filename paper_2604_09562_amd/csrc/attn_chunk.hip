@@ -160,8 +160,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
         const scalar_ints table = (scalar_ints)(uintptr_t)(block_table + (int64_t)s.b * a.max_blocks);
         const scalar_ints k_scales = (scalar_ints)(uintptr_t)k_scale, v_scales = (scalar_ints)(uintptr_t)v_scale;
         const int last_block = (int)(((unsigned)s.u.kv_len + kTile - 1) / kTile) - 1;
-        // block j of a step (the last block again where there is none: what stands there is masked)
-        auto block_id = [&](int step, int j) __attribute__((always_inline)) { return chunk_block(a, table[min(step * 2 + j, last_block)]); };
+        // block j of a step (the last block again where there is none: what stands there is masked).  Bounded where it is followed, not here, where that would wait for it.
+        auto block_id = [&](int step, int j) __attribute__((always_inline)) { return table[min(step * 2 + j, last_block)]; };
         const uint32_t block_stride = (uint32_t)a.num_kv_heads * BLOCK_BYTES;
         const char *k_base = static_cast<const char *>(a.k) + (int64_t)g * BLOCK_BYTES, *v_base = static_cast<const char *>(a.v) + (int64_t)g * BLOCK_BYTES;
 
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
         u32x4 in_k[FP8 ? LOADS : 1], in_v[FP8 ? LOADS : 1];
         // (a descriptor of its own for each block, so that a lane's place in it is all that the vector unit has to keep)
         auto block_at = [&](const char *cache, int id) __attribute__((always_inline)) {
-            return cache + (uint64_t)(uint32_t)id * block_stride;
+            return cache + (uint64_t)(uint32_t)chunk_block(a, id) * block_stride;
         };
         auto bring_part = [&](const char *at, int i, Tile<D> &tile, int quarter, u32x4 (&in)[FP8 ? LOADS : 1]) __attribute__((always_inline)) {
             const __amdgpu_buffer_rsrc_t block = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, BLOCK_BYTES, 0x00020000);
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
         float vl[2] = {}, vl_next[2] = {}, vr[2] = {}, vr_next[2] = {};   // the scale of values: its logarithm, its inverse
         int k_raw[2] = {}, v_raw[2] = {};                                // and, as bits, those of the step behind it
         int sid[2] = {0, 0};                                             // and the blocks of the one behind that
-        auto scale_of = [&](scalar_ints scales, int id) __attribute__((always_inline)) { return scales[(int64_t)id * a.num_kv_heads + g]; };
+        auto scale_of = [&](scalar_ints scales, int id) __attribute__((always_inline)) { return scales[(uint32_t)chunk_block(a, id) * (uint32_t)a.num_kv_heads + (uint32_t)g]; };
         auto fraction = [&](int scale) __attribute__((always_inline)) { return __int_as_float((scale & 0x7fffff) | 0x3f800000); };
         auto ask_scales = [&]() __attribute__((always_inline)) {
             if constexpr (FP8)
