@@ -150,8 +150,10 @@ __global__ __launch_bounds__(256) void kv_write_e4m3_kernel(KvWriteArgs a, int w
         begins &= begins - 1;
         const int first = __builtin_amdgcn_readlane(slot, p);
         const int place = first % kTile, row0 = r0 - BACK + p;
-        // bit j: the row j behind the first one is the run's (at most 16; rows that are left out may stand between)
-        const uint32_t run = (uint32_t)(__ballot(slot >= 0 && slot / kTile == first / kTile && slot - first == lane - p) >> p);
+        // bit j: the row j behind the first one is the run's (at most 16; rows that are left out or another block's may stand between)
+        const uint64_t rows = __ballot(slot >= 0 && slot / kTile == first / kTile && slot - first == lane - p);
+        if (rows & ((1ull << p) - 1)) continue;   // (the run began in front of this row, with another block's row between)
+        const uint32_t run = (uint32_t)(rows >> p);
         const int64_t tile = (int64_t)(first / kTile) * a.num_kv_heads + h;
         Eight<NEW_DT> x[N];
         float top = 0.f;

@@ -191,3 +191,31 @@ def test_e4m3_codes_at_and_beside_ties(new):
     c.update(num_blocks=total, k_cache=k, v_cache=v, k_scale=ks, v_scale=vs, wide=torch.cat(wide).to(ref.TORCH[new]), total_rows=len(slots),
              slots=torch.tensor(slots, dtype=torch.int32))
     run(c)
+
+
+@pytest.mark.parametrize("hkv,groups", [(2, 30), (8, 30), (8, 120), (8, 300)])
+@pytest.mark.parametrize("new", ["f32", "bf16"])
+def test_blocks_whose_rows_stand_between_each_other(new, hkv, groups):
+    """e4m3: rows of two or three blocks in turn or at random, each block's as far apart as their slots; all of a block's rows make its scale (windows of 1, 4 and 16 rows)."""
+    rng = np.random.default_rng(groups)
+    total = groups * 3 + 2
+    blocks, slots = rng.permutation(total), []
+    for g in range(groups):
+        mine, begins = blocks[3 * g:3 * g + 3], [0, int(rng.integers(0, 4)), int(rng.integers(0, 16))]
+        if g % 4 == 0:
+            begins[0] = -int(rng.integers(1, 8))         # a block that the call goes on
+        for r in range(16):
+            at = [i for i in range(2 + g % 2) if 0 <= r - begins[i] < 16]
+            i = at[r % len(at)] if g % 3 == 0 else int(rng.choice(at))
+            slots.append(int(mine[i]) * 16 + r - begins[i])
+    gen = torch.Generator().manual_seed(groups)
+    k, ks = ref.cache_values((total, hkv, 16, 64), "fp8", gen, "cpu")
+    v, vs = ref.cache_values((total, hkv, 16, 64), "fp8", gen, "cpu")
+    c = dict(num_kv_heads=hkv, head_dim=64, block_size=16, num_blocks=total, kv_dtype="fp8", k_cache=k, v_cache=v, k_scale=ks, v_scale=vs,
+             wide=torch.randn((len(slots), 2 * hkv * 64), generator=gen).to(ref.TORCH[new]), new_dtype=new, total_rows=len(slots), slots=torch.tensor(slots, dtype=torch.int32))
+    run(c)
+    binding.ss_set_option("validate", 1)
+    try:
+        run(c)
+    finally:
+        binding.ss_set_option("validate", 0)
