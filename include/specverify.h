@@ -299,7 +299,8 @@ int32_t ss_spec_accept_tree_sample(int32_t batch, int32_t vocab, int64_t row_str
  * byte = nearest e4m3fn (ties to even) of clamp(x / scale, +-448) with x / scale one float32
  * division.  A block whose slot 0 is written by this call gets scale = amax / 448 (1.0 if amax is 0)
  * over this call's values for that block and KV head, keys and values separately; a block that already
- * holds older tokens keeps its scale.  NaN inputs give unspecified NaN payloads.
+ * holds older tokens keeps its scale.  NaN inputs give unspecified NaN payloads in SS_F32 and SS_BF16 caches and finite codes in
+ * SS_FP8_E4M3 ones (ss_kv_write keeps them).
  * The caller owns all buffers; nothing is allocated; the kernel is enqueued on `stream`.
  * Errors: SS_ERR_INVALID_ARG (NULL pointers, bad dtypes or sizes), SS_ERR_DEVICE (launch failure).
  * Device-side contents (block ids in range, kv_len >= q_len, q_len <= SS_OUT_WIDTH) are the caller's contract.
@@ -389,7 +390,9 @@ int32_t ss_block_map(const ss_batch *batch, const ss_block_pool *pool, int32_t *
  * The write of new keys and values by slot: row r goes to place slot_map[r] % 16 of block slot_map[r] / 16, for every KV head.
  * Rows whose slot is negative or outside the cache are left out.  Values are stored as by ss_kv_append: SS_F32 the value, SS_BF16
  * nearest, ties to even, SS_FP8_E4M3 nearest e4m3fn of clamp(x / scale, +-448), the scale of a block whose place 0 is written by the
- * call being amax / 448 (1.0 if amax is 0) over what the call brings for that block and head; other blocks keep theirs.
+ * call being amax / 448 (1.0 if amax is 0) over what the call brings for that block and head; other blocks keep theirs.  NaN is
+ * stored as NaN and left out of amax; an infinity makes the scale of a block that it begins with infinite (all of that block and head
+ * then reads as NaN) and is cut at 448 in a block whose scale stands.
  *   kv              the cache; k, v, k_scale and v_scale are WRITTEN through although the struct declares them const
  *   slot_map        device int32 [total_rows], no slot twice.  For SS_FP8_E4M3 the rows of one block must stand as far apart in the
  *                   call as their slots, as ss_block_map gives them (rows that are left out may stand between)

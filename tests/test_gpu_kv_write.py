@@ -219,3 +219,63 @@ def test_blocks_whose_rows_stand_between_each_other(new, hkv, groups):
         run(c)
     finally:
         binding.ss_set_option("validate", 0)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", ["f32", "bf16"])
+@pytest.mark.parametrize("kv", ["f32", "bf16", "fp8"])
+def test_values_that_are_not_finite(kv, new, d):
+    """NaN is stored as NaN and is no part of a scale; an infinity is cut at 448 where a scale stands, and makes a new block's scale infinite; the rest is unchanged."""
+    hkv, nan, inf = 2, float("nan"), float("inf")
+    c = batch([(16, 16), (16, 16), (10, 26), (16, 16), (10, 26), (3, 9), (10, 30), (10, 30)], hkv, d, kv, new, seed=8)
+    if kv == "fp8":                                      # scales that stand, of each form of the quotient
+        blk = [int(c["slots"][r]) // 16 for r in (71, 81, 68)]
+        for scale in (c["k_scale"], c["v_scale"]):
+            scale[blk[0]], scale[blk[1]], scale[blk[2]] = 0.02, 1.0e-30, 0.0
+    x = c["wide"].view(-1, 2, hkv, d)                    # [rows][key or value][head][d]
+    x[58:68] *= 1.0e-29
+    x[81:] *= 1.0e-29
+    x[68:71, :, 0, :8] = 0.0                               # a scale of zero, as of values that are next to nothing
+    odd = torch.zeros(x.shape, dtype=torch.bool)
+    odd[3, :, 0, 5] = odd[9, 0, 1, 0] = odd[35, :, 1, d - 1] = odd[60, :, 0, 7] = True       # NaN in blocks that begin,
+    odd[75, :, 1, 4] = odd[85, 0, 0, 6] = odd[69, 1, 1, 1] = True                            # in blocks whose scales stand
+    odd[10:26, 1, 0] = True                              # all of a row and more
+    clean = dict(c, wide=torch.where(odd.view(c["wide"].shape), torch.zeros(()), c["wide"]))
+    x[odd] = nan
+    infinite = torch.zeros(x.shape)
+    infinite[34, :, 0, 3], infinite[61, 0, 1, 9], infinite[44, 1, 0, 2] = inf, -inf, -inf     # the same
+    infinite[72, :, 0, 3], infinite[83, 0, 1, 9], infinite[86, 1, 1, 1] = inf, -inf, inf
+    x[infinite != 0] = infinite[infinite != 0].to(x.dtype)
+    clean["wide"] = torch.where(torch.isinf(infinite).view(c["wide"].shape), torch.zeros(()), clean["wide"])
+    want = plain(clean)                                  # what the other values give (a zero changes no amax)
+    dev = {k: (v.cuda() if isinstance(v, torch.Tensor) else v) for k, v in c.items()}
+    dev["k_new"], dev["v_new"] = dev["wide"][:, :hkv * d].unflatten(1, (hkv, d)), dev["wide"][:, hkv * d:].unflatten(1, (hkv, d))
+    binding.ss_kv_write(dev, dev["slots"])
+    torch.cuda.synchronize()
+    slots = c["slots"].long()
+    for side, name in enumerate(("k", "v")):
+        got, scale = dev[name + "_cache"].cpu(), dev[name + "_scale"]
+        rows = got.view(torch.uint8)[slots // 16, :, slots % 16].view(got.dtype).float() if kv == "fp8" else got[slots // 16, :, slots % 16].float()
+        assert torch.isnan(rows[odd[:, side]]).all()
+        skip = odd[:, side].clone()
+        for r, h, e in infinite[:, side].nonzero().tolist():
+            skip[r, h, e] = True
+            if kv != "fp8":
+                assert rows[r, h, e] == infinite[r, side, h, e]
+            elif (slots == slots[r] // 16 * 16).any():   # (a block that begins: one with it has an infinite scale: codes of zero and NaN, which all read as NaN)
+                here = (slots // 16 == slots[r] // 16).nonzero()[:, 0]
+                assert torch.isinf(scale.cpu()[slots[r] // 16, h]) and torch.isnan(rows[here, h] * scale.cpu()[slots[r] // 16, h]).all()
+                skip[here, h] = True
+                want[2 * side + 1][slots[r] // 16, h] = inf
+            else:
+                assert rows[r, h, e] == (448.0 if infinite[r, side, h, e] > 0 else -448.0)
+        ideal = want[2 * side]
+        ideal = ideal.view(torch.uint8)[slots // 16, :, slots % 16].view(ideal.dtype).float() if kv == "fp8" else ideal[slots // 16, :, slots % 16].float()
+        ideal[68:71, 0, :8] = 0.0
+        assert torch.equal(rows[~skip], ideal[~skip])
+        if kv == "fp8":
+            assert torch.equal(scale.cpu(), want[2 * side + 1])
+        untouched = torch.ones(got.shape[0], 16, dtype=torch.bool)
+        untouched[slots // 16, slots % 16] = False
+        pick = lambda t: (t.view(torch.uint8) if kv == "fp8" else t).transpose(1, 2)[untouched]  # noqa: E731
+        assert torch.equal(pick(got), pick(c[name + "_cache"]))
