@@ -281,37 +281,87 @@ def alloc_attention_outputs(d: Dict[str, object], device="cuda:0", max_q_len: in
 # --------------------------------------------------------------------------------------------
 # filling the cache
 # --------------------------------------------------------------------------------------------
+# What stands behind an address is looked at first: a 64-bit slot map (torch's own kind of index) would be read as pairs, and these calls write where it says.
+# What a call gets of its own is checked at each call, the batch that it gets it for where outputs and workspaces are allocated (all of it at each call
+# would be 2 of 10 us).
+_INT32 = torch.int32
+_SIZE = {"f32": 4, "bf16": 2, "fp8": 1}
+
+
+def _ints(name: str, t: torch.Tensor, n: int) -> int:
+    """The address of a dense int32 tensor on the GPU of at least n elements."""
+    if t.dtype is not _INT32 or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
+        raise SpecVerifyError(f"{name} must be a dense int32 tensor of at least {n} elements on the GPU, got {t.dtype}, shape {tuple(t.shape)}, strides {t.stride()} "
+                              f"on {t.device}")
+    return t.data_ptr()
+
+
+def _dense(name: str, t: torch.Tensor, size: int, n: int) -> int:
+    """The address of a dense tensor on the GPU of at least n elements of `size` bytes, whatever type holds them."""
+    if t.element_size() != size or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
+        raise SpecVerifyError(f"{name} must be a dense tensor of at least {n} elements of {size} bytes on the GPU, got {t.dtype}, shape {tuple(t.shape)}, "
+                              f"strides {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
+def _rows(name: str, t: torch.Tensor, dtype: str, rows: int, heads: int, head_dim: int):
+    """Address and stride of rows that may be apart."""
+    stride = _row_stride(t, rows, heads, head_dim)
+    if t.element_size() != _SIZE[dtype] or not t.is_cuda:
+        raise SpecVerifyError(f"{name} must be of type {dtype} (or its bits) on the GPU, got {t.dtype} on {t.device}")
+    return t.data_ptr(), stride
+
+
 def _row_stride(t: torch.Tensor, rows: int, heads: int, head_dim: int) -> int:
     """Elements from one row of [rows][heads][head_dim] to the next; a row's own values have to be side by side."""
-    if t.dim() != 3 or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != head_dim:
-        raise SpecVerifyError(f"expected {rows} rows of [{heads}][{head_dim}], got a tensor of shape {tuple(t.shape)}")
+    shape = t.shape
+    if len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != head_dim:
+        raise SpecVerifyError(f"expected {rows} rows of [{heads}][{head_dim}], got a tensor of shape {tuple(shape)}")
     r, h, e = t.stride()
     if (e != 1 and head_dim > 1) or (h != head_dim and heads > 1):
         raise SpecVerifyError("the values of a row must be side by side (only the rows themselves may be apart)")
-    return r if t.shape[0] > 1 else heads * head_dim
+    return r if shape[0] > 1 else heads * head_dim
 
 
 def _cache_descriptor(d: Dict[str, object]) -> ss_paged_kv:
-    return ss_paged_kv(d["num_blocks"], d["block_size"], d["num_kv_heads"], d["head_dim"], _DT[d["kv_dtype"]], _ptr(d["k_cache"]),
-                       _ptr(d["v_cache"]), _ptr(d["k_scale"]), _ptr(d["v_scale"]))
+    return ss_paged_kv(d["num_blocks"], d["block_size"], d["num_kv_heads"], d["head_dim"], _DT[d["kv_dtype"]], d["k_cache"].data_ptr(),
+                       d["v_cache"].data_ptr(), _ptr(d["k_scale"]), _ptr(d["v_scale"]))
 
 
 def _batch_descriptor(d: Dict[str, object], max_q_len: int = 0) -> ss_batch:
-    return ss_batch(d["batch"], d["max_blocks_per_seq"], max_q_len, 0, _ptr(d["block_table"]), _ptr(d["kv_len"]), _ptr(d["q_indptr"]),
+    return ss_batch(d["batch"], d["max_blocks_per_seq"], max_q_len, 0, d["block_table"].data_ptr(), d["kv_len"].data_ptr(), d["q_indptr"].data_ptr(),
                     _ptr(d.get("tree_mask")))
+
+
+def _check_cache(d: Dict[str, object]) -> None:
+    heads = d["num_blocks"] * d["num_kv_heads"]
+    for name in ("k", "v"):
+        _dense(name + "_cache", d[name + "_cache"], _SIZE[d["kv_dtype"]], heads * d["block_size"] * d["head_dim"])
+        if d[name + "_scale"] is not None:
+            _dense(name + "_scale", d[name + "_scale"], 4, heads)
+
+
+def _check_batch(d: Dict[str, object]) -> None:
+    _ints("block_table", d["block_table"], d["batch"] * d["max_blocks_per_seq"])
+    _ints("kv_len", d["kv_len"], d["batch"])
+    _ints("q_indptr", d["q_indptr"], d["batch"] + 1 if d["batch"] else 0)
 
 
 def ss_block_map(d: Dict[str, object], slot_map: torch.Tensor, positions: Optional[torch.Tensor], status: torch.Tensor,
                  workspace: torch.Tensor) -> None:
     """Enqueue the update of `block_table`, `held`, `free_ids` and `free_count` (all in place) for the lengths in `kv_len` and
-    `q_indptr`, and the slots and positions of the new tokens.  What stands in `status` after it says whether it was done."""
-    bt = _batch_descriptor(d)
-    pool = ss_block_pool(d["num_blocks"], _ptr(d["free_ids"]), _ptr(d["free_count"]))
-    _check(lib().ss_block_map(ctypes.byref(bt), ctypes.byref(pool), _ptr(d["held"]), d["total_rows"], _ptr(slot_map), _ptr(positions),
-                              _ptr(status), _ptr(workspace), workspace.nbytes, _stream()))
+    `q_indptr`, and the slots and positions of the new tokens (int32).  What stands in `status` after it says whether it was done."""
+    bt, rows = _batch_descriptor(d), d["total_rows"]
+    pool = ss_block_pool(d["num_blocks"], d["free_ids"].data_ptr(), d["free_count"].data_ptr())
+    _check(lib().ss_block_map(ctypes.byref(bt), ctypes.byref(pool), d["held"].data_ptr(), rows, _ints("slot_map", slot_map, rows),
+                              0 if positions is None else _ints("positions", positions, rows), _ints("status", status, 1), workspace.data_ptr(), workspace.nbytes, _stream()))
 
 
 def alloc_block_map_workspace(d: Dict[str, object], device="cuda:0") -> torch.Tensor:
+    _check_batch(d)
+    _ints("held", d["held"], d["batch"])
+    _ints("free_ids", d["free_ids"], d["num_blocks"])
+    _ints("free_count", d["free_count"], 1)
     n = lib().ss_block_map_workspace(d["batch"])
     if n == 0:
         raise SpecVerifyError(lib().ss_last_error().decode())
@@ -319,11 +369,11 @@ def alloc_block_map_workspace(d: Dict[str, object], device="cuda:0") -> torch.Te
 
 
 def ss_kv_write(d: Dict[str, object], slot_map: torch.Tensor) -> None:
-    """Enqueue the write of `k_new`/`v_new` [rows][kv heads][head_dim] (rows may be apart) to the slots of the device batch's paged cache."""
+    """Enqueue the write of `k_new`/`v_new` [rows][kv heads][head_dim] (rows may be apart) to the slots (int32) of the device batch's paged cache."""
     kv = _cache_descriptor(d)
-    rows, heads, dim = d["total_rows"], d["num_kv_heads"], d["head_dim"]
-    _check(lib().ss_kv_write(ctypes.byref(kv), _ptr(slot_map), _ptr(d["k_new"]), _row_stride(d["k_new"], rows, heads, dim), _ptr(d["v_new"]),
-                             _row_stride(d["v_new"], rows, heads, dim), _DT[d["new_dtype"]], rows, _stream()))
+    rows, heads, dim, kind = d["total_rows"], d["num_kv_heads"], d["head_dim"], d["new_dtype"]
+    _check(lib().ss_kv_write(ctypes.byref(kv), _ints("slot_map", slot_map, rows), *_rows("k_new", d["k_new"], kind, rows, heads, dim),
+                             *_rows("v_new", d["v_new"], kind, rows, heads, dim), _DT[kind], rows, _stream()))
 
 
 def ss_chunk_attn_workspace(d: Dict[str, object], max_q_len: int = 0) -> int:
@@ -336,15 +386,18 @@ def ss_chunk_attn_workspace(d: Dict[str, object], max_q_len: int = 0) -> int:
 
 def ss_chunk_attn(d: Dict[str, object], out: torch.Tensor, lse: Optional[torch.Tensor], workspace: torch.Tensor,
                   max_q_len: int = 0) -> None:
-    """Enqueue attention of a device batch's chunks; `q` [rows][heads][head_dim] may have its rows apart, `out` is dense."""
+    """Enqueue attention of a device batch's chunks; `q` [rows][heads][head_dim] may have its rows apart, `out` and `lse` are dense."""
     kv, bt = _cache_descriptor(d), _batch_descriptor(d, max_q_len)
-    _check(lib().ss_chunk_attn(ctypes.byref(kv), ctypes.byref(bt), _ptr(d["q"]), _row_stride(d["q"], d["total_rows"], d["num_q_heads"], d["head_dim"]),
-                               _DT[d["q_dtype"]], d["num_q_heads"], d["total_rows"], d["sm_scale"], _ptr(out), _ptr(lse),
-                               _ptr(workspace), workspace.nbytes, _stream()))
+    rows, heads, dim, kind = d["total_rows"], d["num_q_heads"], d["head_dim"], d["q_dtype"]
+    _check(lib().ss_chunk_attn(ctypes.byref(kv), ctypes.byref(bt), *_rows("q", d["q"], kind, rows, heads, dim), _DT[kind], heads, rows, d["sm_scale"],
+                               _dense("out", out, _SIZE[kind], rows * heads * dim), 0 if lse is None else _dense("lse", lse, 4, rows * heads),
+                               workspace.data_ptr(), workspace.nbytes, _stream()))
 
 
 def alloc_chunk_outputs(d: Dict[str, object], device="cuda:0", max_q_len: int = 0):
     """Allocate (out, lse, workspace) for a device batch's chunks.  `out` holds raw storage (int16 = bf16 bits)."""
+    _check_batch(d)
+    _check_cache(d)
     shape = (d["total_rows"], d["num_q_heads"], d["head_dim"])
     out = torch.empty(shape, dtype=torch.float32 if d["q_dtype"] == "f32" else torch.int16, device=device)
     lse = torch.empty(shape[:2], dtype=torch.float32, device=device)

@@ -298,3 +298,26 @@ def test_the_example_stops_where_blocks_are_missing(monkeypatch):
     with pytest.raises(RuntimeError, match="status 4"):
         example.run(steps=2, batch=4, layers=1, vocab=4096, seed=1, verbose=False, chunk=4000)
     assert steps[0] == 2 and not calls
+
+
+def test_tensors_that_are_not_what_a_call_writes():
+    """On the GPU, where only the type, the length or the strides are wrong: refused before anything is enqueued."""
+    lane = Lane(2, 10, 33, 1, 4, 2, 64, "bf16", "bf16", seed=1)
+    b, wide, slots, positions = lane.batch_of([(20, 20), (5, 5)])
+    d, ws = lane.layer(b, wide, 0), binding.alloc_block_map_workspace(b)
+    out, z, wc = binding.alloc_chunk_outputs(d)
+    n = slots.numel()
+    for call, text in [
+        (lambda: binding.ss_block_map(d, slots.long(), positions, lane.status, ws), "slot_map"), (lambda: binding.ss_block_map(d, slots, positions[:-1], lane.status, ws), "positions"),
+        (lambda: binding.ss_block_map(d, slots, None, lane.status.float(), ws), "status"), (lambda: binding.ss_kv_write(d, slots.long()), "slot_map"),
+        (lambda: binding.ss_kv_write(d, torch.zeros(2 * n, dtype=torch.int32, device=DEV)[::2]), "slot_map"), (lambda: binding.ss_kv_write(dict(d, k_new=d["k_new"].float()), slots), "k_new"),
+        (lambda: binding.ss_kv_write(dict(d, v_new=d["v_new"].float()), slots), "v_new"), (lambda: binding.ss_chunk_attn(d, out.float(), z, wc), "out"),
+        (lambda: binding.ss_chunk_attn(d, torch.zeros((n, 4, 128), dtype=torch.int16, device=DEV)[..., :64], z, wc), "out"), (lambda: binding.ss_chunk_attn(d, out, z.half(), wc), "lse"),
+        (lambda: binding.ss_chunk_attn(d, out, z[:-1], wc), "lse"), (lambda: binding.alloc_chunk_outputs(dict(d, k_cache=d["k_cache"].float())), "k_cache"),
+        (lambda: binding.alloc_chunk_outputs(dict(d, v_cache=d["v_cache"][1:])), "v_cache"), (lambda: binding.alloc_chunk_outputs(dict(d, kv_len=d["kv_len"].long())), "kv_len"),
+        (lambda: binding.alloc_block_map_workspace(dict(d, held=d["held"].long())), "held"), (lambda: binding.alloc_block_map_workspace(dict(d, free_ids=d["free_ids"][1:])), "free_ids")]:
+        with pytest.raises(binding.SpecVerifyError, match=text):
+            call()
+    binding.ss_block_map(d, slots, positions, lane.status, ws)
+    torch.cuda.synchronize()
+    assert int(lane.status) == 0

@@ -104,3 +104,37 @@ def test_rows_of_tensors():
                     (torch.empty(6, 64, 4).transpose(1, 2), (6, 4, 64))):
         with pytest.raises(binding.SpecVerifyError):
             stride(t, *args)
+
+
+def test_tensors_that_are_not_what_an_address_says():
+    """Types, lengths and strides are looked at before the library is called; so is the device, on which everything else of these is wrong."""
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    half = lambda *s: torch.zeros(s, dtype=torch.bfloat16)  # noqa: E731
+    base = dict(batch=2, num_q_heads=4, num_kv_heads=2, head_dim=64, block_size=16, num_blocks=6, max_blocks_per_seq=3, total_rows=5, kv_dtype="bf16", q_dtype="bf16",
+                new_dtype="bf16", sm_scale=0.1, block_table=i32(2, 3), kv_len=i32(2), q_indptr=i32(3), held=i32(2), free_ids=i32(6), free_count=i32(1),
+                k_cache=half(6, 2, 16, 64), v_cache=half(6, 2, 16, 64), k_scale=None, v_scale=None, k_new=half(5, 2, 64), v_new=half(5, 2, 64), q=half(5, 4, 64))
+    ws = torch.zeros(1024, dtype=torch.uint8)
+
+    def calls(d, slots=i32(5), positions=i32(5), status=i32(1), out=half(5, 4, 64), lse=torch.zeros(5, 4)):
+        binding.ss_block_map(d, slots, positions, status, ws)
+        binding.ss_kv_write(d, slots)
+        binding.ss_chunk_attn(d, out, lse, ws)
+
+    write = lambda d, slots=i32(5): binding.ss_kv_write(d, slots)  # noqa: E731
+    attend = lambda d, out=half(5, 4, 64), lse=torch.zeros(5, 4): binding.ss_chunk_attn(d, out, lse, ws)  # noqa: E731
+    long = torch.int64
+    for call, text in [
+        (lambda: calls(base, slots=i32(5).to(long)), "slot_map .* torch.int64"), (lambda: calls(base, slots=i32(4)), "slot_map .* at least 5"),
+        (lambda: calls(base, slots=i32(10)[::2]), "slot_map .*strides"), (lambda: write(base, i32(5).to(long)), "slot_map .* torch.int64"),
+        (lambda: write(base, i32(4)), "slot_map .* at least 5"),
+        (lambda: write(dict(base, k_new=torch.zeros(5, 2, 64))), "slot_map .* on cpu"),
+        (lambda: attend(dict(base, q=torch.zeros(5, 4, 64))), "q must be of type bf16"), (lambda: attend(dict(base, q=half(4, 4, 64))), "expected 5 rows"),
+        (lambda: binding.alloc_chunk_outputs(dict(base, block_table=i32(3, 2).T)), "block_table"), (lambda: binding.alloc_block_map_workspace(dict(base, block_table=i32(5))), "block_table"),
+        (lambda: binding.alloc_block_map_workspace(base), "block_table .* on cpu"), (lambda: calls(base), "slot_map .* on cpu"), (lambda: attend(base), "q must be .* on cpu")]:
+        with pytest.raises(binding.SpecVerifyError, match=text):
+            call()
+    for check, args, text in [
+        (binding._ints, ("x", i32(3).float(), 3), "float32"), (binding._dense, ("x", half(4), 4, 4), "4 bytes"), (binding._dense, ("x", torch.zeros(4, 4).T, 4, 16), "strides"),
+        (binding._dense, ("x", torch.zeros(3), 4, 4), "at least 4"), (binding._dense, ("x", torch.zeros(4), 4, 4), "on cpu"), (binding._rows, ("x", torch.zeros(2, 1, 64), "bf16", 2, 1, 64), "type bf16")]:
+        with pytest.raises(binding.SpecVerifyError, match=text):
+            check(*args)
