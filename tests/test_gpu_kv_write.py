@@ -196,7 +196,7 @@ def test_e4m3_codes_at_and_beside_ties(new):
 @pytest.mark.parametrize("hkv,groups", [(2, 30), (8, 30), (8, 120), (8, 300)])
 @pytest.mark.parametrize("new", ["f32", "bf16"])
 def test_blocks_whose_rows_stand_between_each_other(new, hkv, groups):
-    """e4m3: rows of two or three blocks in turn or at random, each block's as far apart as their slots; all of a block's rows make its scale (windows of 1, 4 and 16 rows)."""
+    """e4m3: rows of two or three blocks in turn or at random, each block's as far apart as their slots; all of a block's rows make its scale (few rows and many, which windows depend on)."""
     rng = np.random.default_rng(groups)
     total = groups * 3 + 2
     blocks, slots = rng.permutation(total), []
