@@ -12,9 +12,14 @@
 
 namespace ss {
 
-constexpr int kMinPiece = 3;         // steps below which a piece costs more than it brings
+// Steps below which a piece costs more than it brings, where there are not spans enough for all workgroups.  With 2 | 3 | 5, us: one token behind 64 14.1 | 11.6 |
+// 12.3, 33 behind 700 18.7 | 21.0 | 21.4, a prompt of 500 28.7 | 26.7 | 28.4, 200 behind 1000 35.2 | 35.2 | 32.7 (32 heads over 8, bf16); over an e4m3 cache a prompt of 500
+// 31.2 | 28.7 | 31.8, 64 behind 2000 27.7 | 27.0 | 30.7; fp32, two requests of 100 behind 400, 25.3 | 25.3 | 38.7.
+constexpr int kMinPiece = 3;
 constexpr int kOpenFew = 1;          // a tile's cost beside its steps where there are not spans enough for all workgroups: their openings run side by side
-constexpr int kSnap = 1;             // steps of a tile that no cut is made for
+// Steps of a tile that no cut is made for.  With 0 | 1 | 2, us: 33 tokens behind 700 21.0 | 21.0 | 22.1, a prompt of 2048 64.2 | 63.2 | 63.2; fp32, four requests
+// of 20 .. 150 tokens, 24.6 | 24.9 | 33.9.
+constexpr int kSnap = 1;
 
 template <typename T>
 __device__ __forceinline__ T wave_incl_sum(T x)
@@ -79,6 +84,7 @@ struct ChunkPos {
 template <int ROWS, int KEYS, int OPEN>
 struct ChunkWalk {
     typedef ChunkUnit<ROWS, KEYS> Unit;
+    static_assert(OPEN > kOpenFew, "begin() takes the cost of few spans once, where the other one does not do");
     // the current piece: steps s0 to before s1 of tile t of request b.  part: place of its partial result, -1 if it is the whole tile.
     int b, t, s0, s1, part;
     Unit u;

@@ -61,7 +61,9 @@ __device__ __forceinline__ int chunk_block(const ChunkArgs &a, int id)
 constexpr int kChunkRecInts = 4;
 constexpr int kChunkKeys = 32, kChunkKeysF32 = 64;   // keys of a step
 constexpr int kChunkRows = 256, kChunkRowsF32 = 64;   // query rows of a tile: bf16 matrix-core kernel, fp32 kernel
-constexpr int kChunkOpen = 9, kChunkOpenF32 = 3;      // what a tile costs beside its steps, in steps
+// What a tile costs beside its steps, in steps.  With 5 | 9 | 13, us: a prompt of 2048 74.5 | 63.2 | 65.1, 24 mixed requests 322 | 316 | 311, four over an e4m3 cache 321 | 309 | 309;
+// fp32: 2, 3 and 6 are level (25.0).
+constexpr int kChunkOpen = 9, kChunkOpenF32 = 3;
 
 struct ChunkShape {               // host-visible sizes a launch and its workspace follow from
     int32_t rows;                 // query rows of a tile
