@@ -179,7 +179,8 @@ int32_t ss_chunk_attn(const ss_paged_kv *kv, const ss_batch *batch, const void *
     if (!batch->block_table || !batch->kv_len || !batch->q_indptr || !out) return fail(SS_ERR_INVALID_ARG, "a required device pointer is NULL");
     if ((rc = check_rows("q", q, q_stride, (int64_t)num_q_heads * kv->head_dim, q_dtype)) != SS_OK) return rc;
     if (!aligned16(out)) return fail(SS_ERR_INVALID_ARG, "out must be 16-byte aligned");
-    if (!(sm_scale > 0.0f) || sm_scale > 3.4e38f) return fail(SS_ERR_INVALID_ARG, "sm_scale must be positive and finite");
+    if (!(sm_scale > 0.0f) || sm_scale > 2.0e38f)   // (times log2(e) it has to be a float, too)
+        return fail(SS_ERR_INVALID_ARG, "sm_scale must be positive and at most 2e38");
     const bool mfma = chunk_mfma_supported(kv->head_dim, kv->dtype, q_dtype);
     const ChunkShape s = chunk_shape(mfma, batch->batch, batch->max_blocks_per_seq, num_q_heads, kv->num_kv_heads, total_rows);
     const size_t need = chunk_workspace_bytes(s, kv->head_dim);

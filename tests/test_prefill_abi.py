@@ -57,6 +57,13 @@ def test_chunk_attention(L):
     assert call(rows=0) == 0 and call(b=bt(batch=0)) == 0         # nothing to do, nothing launched
 
 
+def test_a_scale_whose_powers_of_two_are_no_float(L):
+    call = lambda scale: L.ss_chunk_attn(kv(), bt(), P, 4096, 1, 32, 100, scale, P, None, P, 100, None)  # noqa: E731
+    refused(L, call(2.5e38), 1, b"sm_scale")
+    refused(L, call(-1.0), 1, b"sm_scale")
+    refused(L, call(1.9e38), 3, b"needed")               # (the next check's refusal)
+
+
 def test_chunk_workspace(L):
     size = lambda rows, blocks, dtype=1, **kw: L.ss_chunk_attn_workspace(kv(**kw), bt(max_blocks_per_seq=blocks), dtype, 32, rows)  # noqa: E731
     assert size(100, 8) >= 256 and size(100, 1000) >= size(100, 100) >= size(100, 8)
