@@ -52,7 +52,19 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y)
     const float2v v = {x, y};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
-__device__ __forceinline__ float bf16_value(const void *base, int64_t i) { return __uint_as_float((uint32_t) static_cast<const uint16_t *>(base)[i] << 16); }
+// four consecutive elements of bf16 or e4m3, from a multiple of four
+template <bool FP8>
+__device__ __forceinline__ float4v load4(const void *base, int64_t i)
+{
+    if constexpr (FP8) {
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(base) + i);
+        const float2v x = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), y = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+        return float4v{x.x, x.y, y.x, y.y};
+    } else {
+        const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(base) + i);
+        return float4v{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u)};
+    }
+}
 // x and the two of a pair of bf16, added
 __device__ __forceinline__ float pair_sum(uint32_t pair, float x)
 {
@@ -350,10 +362,6 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
             if constexpr (FP8) return max_of_halves(__builtin_elementwise_maximum(top[0] * ks_next[0], top[1] * ks_next[1]));
             else return max_of_halves(__builtin_elementwise_maximum(top[0], top[1])) * c;
         };
-        auto element = [&](const void *cache, int64_t i) __attribute__((always_inline)) {
-            if constexpr (FP8) return __builtin_amdgcn_cvt_f32_fp8((int)static_cast<const uint8_t *>(cache)[i], 0);
-            else return bf16_value(cache, i);
-        };
         auto follow = [&](const float (&top)[NB]) __attribute__((always_inline)) {
             bool rise = false;
 #pragma unroll
@@ -421,7 +429,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
                     for (int b = 0; b < DB; ++b)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            float v = element(a.v, at0 + b * 32 + i / 4 * 8 + i % 4);
+                            const int64_t at = at0 + b * 32 + i / 4 * 8 + i % 4;
+                            float v;
+                            if constexpr (FP8) v = __builtin_amdgcn_cvt_f32_fp8((int)static_cast<const uint8_t *>(a.v)[at], 0);
+                            else v = __uint_as_float((uint32_t) static_cast<const uint16_t *>(a.v)[at] << 16);
                             if constexpr (FP8) v *= scale;
                             if (!__builtin_isfinite(v)) o[e][b][i] += v;
                         }
@@ -637,7 +648,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
             store(e, o[e], m[e], used, LSE ? sum_of_halves(l[e]) : used);
         }
         // The wavefront's rows again, a key at a time in fp32, the scale applied before the reference is taken off: the largest score's weight is one whatever
-        // its size.  (By itself, so that the steps need no register for it; some 2 us a key.)
+        // its size.  (By itself, so that the steps need no register for it: 0.45 ms for 64 tokens behind 1936, 1.4 for a prompt of 2048, with 8 heads over 2.)
         if (__builtin_expect((uniform(special) & kFarRows) != 0, 0)) {
 #pragma unroll 1
             for (int e = 0; e < NB; ++e) {
@@ -650,8 +661,12 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
 #pragma clang fp contract(off)   // (a score is rounded before the reference, which is one of them, is taken off)
                     const int64_t block = (int64_t)chunk_block(a, block_table[(int64_t)s.b * a.max_blocks + pos / kTile]) * a.num_kv_heads + g, at = (block * kTile + pos % kTile) * D;
                     float y = 0.f;
-#pragma unroll 4
-                    for (int i = 0; i < D / 2; ++i) y = __builtin_fmaf(element(a.k, at + half * (D / 2) + i), bf16_value(a.q, q_at + i), y);
+#pragma unroll
+                    for (int j = 0; j < D / 2; j += 4) {
+                        const float4v key = load4<FP8>(a.k, at + half * (D / 2) + j), query = load4<false>(a.q, q_at + j);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y = __builtin_fmaf(key[i], query[i], y);
+                    }
                     y = (FP8 ? sum_of_halves(y) * k_scale[block] : sum_of_halves(y)) * c;
                     if (pos > last) continue;
                     const float up = fmaxf(ref, y), down = __builtin_amdgcn_exp2f(ref - up), w = __builtin_amdgcn_exp2f(y - up);
@@ -660,9 +675,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void chunk_kernel(ChunkArgs a, cons
 #pragma unroll
                     for (int b = 0; b < DB; ++b)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float v = element(a.v, at + half * 4 + b * 32 + i / 4 * 8 + i % 4);
-                            x[b][i] = x[b][i] * down + w * (FP8 ? v * v_scale[block] : v);
+                        for (int j = 0; j < 4; ++j) {
+                            const float4v v = load4<FP8>(a.v, at + half * 4 + b * 32 + j * 8);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) x[b][4 * j + i] = x[b][4 * j + i] * down + w * (FP8 ? v[i] * v_scale[block] : v[i]);
                         }
                 }
                 store(e, x, ref, sum, sum);
