@@ -29,6 +29,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 # Matrix instructions of attn_chunk.hip take either half of its 512 registers: left to itself the compiler puts the results of all of them, scores too, into the
 # half that ordinary arithmetic does not reach, moves every score over and spills (4096 tokens behind 12288: 1516 us against 903; four chunks over an e4m3 cache: 917 against 307).
+# A compiler that does not know the switch ends the build with its name; without it the kernel is slow, not wrong.
 FLAGS_OF = {"attn_chunk.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 # the host pass reports that it does not know the packed-fp32 feature; that line is noise
 NOISE = "is not a recognized feature for this target"

@@ -17,8 +17,8 @@
 // Outputs are divided by the sum of the weights as rounded, a sum of its own (5 %): where a few weights are most of it their roundings cancel, and the error
 // against 64 bits is 1.2 of what rounding the outputs costs instead of 1.4 (scores that spread by 1 to 4).  The log-sum-exp takes the sum of the weights
 // themselves; calls that do not ask for it have a form without that sum (3 % faster).
-// 903 us there, 1.07 PFLOP/s, where a large bf16 product of the library reaches 1.27 .. 1.36; 62 us for a prompt of 2048 tokens (32 heads over 8); e4m3 caches:
-// 307 us, 773 TFLOP/s, for four requests of 200 .. 1000 tokens behind 1000 .. 6000 (64 heads over 8), their codes turned to bf16 on the way into LDS.
+// 900 .. 940 us there by card, 1.02 .. 1.07 PFLOP/s, where a large bf16 product of the library reaches 1.27 .. 1.36; 63 us for a prompt of 2048 tokens (32 heads over 8); e4m3 caches:
+// 309 us, 768 TFLOP/s, for four requests of 200 .. 1000 tokens behind 1000 .. 6000 (64 heads over 8), their codes turned to bf16 on the way into LDS.
 #include <type_traits>
 
 #include "chunk_merge.h"
