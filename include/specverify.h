@@ -395,7 +395,7 @@ int32_t ss_block_map(const ss_batch *batch, const ss_block_pool *pool, int32_t *
  * then reads as NaN) and is cut at 448 in a block whose scale stands.
  *   kv              the cache; k, v, k_scale and v_scale are WRITTEN through although the struct declares them const
  *   slot_map        device int32 [total_rows], no slot twice.  For SS_FP8_E4M3 the rows of one block must stand as far apart in the
- *                   call as their slots, as ss_block_map gives them (rows that are left out may stand between)
+ *                   call as their slots, as ss_block_map gives them (rows that are left out, or other blocks', may stand between)
  *   k_new, v_new    device, rows of [num_kv_heads][head_dim] in new_dtype (SS_F32 or SS_BF16), k_stride / v_stride elements
  *                   apart (so they may be parts of wider rows); rows start 16-byte aligned
  */
@@ -411,6 +411,7 @@ int32_t ss_kv_write(const ss_paged_kv *kv, const int32_t *slot_map, const void *
  * block: nothing outside the arrays is read or written, whatever lengths and table hold.
  *   q          device, rows of [num_q_heads][head_dim] in q_dtype (SS_F32 or SS_BF16), q_stride elements apart (>= num_q_heads *
  *              head_dim); rows start 16-byte aligned
+ *   sm_scale   positive, at most 2e38
  *   out        device, dense [total_rows][num_q_heads][head_dim] in q_dtype; lse device float [total_rows][num_q_heads] or NULL.
  *              Rows from q_indptr[batch] on keep what they hold
  *   workspace  device, >= ss_chunk_attn_workspace(...) bytes, 256-byte aligned; contents are scratch.  It follows from the

@@ -160,7 +160,7 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
         l += __shfl_xor(l, 32);
         // the reference in powers of two, and what its rounding leaves (of references so large that this is no factor, nothing: it is within the scores' own rounding)
         const float ref = l == 0.f ? kChunkNoMax : fmaxf(m * c_hi, kChunkNoMax);
-        const float rest = fabsf(ref) < 0x1p20f ? __builtin_amdgcn_exp2f(__builtin_fmaf(m, c_hi, __builtin_fmaf(m, c_lo, -ref))) : 1.0f;
+        const float rest = fabsf(ref) < 0x1p20f ? __builtin_amdgcn_exp2f(__builtin_fmaf(m, c_lo, __builtin_fmaf(m, c_hi, -ref))) : 1.0f;
         if (s.part >= 0) {
             const int64_t part = (int64_t)s.part * a.num_kv_heads + g;
             float4v *po = reinterpret_cast<float4v *>(a.part_o) + part * (kRows * D / 4) + wave * (16 * D / 4) + lane;
