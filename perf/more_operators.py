@@ -566,15 +566,16 @@ def _plain_release(s):
     need = (k["kv_len"] + BLOCK - 1) // BLOCK
     j = torch.arange(s.width, device=DEV)
     given = ((j >= need[:, None]) & (j < k["held"][:, None])).view(-1)
-    ids = torch.where(given, k["table"].view(-1), s.num_blocks).long()
-    at = torch.arange(ids.numel(), device=DEV)
-    times = torch.zeros((s.num_blocks + 1,), dtype=torch.int32, device=DEV).scatter_add_(0, ids, given.to(torch.int32))
-    last = torch.full((s.num_blocks + 1,), -1, dtype=torch.int64, device=DEV).scatter_reduce_(0, ids, at, "amax")
-    gone = times[:-1] > k["shares"]
-    free = given & (last[ids] == at) & torch.cat([gone, gone.new_zeros(1)])[ids]
-    place = torch.where(free, k["free_count"] + free.cumsum(0) - 1, s.num_blocks)
-    pad = torch.cat([k["free_ids"], k["free_ids"].new_zeros(1)]).scatter_(0, place, k["table"].view(-1))
-    return dict(k, held=torch.minimum(k["held"], need), shares=(k["shares"] - times[:-1]).clamp(min=0), free_ids=pad[:-1],
+    N = s.num_blocks
+    at = torch.arange(given.numel(), device=DEV)
+    ids = torch.where(given, k["table"].view(-1).long(), N + at)                   # (what is kept: a place of its own behind the blocks)
+    times = torch.zeros((N + at.numel(),), dtype=torch.int32, device=DEV).scatter_add_(0, ids, given.to(torch.int32))
+    last = torch.full((N + at.numel(),), -1, dtype=torch.int64, device=DEV).scatter_reduce_(0, ids, at, "amax")
+    gone = torch.cat([times[:N] > k["shares"], given.new_zeros(at.numel())])
+    free = given & (last[ids] == at) & gone[ids]
+    place = torch.where(free, k["free_count"] + free.cumsum(0) - 1, N + at)
+    pad = torch.cat([k["free_ids"], k["free_ids"].new_zeros(at.numel())]).scatter_(0, place, k["table"].view(-1))
+    return dict(k, held=torch.minimum(k["held"], need), shares=(k["shares"] - times[:N]).clamp(min=0), free_ids=pad[:N],
                 free_count=k["free_count"] + free.sum().to(torch.int32), status=torch.zeros((1,), dtype=torch.int32, device=DEV))
 
 
