@@ -18,6 +18,11 @@
  * requests' lengths), ss_kv_write (a chunk's keys and values by slot) and ss_chunk_attn
  * (attention of a chunk of new tokens, of any length, over the cache).
  *
+ * For draft trees of any width and caches that requests share: ss_tree_attn (attention of a tree's
+ * nodes over the cache), ss_tree_verify (the walk through a tree whose tokens come without proposal
+ * distributions), ss_block_fork, ss_block_release, ss_block_compact and ss_block_copy (blocks that
+ * several requests hold).
+ *
  * Around them, the other steps of a decode loop: ss_kv_append (write the new
  * tokens' K/V before verification), ss_kv_commit (valid lengths after
  * acceptance), for tree-shaped drafts ss_batch.tree_mask,
@@ -318,8 +323,9 @@ int32_t ss_kv_append(const ss_paged_kv *kv, const ss_batch *batch, const void *k
  * blocks: byte' = nearest e4m3fn (ties to even) of clamp((decode(byte) * scale_src) / scale_dst, +-448),
  * product and quotient one float32 operation each.  No scale changes; all other slots, the rejected
  * ones included, keep their contents.  For a chain (a_j = j) nothing moves.
- *   kv, batch       as for ss_kv_append (kv_len still counts all q_len new tokens; the cache is WRITTEN)
- *   accepted_nodes  device int32 [batch][SS_MAX_DEPTH], as written by ss_spec_accept_tree_greedy
+ *   kv, batch       as for ss_kv_append (kv_len still counts all q_len new tokens; the cache is WRITTEN), but a request may bring any
+ *                   number of new tokens, and max_q_len be any bound of them
+ *   accepted_nodes  device int32 [batch][SS_MAX_DEPTH], as written by ss_spec_accept_tree_greedy or ss_tree_verify
  *   accepted_len    device int32 [batch]
  * A row of accepted_nodes that is not increasing within 1..q_len-1 ends that request's moves at the
  * offending entry (nothing outside the request's new slots is ever touched).
@@ -332,7 +338,7 @@ int32_t ss_kv_compact(const ss_paged_kv *kv, const ss_batch *batch, const int32_
  * Commit after acceptance (same passage): request b keeps its accepted_len[b] accepted drafts, so its
  * valid cache length becomes kv_len[b] - k_b + accepted_len[b] with k_b = q_indptr[b+1]-q_indptr[b]-1;
  * the rejected slots fall past the end (no data moves), and the token the acceptance step drew is
- * appended by the next step.  All arrays are device arrays; kv_len [batch] is updated in place.
+ * appended by the next step; a request without new tokens keeps its length.  All arrays are device arrays; kv_len [batch] is updated in place.
  * Errors: SS_ERR_INVALID_ARG (NULL pointers, negative batch), SS_ERR_DEVICE.
  */
 int32_t ss_kv_commit(int32_t batch, const int32_t *q_indptr, const int32_t *accepted_len, int32_t *kv_len,
@@ -380,7 +386,8 @@ typedef struct ss_block_pool {
  *               ss_kv_write writes nothing; ss_chunk_attn behind it stays inside its arrays, but what it puts out is of no use.  Calls
  *               that follow the table without bounds (ss_kv_append, ss_spec_verify_attn) must not be made before status is known to be 0.
  *   workspace   device, >= ss_block_map_workspace(batch) bytes, 256-byte aligned; contents are scratch
- * One call at a time for one pool; a block belongs to one request only (shared prefixes are the caller's).
+ * One call at a time for one pool.  A block that a request gives back here must be its own alone: where blocks may be shared,
+ * ss_block_release stands in front of this call and leaves it nothing to give back.
  */
 size_t ss_block_map_workspace(int32_t batch);
 int32_t ss_block_map(const ss_batch *batch, const ss_block_pool *pool, int32_t *held, int32_t total_rows, int32_t *slot_map,
@@ -425,6 +432,129 @@ size_t ss_chunk_attn_workspace(const ss_paged_kv *kv, const ss_batch *batch, int
 int32_t ss_chunk_attn(const ss_paged_kv *kv, const ss_batch *batch, const void *q, int64_t q_stride, int32_t q_dtype, int32_t num_q_heads,
                       int32_t total_rows, float sm_scale, void *out, float *lse, void *workspace, size_t workspace_bytes,
                       void *stream);
+
+/*
+ * Draft trees wider than ss_spec_verify_attn's (Section 2.2: dynamic draft trees, verified in one parallel pass).  A request brings any
+ * number of new tokens, none included, the nodes of its tree in an order in which parents precede children, node 0 the last accepted
+ * token; node j is at cache position kv_len - q_len + j.  A step:
+ *     ss_block_map, ss_kv_write, ss_tree_attn     blocks, keys and values, attention (the latter two once a layer)
+ *     ss_tree_verify                              the accepted path and the next token
+ *     ss_kv_compact, ss_kv_commit                 the path to where a chain would stand; new lengths
+ * As in the calls above, q_indptr[batch] may be smaller than total_rows and ss_batch.max_q_len is an upper bound of any size (0 = unknown);
+ * SS_BATCH_REUSE_PLAN has no effect, and ss_batch.tree_mask must be NULL.
+ */
+
+/*
+ * Attention of the nodes of draft trees over the paged cache, in which their keys and values already are.  With P = kv_len_b - q_len_b, row i
+ * of request b attends cache position t iff t < P, or node t - P is one that its mask names:
+ *     s_t = sm_scale * <q[row,h,:], K_b[t,:]>,   out[row,h,:] = sum_t softmax(s)_t * V_b[t,:],   lse[row,h] = ln sum_t exp(s_t)
+ * A row that attends nothing (no context, an empty mask): zeros, and lse minus infinity.
+ *   node_mask   device uint32, rows of mask_words words, dense: bit j % 32 of word j / 32 of a row says that the row attends node j of its own
+ *               request, in any pattern (a tree's: its own node and its ancestors).  Bits at or behind q_len_b are not looked at
+ *   mask_words  words of a mask row; a request with more than 32 * mask_words new tokens is left out, as one whose rows lie outside
+ *               [0, total_rows] or whose kv_len passes its row of the table (its rows keep what they hold); a block id outside the cache is
+ *               read as its last block: nothing outside the arrays is read or written
+ *   batch->max_q_len  also picks the number of query rows that a workgroup takes at a time: a tight bound is up to twice as fast for
+ *               small trees, a wrong one costs time only
+ * q, sm_scale, out, lse, total_rows and workspace as for ss_chunk_attn (a workspace sized for a bound, or for 0, serves that bound only); so are
+ * types, head counts and what is computed in which type.
+ */
+size_t ss_tree_attn_workspace(const ss_paged_kv *kv, const ss_batch *batch, int32_t q_dtype, int32_t num_q_heads, int32_t total_rows);
+int32_t ss_tree_attn(const ss_paged_kv *kv, const ss_batch *batch, const uint32_t *node_mask, int32_t mask_words, const void *q, int64_t q_stride,
+                     int32_t q_dtype, int32_t num_q_heads, int32_t total_rows, float sm_scale, void *out, float *lse, void *workspace,
+                     size_t workspace_bytes, void *stream);
+
+/*
+ * Verification of draft trees whose tokens come without the distributions they were proposed from (the likeliest candidates of a draft model, an
+ * n-gram table): the target draws its own token at every node from a given uniform, and the walk goes on while a child carries it.
+ *     cur = 0; repeat: p = softmax(target row of cur / T_b)
+ *         y = first token whose running sum of p (token order) exceeds uniforms[row of cur]; T_b <= 0: the largest logit's, the lowest of several
+ *         c = lowest-numbered child of cur whose token is y; none, or max_depth nodes accepted: emit y and stop;  else accept c, emit y, cur = c
+ * Every emitted token is a draw from the target's distribution behind what was emitted before it, whatever the tree proposes.
+ *   max_depth       1 .. SS_MAX_DEPTH, or 0 for SS_MAX_DEPTH: a request accepts at most this many nodes
+ *   tree_parent     device int32 [total_rows]; of a request's node 0 it is not looked at; a node is a child of an earlier one or of none
+ *   node_tokens     device int32 [total_rows]: the nodes' tokens (node 0's is not looked at)
+ *   target_logits   rows of vocab entries, row_stride elements apart (>= vocab), in logit_dtype (SS_F32 or SS_BF16), 16-byte aligned; minus
+ *                   infinity and NaN are masked.  A row with an infinite logit gives the first such token, one with nothing but masked ones token 0
+ *   uniforms        device float [total_rows] in [0, 1), one for the draw at each node; NULL if temperature is NULL and temperature_scalar <= 0
+ *   temperature     device float [batch], or NULL to use temperature_scalar for all; 0 and below (and NaN): the largest logit's token
+ *   accepted_len    device int32 [batch]: accepted nodes n (0 for a request without rows, whose other outputs are all -1 and 0; so is one whose rows lie
+ *                   outside [0, total_rows])
+ *   out_tokens      device int32 [batch][SS_OUT_WIDTH]: the n + 1 emitted tokens, then -1
+ *   accepted_nodes  device int32 [batch][SS_MAX_DEPTH]: the accepted node numbers in path order, then -1 (what ss_kv_compact takes)
+ *   logprobs        device float [batch][SS_OUT_WIDTH] or NULL: ln p of each emitted token (0 where it was not drawn from a distribution), then 0
+ *   workspace       device, >= ss_tree_verify_workspace(...) bytes, 256-byte aligned; contents are scratch
+ * Sums and the draw are fp64 with fixed orders, so that the tokens are those of a 64-bit reference.
+ */
+size_t ss_tree_verify_workspace(int32_t batch, int32_t total_rows, int32_t vocab);
+int32_t ss_tree_verify(int32_t batch, int32_t vocab, int64_t row_stride, int32_t logit_dtype, int32_t total_rows, int32_t max_depth, const int32_t *q_indptr,
+                       const int32_t *tree_parent, const int32_t *node_tokens, const void *target_logits, const float *uniforms, const float *temperature,
+                       float temperature_scalar, int32_t *accepted_len, int32_t *out_tokens, int32_t *accepted_nodes, float *logprobs, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/*
+ * Blocks that several requests hold (Section 2.4: paged KV): samples of one prompt, the continuations of a search, prefixes that stay.
+ * shares, device int32 [pool->num_blocks], says of each block how many requests hold it beyond the first: 0 for a free block and for one that a single
+ * request holds, so a cache that was never forked is all zeros and ss_block_map works on it as ever.  New tokens go to blocks that one request holds
+ * alone: a request that is shortened (ss_kv_commit never does this) into a block that it shares is forked at its length into another row of the batch
+ * and left.  As for ss_block_map: block_table and kv_len are WRITTEN through although the struct declares them const, q_indptr is not
+ * read, one call at a time for one pool; status says whether it was done, all or nothing; ids that are no block's are never followed.
+ */
+
+/*
+ * Forks: child[i] becomes a request of the first length[i] tokens of parent[i].  Blocks that these fill are shared; of one that they fill in part the
+ * child gets one of its own, from the top of the free list in the order of i, to be filled by ss_block_copy.
+ *   num_forks, parent, child   device int32 [num_forks]: rows of the batch.  A child holds nothing before (held 0) and is named once, and no parent of
+ *               the call; a parent may be named often.  parent[i] < 0: no fork (copy_src[i] = copy_dst[i] = -1)
+ *   length      device int32 [num_forks], 0 .. kv_len[parent[i]], or NULL: all of kv_len[parent[i]]
+ *   held, kv_len, block_table  of the children are set, free_count and shares follow
+ *   copy_src, copy_dst   device int32 [num_forks]: the block to copy and where to, -1 where there is none
+ *   status      device int32 [1]: 0; s > 0: s blocks are missing; s < 0: fork -1-s is impossible (rows, lengths, a child that holds blocks or is
+ *               named before, a parent that is a child), s = -1-num_forks: the free list's length is.  Then nothing else changed, and all pairs are -1
+ */
+size_t ss_block_fork_workspace(int32_t batch, int32_t num_forks);
+int32_t ss_block_fork(const ss_batch *batch, const ss_block_pool *pool, int32_t *shares, int32_t *held, int32_t num_forks, const int32_t *parent,
+                      const int32_t *child, const int32_t *length, int32_t *copy_src, int32_t *copy_dst, int32_t *status, void *workspace,
+                      size_t workspace_bytes, void *stream);
+
+/*
+ * Gives back what requests hold beyond ceil(kv_len[b]/16) blocks (a request that has ended: kv_len 0), as ss_block_map does, but counting holders: in the
+ * order of (request, logical block) a block loses a holder, and the last one puts it on top of the free list.  (A block that is given back more
+ * often than it is held is put there once.)  Requests that hold less keep what they hold.
+ *   held        device int32 [batch]: min(held, ceil(kv_len/16)) after the call
+ *   status      device int32 [1]: 0; s < 0: request -1-s has impossible lengths (kv_len or held below 0, held beyond the table's columns), s = -1-batch: the free
+ *               list's length is.  Then nothing else changed
+ */
+size_t ss_block_release_workspace(int32_t batch, int32_t max_blocks_per_seq);
+int32_t ss_block_release(const ss_batch *batch, const ss_block_pool *pool, int32_t *shares, int32_t *held, int32_t *status, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+/*
+ * Moves the blocks in use to the front of the cache.  With U = num_blocks - *free_count, the blocks in use with ids from U on take the free ids below
+ * U, both in ascending order; after ss_block_copy has followed for every layer all ids from U on are free, and the cache can be cut there.
+ *   block_table  its first held[b] entries of each row are renumbered
+ *   free_ids     its first *free_count entries become num_blocks - 1 down to U (the lowest is taken first)
+ *   shares       moves with its blocks (NULL: no block is shared)
+ *   remap        device int32 [num_blocks] or NULL: the new id of every block (for tables that are not in this batch; a free block's is its own)
+ *   copy_src, copy_dst   device int32 [num_blocks / 2]: the pairs to copy, then -1.  No block is in both
+ *   num_copies   device int32 [1]: how many
+ *   status      device int32 [1]: 0; s < 0: request -1-s has an impossible held, s = -1-batch: the free list has an impossible length, an id that is no block's, or one
+ *               twice.  Then nothing else changed, num_copies is 0, all pairs are -1 and remap is every id itself
+ */
+size_t ss_block_compact_workspace(int32_t num_blocks);
+int32_t ss_block_compact(const ss_batch *batch, const ss_block_pool *pool, int32_t *shares, const int32_t *held, int32_t *remap, int32_t *copy_src,
+                         int32_t *copy_dst, int32_t *num_copies, int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Copies blocks, keys, values and scales as they are, in all layers of a cache: block copy_dst[i] becomes what block copy_src[i] is.
+ *   layers      host, num_layers caches of one shape and type (num_blocks, heads, head_dim, dtype); k, v, k_scale, v_scale are WRITTEN through.  The
+ *               array is read before the call returns
+ *   copy_src, copy_dst   device int32 [max_copies]; pairs with an id that is no block's are left out.  A block that is written by one pair and read or
+ *               written by another holds parts of either afterwards
+ *   num_copies  device int32 [1] or NULL: only the first *num_copies pairs (at most max_copies)
+ */
+int32_t ss_block_copy(const ss_paged_kv *layers, int32_t num_layers, const int32_t *copy_src, const int32_t *copy_dst, int32_t max_copies,
+                      const int32_t *num_copies, void *stream);
 
 /*
  * Speculation-depth controller (paper Section 3.5, Eq. 8-16, Algorithm 4): host arithmetic only, no

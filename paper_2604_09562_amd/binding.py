@@ -25,7 +25,8 @@ EXPORTS = ("ss_version", "ss_last_error", "ss_spec_verify_attn_workspace", "ss_s
            "ss_spec_accept_workspace", "ss_spec_accept", "ss_spec_accept_static", "ss_spec_accept_static_capacity",
            "ss_spec_accept_tree_greedy", "ss_spec_accept_tree_sample_workspace",
            "ss_spec_accept_tree_sample", "ss_block_map_workspace", "ss_block_map", "ss_kv_write", "ss_chunk_attn_workspace",
-           "ss_chunk_attn", "ss_kv_append", "ss_kv_compact", "ss_kv_commit", "ss_depth_init",
+           "ss_chunk_attn", "ss_tree_attn_workspace", "ss_tree_attn", "ss_tree_verify_workspace", "ss_tree_verify", "ss_block_fork_workspace",
+           "ss_block_fork", "ss_block_release_workspace", "ss_block_release", "ss_block_compact_workspace", "ss_block_compact", "ss_block_copy", "ss_kv_append", "ss_kv_compact", "ss_kv_commit", "ss_depth_init",
            "ss_depth_update", "ss_route_select", "ss_set_option",
            "ss_profile_begin", "ss_profile_collect")
 
@@ -135,6 +136,20 @@ def lib() -> ctypes.CDLL:
         L.ss_chunk_attn.argtypes = [ctypes.POINTER(ss_paged_kv), ctypes.POINTER(ss_batch), ctypes.c_void_p, ctypes.c_int64,
                                     ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p,
                                     ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+        ptr, i32, i64, size, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
+        kv_p, batch_p, pool_p = ctypes.POINTER(ss_paged_kv), ctypes.POINTER(ss_batch), ctypes.POINTER(ss_block_pool)
+        for name, args in (("ss_tree_attn", [kv_p, batch_p, ptr, i32, ptr, i64, i32, i32, i32, f32] + [ptr] * 3 + [size, ptr]),
+                           ("ss_tree_verify", [i32, i32, i64, i32, i32, i32] + [ptr] * 6 + [f32] + [ptr] * 5 + [size, ptr]),
+                           ("ss_block_fork", [batch_p, pool_p, ptr, ptr, i32] + [ptr] * 7 + [size, ptr]),
+                           ("ss_block_release", [batch_p, pool_p] + [ptr] * 4 + [size, ptr]),
+                           ("ss_block_compact", [batch_p, pool_p] + [ptr] * 8 + [size, ptr]),
+                           ("ss_block_copy", [kv_p, i32, ptr, ptr, i32, ptr, ptr])):
+            fn = getattr(L, name)
+            fn.restype, fn.argtypes = i32, args
+        for name, args in (("ss_tree_attn_workspace", [kv_p, batch_p, i32, i32, i32]), ("ss_tree_verify_workspace", [i32] * 3),
+                           ("ss_block_fork_workspace", [i32] * 2), ("ss_block_release_workspace", [i32] * 2), ("ss_block_compact_workspace", [i32])):
+            fn = getattr(L, name)
+            fn.restype, fn.argtypes = size, args
         L.ss_kv_commit.argtypes = [ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
         L.ss_depth_init.restype = ctypes.c_int32
         L.ss_depth_init.argtypes = [ctypes.POINTER(ss_depth_state)]
@@ -402,6 +417,148 @@ def alloc_chunk_outputs(d: Dict[str, object], device="cuda:0", max_q_len: int = 
     out = torch.empty(shape, dtype=torch.float32 if d["q_dtype"] == "f32" else torch.int16, device=device)
     lse = torch.empty(shape[:2], dtype=torch.float32, device=device)
     return out, lse, torch.empty(ss_chunk_attn_workspace(d, max_q_len), dtype=torch.uint8, device=device)
+
+
+# --------------------------------------------------------------------------------------------
+# draft trees of any width, blocks that several requests hold
+# --------------------------------------------------------------------------------------------
+def ss_tree_attn_workspace(d: Dict[str, object], max_q_len: int = 0) -> int:
+    kv, bt = _cache_descriptor(d), _batch_descriptor(d, max_q_len)
+    n = lib().ss_tree_attn_workspace(ctypes.byref(kv), ctypes.byref(bt), _DT[d["q_dtype"]], d["num_q_heads"], d["total_rows"])
+    if n == 0:
+        raise SpecVerifyError(lib().ss_last_error().decode())
+    return int(n)
+
+
+def _mask_rows(d: Dict[str, object]):
+    """Address and words to a row of `node_mask`, [rows][words] of 32 bits."""
+    m, rows = d["node_mask"], d["total_rows"]
+    if m.element_size() != 4 or m.is_floating_point() or not m.is_contiguous() or not m.is_cuda or rows == 0 or m.numel() % rows or m.numel() == 0:
+        raise SpecVerifyError(f"node_mask must be a dense tensor of {rows} rows of 32-bit words on the GPU, got {m.dtype}, shape {tuple(m.shape)}, strides {m.stride()} on {m.device}")
+    return m.data_ptr(), m.numel() // rows
+
+
+def ss_tree_attn(d: Dict[str, object], out: torch.Tensor, lse: Optional[torch.Tensor], workspace: torch.Tensor, max_q_len: int = 0) -> None:
+    """Enqueue attention of the nodes of a device batch's draft trees, which of them a row attends in `node_mask` (dense, total_rows rows of words); `q`
+    [rows][heads][head_dim] may have its rows apart, `out` and `lse` are dense."""
+    rows, heads, dim, kind = d["total_rows"], d["num_q_heads"], d["head_dim"], d["q_dtype"]
+    if d["batch"] == 0 or rows == 0:
+        return
+    kv, bt = _cache_descriptor(d), _batch_descriptor(d, max_q_len)
+    _check(lib().ss_tree_attn(ctypes.byref(kv), ctypes.byref(bt), *_mask_rows(d), *_rows("q", d["q"], kind, rows, heads, dim), _DT[kind], heads, rows,
+                              d["sm_scale"], _dense("out", out, _SIZE[kind], rows * heads * dim), 0 if lse is None else _dense("lse", lse, 4, rows * heads),
+                              workspace.data_ptr(), workspace.nbytes, _stream()))
+
+
+def alloc_tree_outputs(d: Dict[str, object], device="cuda:0", max_q_len: int = 0):
+    """Allocate (out, lse, workspace) for a device batch's draft trees.  `out` holds raw storage (int16 = bf16 bits)."""
+    _check_batch(d)
+    _check_cache(d)
+    shape = (d["total_rows"], d["num_q_heads"], d["head_dim"])
+    out = torch.empty(shape, dtype=torch.float32 if d["q_dtype"] == "f32" else torch.int16, device=device)
+    lse = torch.empty(shape[:2], dtype=torch.float32, device=device)
+    return out, lse, torch.empty(ss_tree_attn_workspace(d, max_q_len), dtype=torch.uint8, device=device)
+
+
+def _logits(d: Dict[str, object]) -> int:
+    """The address of the target's logits, rows of `row_stride` elements of which the last may end behind its vocabulary."""
+    t, rows = d["target_logits"], d["total_rows"]
+    if t.element_size() != _SIZE[d["logit_dtype"]] or not t.is_contiguous() or not t.is_cuda or t.numel() < (rows - 1) * d["row_stride"] + d["vocab"] * (rows > 0):
+        raise SpecVerifyError(f"target_logits must be a dense tensor of {rows} rows, {d['row_stride']} elements apart, of type {d['logit_dtype']} (or its bits) on the "
+                              f"GPU, got {t.dtype}, shape {tuple(t.shape)}, strides {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
+def ss_tree_verify(d: Dict[str, object], accepted_len: torch.Tensor, out_tokens: torch.Tensor, accepted_nodes: torch.Tensor,
+                   logprobs: Optional[torch.Tensor], workspace: torch.Tensor, max_depth: int = 0) -> None:
+    """Enqueue the walk through a device batch's draft trees by the target's own draws.  `tree_parent`, `node_tokens` (int32) and `uniforms` (float32) have an
+    entry for each row, `temperature` is a tensor (float32) with one for each request or None, where `temperature_scalar` holds for all."""
+    B, rows = d["batch"], d["total_rows"]
+    u, temp = d["uniforms"], d["temperature"]
+    _check(lib().ss_tree_verify(B, d["vocab"], d["row_stride"], _DT[d["logit_dtype"]], rows, max_depth, _ints("q_indptr", d["q_indptr"], B + 1),
+                                _ints("tree_parent", d["tree_parent"], rows), _ints("node_tokens", d["node_tokens"], rows), _logits(d),
+                                0 if u is None else _dense("uniforms", u, 4, rows), 0 if temp is None else _dense("temperature", temp, 4, B),
+                                0.0 if temp is not None else float(d["temperature_scalar"]), _ints("accepted_len", accepted_len, B),
+                                _ints("out_tokens", out_tokens, B * SS_OUT_WIDTH), _ints("accepted_nodes", accepted_nodes, B * SS_MAX_DEPTH),
+                                0 if logprobs is None else _dense("logprobs", logprobs, 4, B * SS_OUT_WIDTH), workspace.data_ptr(), workspace.nbytes, _stream()))
+
+
+def alloc_tree_verify_outputs(d: Dict[str, object], device="cuda:0"):
+    """Allocate (accepted_len, out_tokens, accepted_nodes, logprobs, workspace)."""
+    B = d["batch"]
+    n = lib().ss_tree_verify_workspace(B, d["total_rows"], d["vocab"])
+    if n == 0:
+        raise SpecVerifyError(lib().ss_last_error().decode())
+    ints = [torch.empty(shape, dtype=torch.int32, device=device) for shape in ((B,), (B, SS_OUT_WIDTH), (B, SS_MAX_DEPTH))]
+    return (*ints, torch.empty((B, SS_OUT_WIDTH), dtype=torch.float32, device=device), torch.empty(int(n), dtype=torch.uint8, device=device))
+
+
+def _books(d: Dict[str, object]):
+    """Descriptors of a batch's table and of its cache's free blocks, looked at each time: these calls write where they point."""
+    B, W, N = d["batch"], d["max_blocks_per_seq"], d["num_blocks"]
+    kv_len = d.get("kv_len")
+    bt = ss_batch(B, W, 0, 0, _ints("block_table", d["block_table"], B * W), 0 if kv_len is None else _ints("kv_len", kv_len, B), 0, 0)
+    return bt, ss_block_pool(N, _ints("free_ids", d["free_ids"], N), _ints("free_count", d["free_count"], 1))
+
+
+def ss_block_fork(d: Dict[str, object], parent: torch.Tensor, child: torch.Tensor, length: Optional[torch.Tensor], copy_src: torch.Tensor,
+                  copy_dst: torch.Tensor, status: torch.Tensor, workspace: torch.Tensor) -> None:
+    """Enqueue the forks parent[i] -> child[i] (int32) of the first length[i] tokens (None: all): `block_table`, `kv_len`, `held`, `shares` and `free_count` in
+    place, and the blocks that ss_block_copy is to copy."""
+    bt, pool = _books(d)
+    n = parent.numel()
+    _check(lib().ss_block_fork(ctypes.byref(bt), ctypes.byref(pool), _ints("shares", d["shares"], d["num_blocks"]), _ints("held", d["held"], d["batch"]), n,
+                               _ints("parent", parent, n), _ints("child", child, n), 0 if length is None else _ints("length", length, n),
+                               _ints("copy_src", copy_src, n), _ints("copy_dst", copy_dst, n), _ints("status", status, 1), workspace.data_ptr(),
+                               workspace.nbytes, _stream()))
+
+
+def ss_block_release(d: Dict[str, object], status: torch.Tensor, workspace: torch.Tensor) -> None:
+    """Enqueue the return of what requests hold beyond their `kv_len`: `held`, `shares`, `free_ids` and `free_count` in place."""
+    bt, pool = _books(d)
+    _check(lib().ss_block_release(ctypes.byref(bt), ctypes.byref(pool), _ints("shares", d["shares"], d["num_blocks"]), _ints("held", d["held"], d["batch"]),
+                                  _ints("status", status, 1), workspace.data_ptr(), workspace.nbytes, _stream()))
+
+
+def ss_block_compact(d: Dict[str, object], remap: Optional[torch.Tensor], copy_src: torch.Tensor, copy_dst: torch.Tensor, num_copies: torch.Tensor,
+                     status: torch.Tensor, workspace: torch.Tensor) -> None:
+    """Enqueue the renumbering of the blocks in use to the front of the cache (`block_table`, `shares` and `free_ids` in place), and what ss_block_copy is to copy."""
+    bt, pool = _books(d)
+    N, shares = d["num_blocks"], d["shares"]
+    _check(lib().ss_block_compact(ctypes.byref(bt), ctypes.byref(pool), 0 if shares is None else _ints("shares", shares, N), _ints("held", d["held"], d["batch"]),
+                                  0 if remap is None else _ints("remap", remap, N), _ints("copy_src", copy_src, N // 2), _ints("copy_dst", copy_dst, N // 2),
+                                  _ints("num_copies", num_copies, 1), _ints("status", status, 1), workspace.data_ptr(), workspace.nbytes, _stream()))
+
+
+def alloc_block_share_workspace(d: Dict[str, object], device="cuda:0", num_forks: int = 0) -> torch.Tensor:
+    """A workspace that ss_block_fork (of up to num_forks), ss_block_release and ss_block_compact can take in turn."""
+    sizes = (lib().ss_block_fork_workspace(d["batch"], num_forks), lib().ss_block_release_workspace(d["batch"], d["max_blocks_per_seq"]),
+             lib().ss_block_compact_workspace(d["num_blocks"]))
+    if 0 in sizes:
+        raise SpecVerifyError(lib().ss_last_error().decode())
+    return torch.empty(max(sizes), dtype=torch.uint8, device=device)
+
+
+class CacheLayers:
+    """The descriptors of all layers of a cache, for ss_block_copy; holds the tensors."""
+
+    def __init__(self, layers):
+        for d in layers:
+            _check_cache(d)
+        self.layers, self.num = list(layers), len(layers)
+        self.descriptors = (ss_paged_kv * max(self.num, 1))(*map(_cache_descriptor, layers))
+
+
+def cache_layers(layers) -> CacheLayers:
+    """A handle of a cache's layers, dicts as ss_kv_write takes them."""
+    return CacheLayers(layers)
+
+
+def ss_block_copy(layers: CacheLayers, copy_src: torch.Tensor, copy_dst: torch.Tensor, num_copies: Optional[torch.Tensor] = None) -> None:
+    """Enqueue the copy of blocks copy_src[i] to copy_dst[i] (int32; negative: none) in all layers; num_copies (int32) bounds the pairs on the device."""
+    n = copy_src.numel()
+    _check(lib().ss_block_copy(layers.descriptors, layers.num, _ints("copy_src", copy_src, n), _ints("copy_dst", copy_dst, n), n,
+                               0 if num_copies is None else _ints("num_copies", num_copies, 1), _stream()))
 
 
 def ss_kv_append(d: Dict[str, object], max_q_len: int = 0) -> None:

@@ -389,7 +389,8 @@ int32_t ss_spec_accept(int32_t batch, int32_t vocab, int64_t row_stride, int32_t
 }
 
 // Host-visible checks shared by the calls that write the cache; *empty is set for a batch of zero requests.
-static int32_t check_kv_write(const ss_paged_kv *kv, const ss_batch *batch, int32_t total_rows, bool *empty)
+// most: new tokens a request may bring, 0 for any number
+static int32_t check_kv_write(const ss_paged_kv *kv, const ss_batch *batch, int32_t total_rows, int32_t most, bool *empty)
 {
     *empty = false;
     if (!kv || !batch) return fail(SS_ERR_INVALID_ARG, "kv and batch descriptors must not be NULL");
@@ -399,16 +400,16 @@ static int32_t check_kv_write(const ss_paged_kv *kv, const ss_batch *batch, int3
         return fail(SS_ERR_INVALID_ARG, "head_dim must be 64 or 128, got %d", kv->head_dim);
     if (kv->num_kv_heads <= 0 || kv->num_blocks < 0) return fail(SS_ERR_INVALID_ARG, "bad num_kv_heads or num_blocks");
     if (kv->dtype < SS_F32 || kv->dtype > SS_FP8_E4M3) return fail(SS_ERR_INVALID_ARG, "unknown KV dtype %d", kv->dtype);
-    if (batch->batch < 0 || total_rows < batch->batch || (int64_t)total_rows > (int64_t)batch->batch * SS_OUT_WIDTH)
-        return fail(SS_ERR_INVALID_ARG, "total_rows (%d) must lie in [batch, %d*batch] for batch %d", total_rows,
-                    SS_OUT_WIDTH, batch->batch);
+    if (batch->batch < 0 || total_rows < 0) return fail(SS_ERR_INVALID_ARG, "negative batch or total_rows");
+    if (most > 0 && (total_rows < batch->batch || (int64_t)total_rows > (int64_t)batch->batch * most))
+        return fail(SS_ERR_INVALID_ARG, "total_rows (%d) must lie in [batch, %d*batch] for batch %d", total_rows, most, batch->batch);
     if (batch->batch == 0) {
         *empty = true;
         return SS_OK;
     }
     if (batch->max_blocks_per_seq <= 0) return fail(SS_ERR_INVALID_ARG, "max_blocks_per_seq must be positive");
-    if (batch->max_q_len < 0 || batch->max_q_len > SS_OUT_WIDTH)
-        return fail(SS_ERR_INVALID_ARG, "max_q_len must be 0 (unknown) or in [1, %d]", SS_OUT_WIDTH);
+    if (batch->max_q_len < 0 || (most > 0 && batch->max_q_len > most))
+        return fail(SS_ERR_INVALID_ARG, "max_q_len must be 0 (unknown) or in [1, %d]", most);
     if ((int64_t)batch->batch * SS_OUT_WIDTH * kv->num_kv_heads > 0x7fffffffll)
         return fail(SS_ERR_UNSUPPORTED, "batch * kv heads too large for one launch");
     if (!kv->k || !kv->v || !batch->block_table || !batch->kv_len || !batch->q_indptr)
@@ -434,7 +435,7 @@ int32_t ss_kv_append(const ss_paged_kv *kv, const ss_batch *batch, const void *k
                      int32_t new_dtype, int32_t total_rows, void *stream)
 {
     bool empty;
-    const int32_t rc0 = check_kv_write(kv, batch, total_rows, &empty);
+    const int32_t rc0 = check_kv_write(kv, batch, total_rows, SS_OUT_WIDTH, &empty);
     if (rc0 != SS_OK || empty) return rc0;
     if (new_dtype != SS_F32 && new_dtype != SS_BF16) return fail(SS_ERR_INVALID_ARG, "new_dtype must be SS_F32 or SS_BF16");
     if (!k_new || !v_new) return fail(SS_ERR_INVALID_ARG, "a required device pointer is NULL");
@@ -453,13 +454,12 @@ int32_t ss_kv_compact(const ss_paged_kv *kv, const ss_batch *batch, const int32_
                       const int32_t *accepted_len, int32_t total_rows, void *stream)
 {
     bool empty;
-    const int32_t rc0 = check_kv_write(kv, batch, total_rows, &empty);
+    const int32_t rc0 = check_kv_write(kv, batch, total_rows, 0, &empty);
     if (rc0 != SS_OK || empty) return rc0;
     if (!accepted_nodes || !accepted_len) return fail(SS_ERR_INVALID_ARG, "a required device pointer is NULL");
     if (g_validate) {
-        const int32_t rc = validate_batch(batch->block_table, batch->kv_len, batch->q_indptr, nullptr, batch->batch,
-                                          batch->max_blocks_per_seq, kv->num_blocks, total_rows, batch->max_q_len,
-                                          static_cast<hipStream_t>(stream), "ss_kv_compact");
+        const int32_t rc = validate_chunk(batch->block_table, batch->kv_len, batch->q_indptr, batch->batch, batch->max_blocks_per_seq, kv->num_blocks,
+                                          total_rows, batch->max_q_len ? batch->max_q_len : total_rows, static_cast<hipStream_t>(stream), "ss_kv_compact");
         if (rc != SS_OK) return rc;
     }
     return kv_compact_launch(kv_write_args(kv, batch), accepted_nodes, accepted_len, static_cast<hipStream_t>(stream));

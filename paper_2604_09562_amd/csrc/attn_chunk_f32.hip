@@ -1,4 +1,5 @@
-// Attention of a chunk of new tokens in fp32 throughout: the path for fp32 queries or caches (the bf16 matrix-core kernel takes the others).
+// Attention of a chunk of new tokens, or of the nodes of a draft tree, in fp32 throughout: the path for fp32 queries or caches (the bf16 matrix-core kernels take the
+// others).
 //
 // A workgroup takes a share (chunk_plan.h) of 64 query rows of a KV head, 16 to a wavefront.  A step brings 64 keys and values into LDS as fp32; a
 // wavefront computes
@@ -35,7 +36,7 @@ __device__ __forceinline__ float4v load4(const void *base, int64_t i)
     }
 }
 
-template <int D, int KV, int QDT>
+template <int D, int KV, int QDT, bool TREE>
 __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
 {
     constexpr int PAD = D + 4, PIECES = kStepKeys * D / 4 / (64 * kWaves);   // fours of a step's keys to a thread
@@ -43,7 +44,7 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
     __shared__ float vs[kStepKeys][PAD];
     const int g = blockIdx.x % a.num_kv_heads, span = blockIdx.x / a.num_kv_heads;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    ChunkWalk<kRows, kStepKeys, kChunkOpenF32> s;
+    ChunkWalk<kRows, kStepKeys, kChunkOpenF32, TREE> s;
     int begun = 0, begun_q0 = 0, begun_rows = 0, begun_row0 = 0;
     for (bool any = s.begin(a, span); any; any = s.next(a)) {
         if (s.part == 2 * span + 1) {
@@ -76,7 +77,10 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
 
         // Steps from `full` on hold keys that some row of the tile does not see.  There a value that is not finite is taken out of the product, in
         // which it would reach every row (0 * inf), and added to the rows that see it.
-        const int full = max((s.u.kv_len - s.u.q_len + s.t * kRows / G + 1) / kStepKeys, 0);
+        const int ctx = s.u.kv_len - s.u.q_len;
+        const int full = max((TREE ? ctx : ctx + s.t * kRows / G + 1) / kStepKeys, 0);
+        const uint32_t *mask = nullptr;
+        if constexpr (TREE) mask = a.node_mask + (int64_t)(s.u.q0 + qi) * a.mask_words;
         for (int step = s.s0; step < s.s1; ++step) {
             bool odd = false;
             __syncthreads();
@@ -100,6 +104,11 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
                 *reinterpret_cast<float4v *>(&vs[t][d]) = v;
             }
             const int any_odd = __syncthreads_or(odd);
+            uint32_t window[2] = {~0u, ~0u};   // TREE: which of the step's keys this lane's row attends
+            if constexpr (TREE)
+                if (step >= full)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) window[h] = tree_window(mask, a.mask_words, s.u.q_len, step * kStepKeys + h * 32 - ctx);
             float4v x[4];
             float top = kChunkNoMax;
 #pragma unroll
@@ -113,7 +122,7 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if (step * kStepKeys + tb * 16 + jq * 4 + i > lim) acc[i] = -__builtin_inff();
+                    if (TREE ? !(window[tb / 2] >> (tb % 2 * 16 + jq * 4 + i) & 1) : step * kStepKeys + tb * 16 + jq * 4 + i > lim) acc[i] = -__builtin_inff();
                     top = fmaxf(top, acc[i]);
                 }
                 x[tb] = acc;
@@ -143,7 +152,9 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
                     for (int i = 0; i < 4; ++i)
                         o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vs[tb * 16 + jq * 4 + i][16 * c + n16], x[tb][i], o[c], 0, 0, 0);
             if (any_odd) {
-                for (int pos = step * kStepKeys; pos < min((step + 1) * kStepKeys, lim + 1); ++pos) {
+                for (int pos = step * kStepKeys; pos < min((step + 1) * kStepKeys, TREE ? s.u.kv_len : lim + 1); ++pos) {
+                    if constexpr (TREE)
+                        if (!((pos % kStepKeys < 32 ? window[0] : window[1]) >> (pos % 32) & 1)) continue;
                     const int64_t tile = (int64_t)chunk_block(a, table[pos / kTile]) * a.num_kv_heads + g, from = (tile * kTile + pos % kTile) * D + 4 * jq;
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) {
@@ -183,30 +194,34 @@ __global__ __launch_bounds__(64 * kWaves) void chunk_f32_kernel(ChunkArgs a)
     chunk_record(a, span, g, begun, begun_q0, begun_rows, begun_row0);
 }
 
-template <int D, int KV, int QDT>
+template <int D, int KV, int QDT, bool TREE>
 int32_t launch(const ChunkArgs &a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((chunk_f32_kernel<D, KV, QDT>), dim3((unsigned)(a.spans * a.num_kv_heads)), dim3(64 * kWaves), 0, stream, a);
+    hipLaunchKernelGGL((chunk_f32_kernel<D, KV, QDT, TREE>), dim3((unsigned)(a.spans * a.num_kv_heads)), dim3(64 * kWaves), 0, stream, a);
     SS_HIP_CHECK(hipGetLastError(), "launch chunk_f32_kernel");
     return chunk_merge_launch<kRows, 16, D, QDT>(a, stream);
 }
 
-template <int D, int QDT>
+template <int D, int QDT, bool TREE>
 int32_t launch_kv(const ChunkArgs &a, hipStream_t stream)
 {
     switch (a.kv_dtype) {
-    case SS_F32: return launch<D, SS_F32, QDT>(a, stream);
-    case SS_BF16: return launch<D, SS_BF16, QDT>(a, stream);
-    default: return launch<D, SS_FP8_E4M3, QDT>(a, stream);
+    case SS_F32: return launch<D, SS_F32, QDT, TREE>(a, stream);
+    case SS_BF16: return launch<D, SS_BF16, QDT, TREE>(a, stream);
+    default: return launch<D, SS_FP8_E4M3, QDT, TREE>(a, stream);
     }
+}
+
+template <bool TREE>
+int32_t launch_all(const ChunkArgs &a, hipStream_t stream)
+{
+    if (a.head_dim == 128) return a.q_dtype == SS_F32 ? launch_kv<128, SS_F32, TREE>(a, stream) : launch_kv<128, SS_BF16, TREE>(a, stream);
+    return a.q_dtype == SS_F32 ? launch_kv<64, SS_F32, TREE>(a, stream) : launch_kv<64, SS_BF16, TREE>(a, stream);
 }
 
 }  // namespace
 
-int32_t chunk_f32_launch(const ChunkArgs &a, hipStream_t stream)
-{
-    if (a.head_dim == 128) return a.q_dtype == SS_F32 ? launch_kv<128, SS_F32>(a, stream) : launch_kv<128, SS_BF16>(a, stream);
-    return a.q_dtype == SS_F32 ? launch_kv<64, SS_F32>(a, stream) : launch_kv<64, SS_BF16>(a, stream);
-}
+int32_t chunk_f32_launch(const ChunkArgs &a, hipStream_t stream) { return launch_all<false>(a, stream); }
+int32_t tree_f32_launch(const ChunkArgs &a, hipStream_t stream) { return launch_all<true>(a, stream); }
 
 }  // namespace ss

@@ -1,0 +1,50 @@
+// Copies of cache blocks, keys, values and scales as they are, for all layers of a cache in one launch: bound by memory, read once and written once.
+#include "block_share.h"
+
+namespace ss {
+namespace {
+
+constexpr int kThreads = 256, kEach = 4;               // 16-byte loads of a lane that are under way together
+constexpr int kPiece = kThreads * kEach * 16;          // bytes of a block's keys or values that a workgroup copies at a time
+constexpr int kWgs = 2048;                             // eight workgroups to a compute unit
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__global__ __launch_bounds__(kThreads) void block_copy_kernel(BlockCopyArgs a)
+{
+    const int tid = threadIdx.x;
+    const int n = a.num_copies ? min(max(a.num_copies[0], 0), a.max_copies) : a.max_copies;
+    const int pieces = (int)((a.block_bytes + kPiece - 1) / kPiece), per = a.layers * 2 * pieces;
+    for (int64_t it = blockIdx.x; it < (int64_t)n * per; it += gridDim.x) {
+        const int pair = (int)(it / per), k = (int)(it % per);
+        const int piece = k % pieces, side = k / pieces % 2, layer = k / pieces / 2;
+        const int src = a.src[pair], dst = a.dst[pair];
+        if ((unsigned)src >= (unsigned)a.num_blocks || (unsigned)dst >= (unsigned)a.num_blocks || src == dst) continue;
+        char *cache = a.layer[layer].side[side];
+        const int64_t at = (int64_t)piece * kPiece + tid * 16;
+        const char *from = cache + (int64_t)src * a.block_bytes + at;
+        char *to = cache + (int64_t)dst * a.block_bytes + at;
+        u32x4 w[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (at + i * kThreads * 16 < a.block_bytes) w[i] = *reinterpret_cast<const u32x4 *>(from + i * kThreads * 16);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (at + i * kThreads * 16 < a.block_bytes) *reinterpret_cast<u32x4 *>(to + i * kThreads * 16) = w[i];
+        float *scale = a.layer[layer].scale[side];
+        if (scale && piece == 0)
+            for (int h = tid; h < a.heads; h += kThreads) scale[(int64_t)dst * a.heads + h] = scale[(int64_t)src * a.heads + h];
+    }
+}
+
+}  // namespace
+
+int32_t block_copy_launch(const BlockCopyArgs &a, hipStream_t stream)
+{
+    const int64_t items = (int64_t)a.max_copies * a.layers * 2 * ((a.block_bytes + kPiece - 1) / kPiece);
+    hipLaunchKernelGGL(block_copy_kernel, dim3((unsigned)(items < kWgs ? items : kWgs)), dim3(kThreads), 0, stream, a);
+    SS_HIP_CHECK(hipGetLastError(), "launch block_copy_kernel");
+    return SS_OK;
+}
+
+}  // namespace ss

@@ -1,0 +1,521 @@
+// Blocks that several requests hold: forks, releases, and the move of all blocks in use to the front of a cache.
+//
+// shares[x] counts a block's holders beyond the first.  All three calls are whole numbers in orders that their definitions fix, so the result does not
+// depend on which thread comes first: additions to shares commute, and where an order counts (which block is taken, where one comes to
+// stand in the free list) it is a prefix sum.  Bound by latency: chains of lengths, sums, ids and counts, about 1 us each.
+#include "block_share.h"
+
+namespace ss {
+namespace {
+
+constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kNone = 0x7fffffff;
+
+__device__ __forceinline__ int blocks_of(int len) { return (int)(((unsigned)len + kTile - 1) / kTile); }
+
+// Inclusive sum over the workgroup of `threads` threads; total: of all of them.
+template <int THREADS>
+__device__ __forceinline__ int group_scan(int x, int *part, int &total)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    if (lane == 63) part[wave] = x;
+    __syncthreads();
+    int add = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        add += w < wave ? part[w] : 0;
+        total += part[w];
+    }
+    __syncthreads();
+    return x + add;
+}
+// What other threads of this kernel have changed by atomics (a plain load may find it in the first cache as it was).
+__device__ __forceinline__ int current(const int32_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// ---- forks -------------------------------------------------------------------------------------------------------------
+struct ForkLds {
+    int part[kWaves];
+    int bad;
+};
+
+// One workgroup: whether all forks can be, and what of each is one number; 0 if it was done.
+__device__ int fork_books(const BlockForkArgs &a, ForkLds &lds)
+{
+    const int tid = threadIdx.x;
+    int32_t *rank = a.scratch, *named = rank + a.num_forks;   // blocks taken by the forks in front; the first fork that names a row as its child
+    for (int b = tid; b < a.batch; b += kThreads) named[b] = kNone;
+    if (tid == 0) lds.bad = kNone;
+    const int count = a.free_count[0];
+    __threadfence_block();
+    __syncthreads();
+    for (int i = tid; i < a.num_forks; i += kThreads) {
+        const int c = a.child[i];
+        if (a.parent[i] >= 0 && (unsigned)c < (unsigned)a.batch) atomicMin(&named[c], i);
+    }
+    __threadfence_block();
+    __syncthreads();
+    int taken = 0;
+    for (int lo = 0; lo < a.num_forks; lo += kThreads) {
+        const int i = lo + tid;
+        int part = 0;
+        if (i < a.num_forks && a.parent[i] >= 0) {
+            const int p = a.parent[i], c = a.child[i];
+            bool ok = p < a.batch && (unsigned)c < (unsigned)a.batch;
+            if (ok) {
+                const int n = a.kv_len[p], h = a.held[p], len = a.length ? a.length[i] : n;
+                ok = current(&named[c]) == i && current(&named[p]) == kNone && a.held[c] == 0 && n >= 0 && len >= 0 && len <= n && h >= 0 &&
+                     blocks_of(len) <= min(h, a.max_blocks);
+                part = ok && len % kTile != 0;
+            }
+            if (!ok) atomicMin(&lds.bad, i);
+        }
+        int total;
+        const int incl = group_scan<kThreads>(part, lds.part, total);
+        if (i < a.num_forks) rank[i] = taken + incl - part;
+        taken += total;
+    }
+    __syncthreads();
+    int status = 0;
+    if (lds.bad != kNone) status = -1 - lds.bad;
+    else if (count < 0 || count > a.num_blocks) status = -1 - a.num_forks;
+    else if (taken > count) status = taken - count;
+    // (every thread has read what it needs of the parents; the rows written here are children, which no fork has as its parent)
+    for (int i = tid; i < a.num_forks; i += kThreads) {
+        int src = -1, dst = -1;
+        const int p = a.parent[i];
+        if (status == 0 && p >= 0) {
+            const int c = a.child[i], len = a.length ? a.length[i] : a.kv_len[p], whole = len / kTile;
+            if (len % kTile) {
+                src = a.block_table[(int64_t)p * a.max_blocks + whole];
+                dst = a.free_ids[count - 1 - rank[i]];
+                a.block_table[(int64_t)c * a.max_blocks + whole] = dst;
+            }
+            a.held[c] = blocks_of(len);
+            a.kv_len[c] = len;
+        }
+        a.copy_src[i] = src;
+        a.copy_dst[i] = dst;
+    }
+    if (tid == 0) {
+        a.status[0] = status;
+        if (status == 0) a.free_count[0] = count - taken;
+    }
+    return status;
+}
+
+__device__ __forceinline__ void share_entry(const BlockForkArgs &a, int p, int c, int j)
+{
+    const int x = a.block_table[(int64_t)p * a.max_blocks + j];
+    a.block_table[(int64_t)c * a.max_blocks + j] = x;
+    if ((unsigned)x < (unsigned)a.num_blocks) atomicAdd(&a.shares[x], 1);
+}
+
+__global__ __launch_bounds__(kThreads) void block_fork_kernel(BlockForkArgs a, int whole_call)
+{
+    __shared__ ForkLds lds;
+    if (fork_books(a, lds) != 0 || !whole_call) return;
+    __threadfence_block();
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.num_forks * a.max_blocks; e += kThreads) {
+        const int i = e / a.max_blocks, j = e % a.max_blocks, p = a.parent[i];
+        if (p < 0) continue;
+        const int len = a.length ? a.length[i] : a.kv_len[p];
+        if (j < len / kTile) share_entry(a, p, a.child[i], j);
+    }
+}
+
+constexpr int kForkThreads = 256, kForkEach = 4;   // entries of a table's row to a thread
+
+__global__ __launch_bounds__(kForkThreads) void block_fork_rows_kernel(BlockForkArgs a)
+{
+    const int i = blockIdx.x, p = a.parent[i];
+    if (a.status[0] != 0 || p < 0) return;
+    const int whole = (a.length ? a.length[i] : a.kv_len[p]) / kTile, c = a.child[i];
+    for (int lo = blockIdx.y * kForkThreads * kForkEach + threadIdx.x; lo < whole; lo += gridDim.y * kForkThreads * kForkEach)
+#pragma unroll
+        for (int k = 0; k < kForkEach; ++k)
+            if (lo + k * kForkThreads < whole) share_entry(a, p, c, lo + k * kForkThreads);
+}
+
+// ---- releases ----------------------------------------------------------------------------------------------------------
+// Release r (they are counted in the order of request, logical block) takes one from its block's shares.  What is below zero then has no holder left, and its releases
+// leave there the last one's number; that release puts the block on the list, behind those of lower number.
+constexpr int kReleaseHead = 4;       // scratch: length of the free list, releases, status; then the releases in front of each request, then freed blocks by pieces
+constexpr int kReleasePiece = 1024;   // releases whose freed blocks are counted together
+constexpr int kReleaseLds = 1024;     // requests whose sums a workgroup keeps in LDS
+constexpr int kReleaseThreads = 256;
+
+__device__ __forceinline__ int claim_of(int r) { return INT32_MIN + (int)(kMaxReleased - 1 - r); }   // the lower the later; far below any count
+
+struct Releases {
+    const BlockReleaseArgs &a;
+    const int32_t *given;             // [batch + 1]
+    // the block of release r, -1 if it is none
+    __device__ int id(int r) const
+    {
+        int lo = 0, hi = a.batch;     // the last request with given[lo] <= r
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (given[mid] <= r) lo = mid; else hi = mid;
+        }
+        const int x = a.block_table[(int64_t)lo * a.max_blocks + blocks_of(a.kv_len[lo]) + r - given[lo]];
+        return (unsigned)x < (unsigned)a.num_blocks ? x : -1;
+    }
+    __device__ void give(int r) const
+    {
+        const int x = id(r);
+        if (x >= 0) atomicSub(&a.shares[x], 1);
+    }
+    __device__ void claim(int r) const
+    {
+        const int x = id(r);
+        if (x >= 0 && current(&a.shares[x]) < 0) atomicMin(&a.shares[x], claim_of(r));
+    }
+    // the block that release r puts on the list, or -1
+    __device__ int freed(int r) const
+    {
+        const int x = id(r);
+        return x >= 0 && current(&a.shares[x]) == claim_of(r) ? x : -1;
+    }
+};
+
+struct ReleaseLds {
+    int part[kWaves];
+    int bad;
+};
+
+// One workgroup: the sums of all requests, and what they hold; false if something does not fit.
+__device__ bool release_sums(const BlockReleaseArgs &a, ReleaseLds &lds, int32_t *given, int &count, int &releases)
+{
+    const int tid = threadIdx.x;
+    if (tid == 0) lds.bad = kNone;
+    count = a.free_count[0];
+    __syncthreads();
+    releases = 0;
+    for (int lo = 0; lo < a.batch; lo += kThreads) {
+        const int b = lo + tid;
+        int g = 0;
+        if (b < a.batch) {
+            const int n = a.kv_len[b], h = a.held[b];
+            if (n < 0 || h < 0 || h > a.max_blocks) atomicMin(&lds.bad, b);
+            else g = max(h - blocks_of(n), 0);
+        }
+        int total;
+        const int incl = group_scan<kThreads>(g, lds.part, total);
+        if (b < a.batch) given[b] = releases + incl - g;
+        releases += total;
+    }
+    __syncthreads();
+    int status = 0;
+    if (lds.bad != kNone) status = -1 - lds.bad;
+    else if (count < 0 || count > a.num_blocks) status = -1 - a.batch;
+    if (tid == 0) {
+        given[a.batch] = releases;
+        a.status[0] = status;
+    }
+    if (status == 0)
+        for (int b = tid; b < a.batch; b += kThreads) a.held[b] = min(a.held[b], blocks_of(a.kv_len[b]));
+    return status == 0;
+}
+
+__global__ __launch_bounds__(kThreads) void block_release_kernel(BlockReleaseArgs a)
+{
+    __shared__ ReleaseLds lds;
+    int32_t *given = a.scratch + kReleaseHead;
+    int count, releases;
+    if (!release_sums(a, lds, given, count, releases)) return;
+    __threadfence_block();
+    __syncthreads();
+    const Releases s = {a, given};
+    for (int r = threadIdx.x; r < releases; r += kThreads) s.give(r);
+    __threadfence_block();
+    __syncthreads();
+    for (int r = threadIdx.x; r < releases; r += kThreads) s.claim(r);
+    __threadfence_block();
+    __syncthreads();
+    int at = count;
+    for (int lo = 0; lo < releases; lo += kThreads) {
+        const int r = lo + threadIdx.x, x = r < releases ? s.freed(r) : -1;
+        int total;
+        const int place = at + group_scan<kThreads>(x >= 0, lds.part, total) - 1;
+        if (x >= 0) {
+            if (place < a.num_blocks) a.free_ids[place] = x;
+            a.shares[x] = 0;    // (no other release's claim, either)
+        }
+        at += total;
+    }
+    if (threadIdx.x == 0) a.free_count[0] = min(at, a.num_blocks);
+}
+
+__global__ __launch_bounds__(kThreads) void block_release_sum_kernel(BlockReleaseArgs a)
+{
+    __shared__ ReleaseLds lds;
+    int count, releases;
+    const bool ok = release_sums(a, lds, a.scratch + kReleaseHead, count, releases);
+    if (threadIdx.x == 0) {
+        a.scratch[0] = count;
+        a.scratch[1] = ok ? releases : 0;
+        a.scratch[2] = !ok;
+    }
+}
+
+enum { kGive, kClaim, kCount, kPlace };
+
+template <int PHASE>
+__global__ __launch_bounds__(kReleaseThreads) void block_release_phase_kernel(BlockReleaseArgs a)
+{
+    constexpr int EACH = kReleasePiece / kReleaseThreads;
+    __shared__ int32_t sums[kReleaseLds + 1];
+    __shared__ int part[kReleaseThreads / 64];
+    const int tid = threadIdx.x, count = a.scratch[0], releases = a.scratch[1];
+    int32_t *given = a.scratch + kReleaseHead, *freed_in = given + a.batch + 1;
+    if (a.batch <= kReleaseLds) {
+        for (int b = tid; b <= a.batch; b += kReleaseThreads) sums[b] = given[b];
+        __syncthreads();
+    }
+    const Releases s = {a, a.batch <= kReleaseLds ? sums : given};
+    const int pieces = (releases + kReleasePiece - 1) / kReleasePiece;
+    for (int piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+        const int first = piece * kReleasePiece + tid * EACH;
+        if constexpr (PHASE == kGive || PHASE == kClaim) {
+#pragma unroll
+            for (int k = 0; k < EACH; ++k)
+                if (first + k < releases) {
+                    if (PHASE == kGive) s.give(first + k);
+                    else s.claim(first + k);
+                }
+        } else {
+            int x[EACH], mine = 0, total;
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                x[k] = first + k < releases ? s.freed(first + k) : -1;
+                mine += x[k] >= 0;
+            }
+            const int incl = group_scan<kReleaseThreads>(mine, part, total);
+            if constexpr (PHASE == kCount) {
+                if (tid == 0) freed_in[piece] = total;
+            } else {
+                int front = 0, before;
+                for (int i = tid; i < piece; i += kReleaseThreads) front += freed_in[i];
+                group_scan<kReleaseThreads>(front, part, before);
+                int place = count + before + incl - mine;
+#pragma unroll
+                for (int k = 0; k < EACH; ++k)
+                    if (x[k] >= 0) {
+                        if (place < a.num_blocks) a.free_ids[place] = x[k];
+                        a.shares[x[k]] = 0;   // (no other release's claim, either)
+                        ++place;
+                    }
+                if (piece == pieces - 1 && tid == 0) a.free_count[0] = min(count + before + total, a.num_blocks);
+            }
+        }
+    }
+}
+
+// ---- all blocks in use to the front ------------------------------------------------------------------------------------
+constexpr int kCompactHead = 4;          // scratch: status, length of the free list, moves
+constexpr int kCompactThreads = 256;
+constexpr int kBitmapWords = 15360;      // of the free blocks, up to which they are put together in LDS (491 520 blocks)
+
+struct Compact {
+    int32_t *head;
+    uint32_t *bits;                      // bit per block: free
+    int32_t *front;                      // free blocks in front of each word; one more
+    __device__ bool free(int i) const { return bits[i >> 5] >> (i & 31) & 1; }
+    __device__ int free_before(int i) const { return front[i >> 5] + __popc(bits[i >> 5] & ((1u << (i & 31)) - 1u)); }
+    // the r-th free block
+    __device__ int nth_free(int r, int words) const
+    {
+        int lo = 0, hi = words;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (front[mid] <= r) lo = mid; else hi = mid;
+        }
+        uint32_t w = bits[lo];
+        for (int k = r - front[lo]; k > 0; --k) w &= w - 1;
+        return lo * 32 + __ffs((int)w) - 1;
+    }
+};
+
+__device__ __forceinline__ int words_of(int num_blocks) { return (num_blocks + 31) / 32; }
+
+struct CompactLds {
+    int part[kWaves];
+    int bad, list;
+};
+
+// One workgroup: which blocks are free, and how many in front of each word of them.  build: where the bits are put together.
+__device__ void compact_bits(const BlockCompactArgs &a, CompactLds &lds, uint32_t *build, const Compact &s)
+{
+    const int tid = threadIdx.x, words = words_of(a.num_blocks);
+    if (tid == 0) { lds.bad = kNone; lds.list = 0; }
+    for (int w = tid; w < words; w += kThreads) build[w] = 0;
+    __threadfence_block();
+    __syncthreads();
+    const int count = a.free_count[0];
+    if (count < 0 || count > a.num_blocks) {
+        if (tid == 0) lds.list = 1;
+    } else {
+        for (int i = tid; i < count; i += kThreads) {
+            const int x = a.free_ids[i];
+            if ((unsigned)x >= (unsigned)a.num_blocks || atomicOr(&build[x >> 5], 1u << (x & 31)) >> (x & 31) & 1) lds.list = 1;
+        }
+    }
+    for (int b = tid; b < a.batch; b += kThreads)
+        if (a.held[b] < 0 || a.held[b] > a.max_blocks) atomicMin(&lds.bad, b);
+    __threadfence_block();
+    __syncthreads();
+    const int status = lds.bad != kNone ? -1 - lds.bad : lds.list ? -1 - a.batch : 0;
+    int before = 0;
+    for (int lo = 0; lo < words; lo += kThreads) {
+        const int w = lo + tid;
+        uint32_t v = 0;
+        if (w < words) v = __hip_atomic_load(&build[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const int n = __popc(v);
+        int total;
+        const int incl = group_scan<kThreads>(n, lds.part, total);
+        if (w < words) {
+            s.bits[w] = v;
+            s.front[w] = before + incl - n;
+        }
+        before += total;
+    }
+    if (tid == 0) {
+        s.front[words] = before;
+        s.head[0] = status;
+        s.head[1] = count;
+        a.status[0] = status;
+    }
+}
+
+// Everything else, shared out over `threads` threads.
+__device__ void compact_rest(const BlockCompactArgs &a, const Compact &s, int64_t first, int64_t threads)
+{
+    const int N = a.num_blocks, words = words_of(N), half = N / 2;
+    const bool ok = s.head[0] == 0;
+    const int count = s.head[1], used = ok ? N - count : N;
+    const int moves = ok && used < N ? s.free_before(used) : 0;   // free ids below `used`, as many as blocks in use from there on
+    if (first == 0) a.num_copies[0] = moves;
+    for (int64_t k = moves + first; k < half; k += threads) a.copy_src[k] = a.copy_dst[k] = -1;
+    for (int64_t i64 = first; i64 < N; i64 += threads) {
+        const int i = (int)i64;
+        int to = i;
+        if (ok) {
+            const bool is_free = s.free(i);
+            const int f = s.free_before(i);
+            if (is_free && i < used) {
+                a.copy_dst[f] = i;
+            } else if (!is_free && i >= used) {
+                const int r = i - used - (f - moves);
+                to = s.nth_free(r, words);
+                a.copy_src[r] = i;
+                if (a.shares) {
+                    a.shares[to] = a.shares[i];
+                    a.shares[i] = 0;
+                }
+            }
+            if (i < count) a.free_ids[i] = N - 1 - i;
+        }
+        if (a.remap) a.remap[i] = to;
+    }
+    if (!ok) return;
+    const int64_t entries = (int64_t)a.batch * a.max_blocks;
+    for (int64_t e = first; e < entries; e += threads) {
+        const int b = (int)(e / a.max_blocks), j = (int)(e % a.max_blocks);
+        if (j >= a.held[b]) continue;
+        const int x = a.block_table[e];
+        if (x < used || x >= N || s.free(x)) continue;
+        a.block_table[e] = s.nth_free(x - used - (s.free_before(x) - moves), words);
+    }
+}
+
+template <bool LDS, bool WHOLE>
+__global__ __launch_bounds__(kThreads) void block_compact_kernel(BlockCompactArgs a, Compact s)
+{
+    extern __shared__ uint32_t bitmap[];   // LDS: words of the bitmap
+    __shared__ CompactLds lds;
+    compact_bits(a, lds, LDS ? bitmap : s.bits, s);
+    if constexpr (WHOLE) {
+        __threadfence_block();
+        __syncthreads();
+        compact_rest(a, s, threadIdx.x, kThreads);
+    }
+}
+
+__global__ __launch_bounds__(kCompactThreads) void block_compact_rest_kernel(BlockCompactArgs a, Compact s)
+{
+    compact_rest(a, s, (int64_t)blockIdx.x * kCompactThreads + threadIdx.x, (int64_t)gridDim.x * kCompactThreads);
+}
+
+// Entries up to which one workgroup does a whole call.
+constexpr int kFewEntries = 4096;
+
+}  // namespace
+
+size_t block_fork_scratch_ints(int batch, int num_forks) { return (size_t)batch + num_forks; }
+
+int32_t block_fork_launch(const BlockForkArgs &a, hipStream_t stream)
+{
+    const bool few = (int64_t)a.num_forks * a.max_blocks <= kFewEntries;
+    hipLaunchKernelGGL(block_fork_kernel, dim3(1), dim3(kThreads), 0, stream, a, few ? 1 : 0);
+    SS_HIP_CHECK(hipGetLastError(), "launch block_fork_kernel");
+    if (few) return SS_OK;
+    constexpr int per = kForkThreads * kForkEach;
+    const int parts = (a.max_blocks + per - 1) / per;
+    hipLaunchKernelGGL(block_fork_rows_kernel, dim3((unsigned)a.num_forks, (unsigned)(parts < 64 ? parts : 64)), dim3(kForkThreads), 0, stream, a);
+    SS_HIP_CHECK(hipGetLastError(), "launch block_fork_rows_kernel");
+    return SS_OK;
+}
+
+size_t block_release_scratch_ints(int batch, int max_blocks)
+{
+    return kReleaseHead + (size_t)batch + 1 + ((size_t)batch * max_blocks + kReleasePiece - 1) / kReleasePiece;
+}
+
+int32_t block_release_launch(const BlockReleaseArgs &a, hipStream_t stream)
+{
+    const int64_t entries = (int64_t)a.batch * a.max_blocks;
+    if (entries <= kFewEntries) {
+        hipLaunchKernelGGL(block_release_kernel, dim3(1), dim3(kThreads), 0, stream, a);
+        SS_HIP_CHECK(hipGetLastError(), "launch block_release_kernel");
+        return SS_OK;
+    }
+    const int64_t pieces = (entries + kReleasePiece - 1) / kReleasePiece;
+    const dim3 grid((unsigned)(pieces < 1024 ? pieces : 1024)), wg(kReleaseThreads);
+    hipLaunchKernelGGL(block_release_sum_kernel, dim3(1), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL(block_release_phase_kernel<kGive>, grid, wg, 0, stream, a);
+    hipLaunchKernelGGL(block_release_phase_kernel<kClaim>, grid, wg, 0, stream, a);
+    hipLaunchKernelGGL(block_release_phase_kernel<kCount>, grid, wg, 0, stream, a);
+    hipLaunchKernelGGL(block_release_phase_kernel<kPlace>, grid, wg, 0, stream, a);
+    SS_HIP_CHECK(hipGetLastError(), "launch block_release kernels");
+    return SS_OK;
+}
+
+size_t block_compact_scratch_ints(int num_blocks) { return kCompactHead + 2 * (((size_t)num_blocks + 31) / 32) + 1; }
+
+int32_t block_compact_launch(const BlockCompactArgs &a, hipStream_t stream)
+{
+    const int words = (a.num_blocks + 31) / 32;
+    const Compact s = {a.scratch, reinterpret_cast<uint32_t *>(a.scratch) + kCompactHead, a.scratch + kCompactHead + words};
+    const int64_t entries = (int64_t)a.batch * a.max_blocks, most = entries > a.num_blocks ? entries : a.num_blocks;
+    const size_t lds = words <= kBitmapWords ? words * sizeof(uint32_t) : 0;
+    if (most <= kFewEntries) {
+        hipLaunchKernelGGL((block_compact_kernel<true, true>), dim3(1), dim3(kThreads), lds, stream, a, s);
+        SS_HIP_CHECK(hipGetLastError(), "launch block_compact_kernel");
+        return SS_OK;
+    }
+    if (lds) hipLaunchKernelGGL((block_compact_kernel<true, false>), dim3(1), dim3(kThreads), lds, stream, a, s);
+    else hipLaunchKernelGGL((block_compact_kernel<false, false>), dim3(1), dim3(kThreads), 0, stream, a, s);
+    const int64_t wgs = (most + kCompactThreads - 1) / kCompactThreads;
+    hipLaunchKernelGGL(block_compact_rest_kernel, dim3((unsigned)(wgs < 2048 ? wgs : 2048)), dim3(kCompactThreads), 0, stream, a, s);
+    SS_HIP_CHECK(hipGetLastError(), "launch block_compact kernels");
+    return SS_OK;
+}
+
+}  // namespace ss

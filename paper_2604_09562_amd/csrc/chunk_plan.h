@@ -40,7 +40,18 @@ __device__ __forceinline__ double lane_value(double x, int lane)
 }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-template <int ROWS, int KEYS>
+// 32 bits of a row's node mask from node n0 on: nodes below 0 are context, which every row attends, nodes from q_len on there are none.
+__device__ __forceinline__ uint32_t tree_window(const uint32_t *row, int words, int q_len, int n0)
+{
+    const int k = n0 >> 5, left = q_len - n0;
+    if (k < -1) return ~0u;
+    const uint32_t lo = k < 0 ? ~0u : k < words ? row[k] : 0u, hi = k + 1 < words ? row[k + 1] : 0u;
+    const uint32_t w = (uint32_t)(((uint64_t)hi << 32 | lo) >> (n0 & 31));
+    return left >= 32 ? w : left <= 0 ? 0u : w & ((1u << left) - 1u);
+}
+
+// TREE: the rows of a request are the nodes of a draft tree, whose keys they all read.
+template <int ROWS, int KEYS, bool TREE = false>
 struct ChunkUnit {                   // a request
     int q0, q_len, kv_len, G, open;  // open: what a tile costs beside its steps
     int tiles, first, last;          // steps of its first and last tile
@@ -48,7 +59,7 @@ struct ChunkUnit {                   // a request
 
     __device__ __forceinline__ int steps(int t) const
     {
-        const int tok = min((int)(((uint32_t)(t + 1) * ROWS - 1) / (uint32_t)G), q_len - 1), seen = kv_len - q_len + tok + 1;
+        const int tok = TREE ? q_len - 1 : min((int)(((uint32_t)(t + 1) * ROWS - 1) / (uint32_t)G), q_len - 1), seen = kv_len - q_len + tok + 1;
         return seen > 0 ? (int)(((unsigned)seen + KEYS - 1) / KEYS) : 0;
     }
     // A request.  One whose rows are outside of the call's or whose cache is longer than its row of the table has no tiles: nothing of it is read or written.
@@ -56,7 +67,8 @@ struct ChunkUnit {                   // a request
     {
         open = open_;
         q0 = q0_;
-        const bool fits = q0_ >= 0 && q1 >= q0_ && q1 <= a.total_rows && len <= (a.num_blocks > 0 ? a.max_blocks * kTile : 0);
+        bool fits = q0_ >= 0 && q1 >= q0_ && q1 <= a.total_rows && len <= (a.num_blocks > 0 ? a.max_blocks * kTile : 0);
+        if constexpr (TREE) fits = fits && q1 - q0_ <= 32 * a.mask_words;
         q_len = fits ? q1 - q0_ : 0;
         kv_len = max(len, 0);
         G = a.num_q_heads / a.num_kv_heads;
@@ -81,9 +93,9 @@ struct ChunkPos {
 };
 
 // A workgroup's span, piece by piece; all of it uniform over a wavefront.
-template <int ROWS, int KEYS, int OPEN>
+template <int ROWS, int KEYS, int OPEN, bool TREE = false>
 struct ChunkWalk {
-    typedef ChunkUnit<ROWS, KEYS> Unit;
+    typedef ChunkUnit<ROWS, KEYS, TREE> Unit;
     static_assert(OPEN > kOpenFew, "begin() takes the cost of few spans once, where the other one does not do");
     // the current piece: steps s0 to before s1 of tile t of request b.  part: place of its partial result, -1 if it is the whole tile.
     int b, t, s0, s1, part;

@@ -101,6 +101,7 @@ __global__ __launch_bounds__(256) void kv_commit_kernel(int batch, const int32_t
     const int b = blockIdx.x * 256 + threadIdx.x;
     if (b >= batch) return;
     const int k = q_indptr[b + 1] - q_indptr[b] - 1;
+    if (k < 0) return;                             // no new tokens
     kv_len[b] = kv_len[b] - k + accepted_len[b];   // the accepted drafts stay, the rejected slots fall past the end
 }
 
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(64) void kv_compact_kernel(KvAppendArgs a, const in
     const int h = blockIdx.x % a.num_kv_heads, b = blockIdx.x / a.num_kv_heads;
     const int q_len = a.q_indptr[b + 1] - a.q_indptr[b];
     const int P = a.kv_len[b] - q_len;
-    const int n = min(accepted_len[b], q_len - 1);
+    const int n = min(accepted_len[b], min(q_len - 1, SS_MAX_DEPTH));
     const int D = a.head_dim;
     const int32_t *bt = a.block_table + (int64_t)b * a.max_blocks;
     int prev = 0;

@@ -51,6 +51,9 @@ struct ChunkArgs {
     int32_t cap;                  // partial results the workspace has room for: two for each span and KV head, or none
     int32_t *rec;                 // [spans][kChunkRecInts] the tile that a span begins and does not end
     float *part_ml, *part_o;      // [cap] partial results
+    // draft trees only
+    const uint32_t *node_mask;    // [total_rows][mask_words] which nodes of its request a row attends
+    int32_t mask_words;
 };
 // A block id of the table as it is followed: one that is no block's, as behind a block map that lacked blocks, as the last block's.
 __device__ __forceinline__ int chunk_block(const ChunkArgs &a, int id)
@@ -75,6 +78,7 @@ size_t chunk_workspace_bytes(const ChunkShape &s, int head_dim);
 void chunk_carve(ChunkArgs &a, const ChunkShape &s, void *workspace);
 int32_t chunk_mfma_launch(const ChunkArgs &a, hipStream_t stream);
 int32_t chunk_f32_launch(const ChunkArgs &a, hipStream_t stream);
+int32_t tree_f32_launch(const ChunkArgs &a, hipStream_t stream);
 
 // ---- optional checks of device-resident metadata -----------------------------------------------
 int32_t validate_chunk(const int32_t *block_table, const int32_t *kv_len, const int32_t *q_indptr, int batch, int max_blocks,
