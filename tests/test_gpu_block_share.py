@@ -1,0 +1,399 @@
+"""Forks, releases, compaction and copies of blocks against their definitions, one block after the other."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_09562_amd import binding
+
+from . import share_ref as ref
+from .prefill_ref import BLOCK, DEV, TORCH, blocks
+
+pytestmark = pytest.mark.gpu
+
+
+def device(k):
+    t = lambda x: torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to(DEV)  # noqa: E731
+    return dict(batch=len(k["held"]), max_blocks_per_seq=k["table"].shape[1], block_table=t(k["table"]), kv_len=t(k["kv_len"]), held=t(k["held"]), shares=t(k["shares"]),
+                num_blocks=k["num_blocks"], free_ids=t(k["free"]), free_count=t([k["count"]]))
+
+
+def same(d, k, label=""):
+    for name, x in (("block_table", k["table"]), ("kv_len", k["kv_len"]), ("held", k["held"]), ("shares", k["shares"]), ("free_ids", k["free"])):
+        assert np.array_equal(d[name].cpu().numpy().reshape(-1), x.reshape(-1)), f"{label}: {name}"
+    assert int(d["free_count"]) == k["count"], label
+
+
+def ints(n, fill=-77):
+    return torch.full((n,), fill, dtype=torch.int32, device=DEV)
+
+
+def workspace(d, forks=0):
+    ws = binding.alloc_block_share_workspace(d, DEV, num_forks=forks)
+    ws.fill_(0xFF)
+    return ws
+
+
+def run_fork(k, parent, child, length=None):
+    d, n = device(k), len(parent)
+    src, dst, status = ints(n), ints(n), ints(1)
+    up = lambda x: torch.tensor(list(x), dtype=torch.int32, device=DEV)  # noqa: E731
+    binding.ss_block_fork(d, up(parent), up(child), None if length is None else up(length), src, dst, status, workspace(d, n))
+    torch.cuda.synchronize()
+    want, wsrc, wdst, wstatus = ref.fork(ref.copy_of(k), parent, child, length)
+    assert int(status) == wstatus
+    assert np.array_equal(src.cpu().numpy(), wsrc) and np.array_equal(dst.cpu().numpy(), wdst)
+    same(d, want)
+    return want, wstatus
+
+
+def run_release(k):
+    d, status = device(k), ints(1)
+    binding.ss_block_release(d, status, workspace(d))
+    torch.cuda.synchronize()
+    want, wstatus = ref.release(ref.copy_of(k))
+    assert int(status) == wstatus
+    same(d, want)
+    return want, wstatus
+
+
+def run_compact(k, shares=True, remap=True):
+    d, N = device(k), k["num_blocks"]
+    m, src, dst, moves, status = ints(N), ints(N // 2), ints(N // 2), ints(1), ints(1)
+    binding.ss_block_compact(d if shares else dict(d, shares=None), m if remap else None, src, dst, moves, status, workspace(d))
+    torch.cuda.synchronize()
+    want, wmap, wsrc, wdst, wmoves, wstatus = ref.compact(ref.copy_of(k))
+    if not shares:
+        want["shares"] = k["shares"]
+    assert int(status) == wstatus and int(moves) == wmoves
+    assert np.array_equal(src.cpu().numpy(), wsrc) and np.array_equal(dst.cpu().numpy(), wdst)
+    assert not remap or np.array_equal(m.cpu().numpy(), wmap)
+    same(d, want)
+    return want, wstatus
+
+
+SHAPES = [(4, 3, 5), (12, 20, 30), (40, 70, 10), (70, 90, 400), (1500, 6, 50)]    # batch, columns, free blocks: one workgroup's, and many workgroups'
+
+
+def random_forks(k, rng, whole=False):
+    """Forks of the held rows into the empty ones, some entries unused."""
+    empty = [b for b in range(len(k["held"])) if k["held"][b] == 0]
+    full = [b for b in range(len(k["held"])) if k["held"][b] > 0]
+    parent, child, length = [], [], []
+    for c in empty:
+        p = int(rng.choice(full))
+        n = int(k["kv_len"][p])
+        parent.append(p)
+        child.append(c)
+        length.append(n if whole else int(rng.integers(0, n + 1)))
+        if rng.random() < 0.4:
+            parent.append(-1 - int(rng.integers(0, 5)))
+            child.append(int(rng.integers(-3, 99)))
+            length.append(int(rng.integers(-3, 99)))
+    return parent, child, length
+
+
+@pytest.mark.parametrize("batch,width,spare", SHAPES)
+@pytest.mark.parametrize("seed", range(4))
+def test_forks(batch, width, spare, seed):
+    rng = np.random.default_rng(seed)
+    k = ref.random_books(rng, batch, width, spare, empty=max(2, batch // 5))
+    ref.check_books(k)
+    parent, child, length = random_forks(k, rng)
+    if seed == 3:
+        length = None
+    got, status = run_fork(k, parent, child, length)
+    if status == 0:
+        ref.check_books(got)
+
+
+def test_forks_need_their_blocks():
+    rng = np.random.default_rng(5)
+    k = ref.random_books(rng, 20, 10, 3, empty=8)
+    full = [b for b in range(20) if k["held"][b] > 0 and k["kv_len"][b] % BLOCK]
+    empty = [b for b in range(20) if k["held"][b] == 0]
+    got, status = run_fork(k, [full[0]] * 8, empty)
+    assert status == 5 and np.array_equal(got["table"], k["table"])
+    got, status = run_fork(k, [full[0]] * 3, empty[:3])
+    assert status == 0 and got["count"] == 0
+    # whole blocks need none
+    got, status = run_fork(got, [full[0]] * 5, empty[3:], [int(k["kv_len"][full[0]]) // BLOCK * BLOCK] * 5)
+    assert status == 0
+    ref.check_books(got)
+
+
+def test_forks_that_cannot_be():
+    rng = np.random.default_rng(6)
+    k = ref.random_books(rng, 12, 10, 20, empty=4)
+    f = [b for b in range(12) if k["held"][b] > 1]
+    e = [b for b in range(12) if k["held"][b] == 0]
+    n = int(k["kv_len"][f[0]])
+    for parent, child, length, bad in (([f[0], 12], [e[0], e[1]], None, 1), ([f[0], f[1]], [e[0], 12], None, 1), ([f[0], f[1]], [e[0], -1], None, 1),
+                                       ([f[0], f[1]], [e[0], e[0]], None, 1), ([f[0], f[1]], [e[0], f[2]], None, 1), ([f[0], f[0]], [e[0], f[0]], None, 0),
+                                       ([f[0], e[0]], [e[0], e[1]], None, 1), ([f[0]], [e[0]], [n + 1], 0), ([f[0]], [e[0]], [-1], 0), ([f[0]], [f[0]], None, 0),
+                                       ([-1, 2 ** 31 - 1], [e[0], e[1]], None, 1)):
+        got, status = run_fork(k, parent, child, length)
+        assert status == -1 - bad, (parent, child, length)
+    for name, at, value in (("kv_len", f[0], -5), ("held", f[0], -1), ("held", f[0], 0), ("kv_len", f[0], 2 ** 31 - 1)):
+        broken = ref.copy_of(k)
+        broken[name][at] = value
+        assert run_fork(broken, [f[0]], [e[0]])[1] == -1
+    for count in (-1, k["num_blocks"] + 1):
+        assert run_fork(dict(k, count=count), [f[0]], [e[0]])[1] == -2
+    got, status = run_fork(k, [f[0], f[1]], [e[0], e[1]], [0, 0])
+    assert status == 0 and got["held"][e[0]] == 0
+    assert run_fork(k, [], [])[1] == 0
+
+
+@pytest.mark.parametrize("batch,width,spare", SHAPES)
+@pytest.mark.parametrize("seed", range(4))
+def test_releases(batch, width, spare, seed):
+    rng = np.random.default_rng(seed + 50)
+    k = ref.random_books(rng, batch, width, spare)
+    for b in range(batch):
+        u = rng.random()
+        if u < 0.4 or seed == 3:
+            k["kv_len"][b] = 0
+        elif u < 0.7:
+            k["kv_len"][b] = rng.integers(0, k["kv_len"][b] + 40)   # less, or more than is held
+    before = ref.copy_of(k)
+    got, status = run_release(k)
+    assert status == 0
+    ref.check_books(dict(got, kv_len=got["kv_len"]))
+    if seed == 3:
+        assert got["count"] == got["num_blocks"] and not got["shares"].any() and not got["held"].any()
+    again, _ = run_release(got)     # nothing is left to give back
+    assert again["count"] == got["count"] and np.array_equal(before["table"], again["table"])
+
+
+def test_many_releases_in_pieces():
+    """More given back than a workgroup counts at a time, most of it shared; the last holder decides the place."""
+    rng = np.random.default_rng(9)
+    for batch, width in ((300, 200), (30, 3000)):
+        k = ref.random_books(rng, batch, width, 7, families=6, empty=1)
+        k["kv_len"][:] = np.where(rng.random(batch) < 0.8, 0, k["kv_len"])
+        got, status = run_release(k)
+        assert status == 0
+        ref.check_books(got)
+
+
+def test_releases_that_cannot_be():
+    k = ref.random_books(np.random.default_rng(10), 9, 8, 5)
+    for name, at, value, want in (("kv_len", 3, -1, -4), ("held", 8, 9, -9), ("held", 0, -2, -1), ("held", 2, 2 ** 31 - 1, -3)):
+        broken = ref.copy_of(k)
+        broken["kv_len"][:] = 0
+        broken[name][at] = value
+        assert run_release(broken)[1] == want
+    for count in (-1, k["num_blocks"] + 1):
+        assert run_release(dict(k, count=count))[1] == -10
+
+
+@pytest.mark.parametrize("batch,width", [(16, 9), (80, 90)])
+def test_blocks_given_back_too_often_and_ids_that_are_none(batch, width):
+    """A block twice in a table goes to the list once; what is no block's id is left where it is, and nothing is written outside the arrays."""
+    rng = np.random.default_rng(11)
+    k = ref.random_books(rng, batch, width, 4, families=1)
+    rows = [b for b in range(batch) if k["held"][b] > 2]
+    assert len(rows) > 2
+    k["table"][rows[0], 1] = k["table"][rows[1], 2]
+    k["table"][rows[0], 0] = k["table"][rows[0], 2]
+    k["table"][rows[1], 1] = k["num_blocks"]
+    k["table"][rows[2], 0] = -2 ** 31
+    k["table"][rows[2], 1] = 2 ** 31 - 1
+    k["kv_len"][rows[:3]] = 0
+    got, status = run_release(k)
+    assert status == 0
+    free = got["free"][:got["count"]]
+    assert len(set(free.tolist())) == len(free)
+
+
+@pytest.mark.parametrize("batch,width,spare", SHAPES)
+@pytest.mark.parametrize("seed", range(3))
+def test_compaction(batch, width, spare, seed):
+    rng = np.random.default_rng(seed + 90)
+    k = ref.random_books(rng, batch, width, spare)
+    got, status = run_compact(k, shares=seed != 1, remap=seed != 2)
+    assert status == 0
+    if seed != 1:
+        ref.check_books(got)
+        again, _ = run_compact(got)
+        assert np.array_equal(again["table"], got["table"])
+    used = got["num_blocks"] - got["count"]
+    assert all(x < used for b in range(batch) for x in got["table"][b, :got["held"][b]])
+
+
+def test_compaction_of_caches_of_any_size():
+    rng = np.random.default_rng(12)
+    for spare in (0, 1, 2):
+        run_compact(ref.random_books(rng, 3, 4, spare, empty=0))
+    for n in (1, 2, 31, 32, 33, 64):      # nothing in use, and nothing free
+        e = dict(table=np.zeros((1, 1), np.int32), held=np.zeros(1, np.int32), kv_len=np.zeros(1, np.int32), shares=np.zeros(n, np.int32), num_blocks=n)
+        run_compact(dict(e, free=rng.permutation(n).astype(np.int32), count=n))
+        run_compact(dict(e, free=np.full(n, -1, np.int32), count=0))
+    n = 600_000      # more than LDS takes
+    perm = rng.permutation(n).astype(np.int32)
+    table = np.full((2, 1000), -1, np.int32)
+    table[0, :900], table[1, :40] = perm[:900], perm[860:900]
+    shares = np.zeros(n, np.int32)
+    shares[perm[860:900]] = 1
+    free = np.full(n, -1, np.int32)
+    free[:n - 900] = perm[900:]
+    run_compact(dict(table=table, held=np.array([900, 40], np.int32), kv_len=np.array([900 * 16, 640], np.int32), shares=shares, free=free, count=n - 900, num_blocks=n))
+
+
+@pytest.mark.parametrize("batch,width,spare", [(6, 5, 20), (60, 80, 300)])
+def test_compaction_of_lists_that_cannot_be(batch, width, spare):
+    k = ref.random_books(np.random.default_rng(13), batch, width, spare)
+    for value in (k["num_blocks"], -1, int(k["free"][3]), 2 ** 31 - 1):
+        broken = ref.copy_of(k)
+        broken["free"][5] = value
+        assert run_compact(broken)[1] == -1 - batch
+    for count in (-1, k["num_blocks"] + 1):
+        assert run_compact(dict(k, count=count))[1] == -1 - batch
+    for value in (-1, width + 1):
+        broken = ref.copy_of(k)
+        broken["held"][2] = value
+        assert run_compact(broken)[1] == -3
+    broken = ref.copy_of(k)
+    row = int(np.argmax(k["held"]))
+    broken["table"][row, :2] = [-5, 2 ** 31 - 1]
+    run_compact(broken)
+
+
+def caches(layers, n, hkv, d, kv, seed=0):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    out = []
+    for _ in range(layers):
+        x = [torch.randint(0, 256, (n * hkv * BLOCK * d * {"f32": 4, "bf16": 2, "fp8": 1}[kv],), dtype=torch.uint8, device=DEV, generator=gen)
+             .view(TORCH[kv]).view(n, hkv, BLOCK, d) for _ in range(2)]     # any bits, NaN among them
+        s = [torch.randn((n, hkv), device=DEV, generator=gen) if kv == "fp8" else None for _ in range(2)]
+        out.append(dict(num_blocks=n, block_size=BLOCK, num_kv_heads=hkv, head_dim=d, kv_dtype=kv, k_cache=x[0], v_cache=x[1], k_scale=s[0], v_scale=s[1]))
+    return out
+
+
+def bits(x):
+    return x.contiguous().view(torch.uint8)
+
+
+@pytest.mark.parametrize("kv", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("layers,hkv,d,n", [(1, 1, 64, 5), (3, 8, 128, 40), (70, 2, 64, 9), (2, 3, 128, 200)])
+def test_copies(kv, layers, hkv, d, n):
+    c = caches(layers, n, hkv, d, kv)
+    rng = np.random.default_rng(n)
+    perm = rng.permutation(n)
+    half = n // 2
+    src, dst = perm[:half].astype(np.int32), perm[half:2 * half].astype(np.int32)
+    src[0], bad = (src[0], None) if half < 4 else (-1, 0)
+    if half >= 4:      # pairs that are none
+        dst[1], src[2], dst[3] = n, 2 ** 31 - 1, -2 ** 31
+    for count in (None, 0, 1, half // 2, half + 100, -3):
+        want = [{name: x.clone() for name, x in l.items() if isinstance(x, torch.Tensor)} for l in c]
+        m = half if count is None else max(min(count, half), 0)
+        for l in want:
+            for x in l.values():
+                for a, b in zip(src[:m], dst[:m]):
+                    if 0 <= a < n and 0 <= b < n:
+                        bits(x)[int(b)] = bits(x)[int(a)].clone()
+        up = lambda x: torch.from_numpy(x).to(DEV)  # noqa: E731
+        binding.ss_block_copy(binding.cache_layers(c), up(src), up(dst), None if count is None else torch.tensor([count], dtype=torch.int32, device=DEV))
+        torch.cuda.synchronize()
+        for l, w in zip(c, want):
+            for name, x in w.items():
+                assert torch.equal(bits(l[name]), bits(x)), (name, count)
+
+
+def test_copies_behind_four_gigabytes():
+    n = 80000       # blocks of 64 KB of keys
+    c = caches(1, 1, 16, 128, "bf16")[0]
+    c.update(num_blocks=n, k_cache=torch.empty((n, 16, BLOCK, 128), dtype=torch.bfloat16, device=DEV), v_cache=torch.empty((n, 16, BLOCK, 128), dtype=torch.bfloat16, device=DEV))
+    for x in (c["k_cache"], c["v_cache"]):
+        x[n - 1].normal_()
+        x[3].zero_()
+        x[n - 2].zero_()
+    src, dst = torch.tensor([n - 1, n - 1], dtype=torch.int32, device=DEV), torch.tensor([3, n - 2], dtype=torch.int32, device=DEV)
+    binding.ss_block_copy(binding.cache_layers([c]), src, dst)
+    torch.cuda.synchronize()
+    for x in (c["k_cache"], c["v_cache"]):
+        assert torch.equal(x[3], x[n - 1]) and torch.equal(x[n - 2], x[n - 1])
+
+
+def test_captured():
+    """The calls of a step of a search, captured once and replayed on other books."""
+    rng = np.random.default_rng(20)
+    start = ref.random_books(rng, 40, 30, 60, empty=8)
+    d = device(start)
+    empty = [b for b in range(40) if start["held"][b] == 0]
+    full = [b for b in range(40) if start["held"][b] > 0]
+    parent = torch.tensor([full[i % 5] for i in range(8)], dtype=torch.int32, device=DEV)
+    child = torch.tensor(empty, dtype=torch.int32, device=DEV)
+    c = caches(2, start["num_blocks"], 2, 64, "fp8")
+    handle = binding.cache_layers(c)
+    N = start["num_blocks"]
+    src, dst, status, ws = ints(8), ints(8), ints(3), workspace(d, 8)
+    msrc, mdst, moves = ints(N // 2), ints(N // 2), ints(1)
+
+    def step():
+        binding.ss_block_release(d, status[0:1], ws)
+        binding.ss_block_fork(d, parent, child, None, src, dst, status[1:2], ws)
+        binding.ss_block_copy(handle, src, dst)
+        binding.ss_block_compact(d, None, msrc, mdst, moves, status[2:3], ws)
+        binding.ss_block_copy(handle, msrc, mdst, moves)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    books = ("block_table", "kv_len", "held", "shares", "free_ids", "free_count")
+    for i in range(3):
+        k = ref.copy_of(start)
+        for b in full[6:]:
+            if rng.random() < 0.5:
+                k["kv_len"][b] = 0
+        new = device(k)
+        for name in books:
+            d[name].copy_(new[name])
+        # what the requests hold, as bytes, before and after
+        held_bytes = lambda: [[bits(l[x])[d["block_table"][b, :blocks(int(d["kv_len"][b]))].long()].clone() for l in c for x in ("k_cache", "v_cache", "k_scale", "v_scale")]  # noqa: E731
+                              for b in full if int(d["kv_len"][b]) <= 16 * int(d["held"][b])]
+        before = held_bytes()
+        graph.replay()
+        torch.cuda.synchronize()
+        k, s0 = ref.release(k)
+        k, _, _, s1 = ref.fork(k, parent.tolist(), child.tolist(), None)
+        k, _, _, _, _, s2 = ref.compact(k)
+        assert status.tolist() == [s0, s1, s2] == [0, 0, 0]
+        same(d, k)
+        ref.check_books(k)
+        for x, y in zip(before, held_bytes()):
+            for p, q in zip(x, y):
+                assert torch.equal(p, q)
+        for j, b in enumerate(empty):        # a child holds what its parent does
+            p = int(parent[j])
+            n = int(k["kv_len"][b])
+            for l in c:
+                for x in ("k_cache", "v_cache", "k_scale", "v_scale"):
+                    a, z = (bits(l[x])[d["block_table"][r, :blocks(n)].long()] for r in (p, b))
+                    assert torch.equal(a, z)
+
+
+def test_binding_refuses():
+    k = ref.random_books(np.random.default_rng(30), 6, 5, 9)
+    d = device(k)
+    src, ws, status = ints(4), workspace(d, 4), ints(1)
+    z = torch.zeros(2, dtype=torch.int32, device=DEV)
+    for name in ("block_table", "kv_len", "held", "shares", "free_ids", "free_count"):
+        for bad in (d[name].long(), d[name].cpu(), d[name].reshape(-1)[:0]):
+            with pytest.raises(binding.SpecVerifyError):
+                binding.ss_block_release(dict(d, **{name: bad}), status, ws)
+    with pytest.raises(binding.SpecVerifyError):
+        binding.ss_block_fork(d, z, z[:1], None, src, src, status, ws)
+    with pytest.raises(binding.SpecVerifyError):
+        binding.ss_block_fork(d, z.long(), z, None, src, src, status, ws)
+    with pytest.raises(binding.SpecVerifyError):
+        binding.ss_block_compact(d, None, src[:1], src, status, status, ws)
+    c = caches(1, 5, 1, 64, "bf16")
+    with pytest.raises(binding.SpecVerifyError):
+        binding.ss_block_copy(binding.cache_layers(c), z, z[:1])
+    with pytest.raises(binding.SpecVerifyError):
+        binding.cache_layers([dict(c[0], k_cache=c[0]["k_cache"][:2])])
+    binding.ss_block_copy(binding.cache_layers([]), z, z)
+    same(d, k)
