@@ -22,16 +22,16 @@ LIB = os.path.join(HERE, "libspecverify.so")
 # the per-grouping attention units take longest: start them first
 SOURCES = ["attn_mfma_g8.hip", "attn_mfma_g4.hip", "attn_mfma_g2.hip", "attn_mfma_g1.hip", "attn_unit.hip", "accept.hip", "accept_tree.hip", "accept_static.hip", "api.hip",
            "attn_chunk.hip", "attn_mfma.hip", "attn_generic.hip", "kvcache.hip", "block_map.hip", "kv_write.hip", "attn_chunk_f32.hip", "api_prefill.hip", "validate.hip",
-           "api_tree.hip", "block_share.hip", "block_copy.hip", "tree_verify.hip",
+           "attn_tree.hip", "attn_tree_unit.hip", "api_tree.hip", "block_share.hip", "block_copy.hip", "tree_verify.hip",
            "depth_controller.cpp", "router.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function", "-Rpass-analysis=kernel-resource-usage",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
-# Matrix instructions of attn_chunk.hip take either half of its 512 registers: left to itself the compiler puts the results of all of them, scores too, into the
+# Matrix instructions of attn_chunk.hip and attn_tree.hip take either half of its 512 registers: left to itself the compiler puts the results of all of them, scores too, into the
 # half that ordinary arithmetic does not reach, moves every score over and spills (4096 tokens behind 12288: 1516 us against 903; four chunks over an e4m3 cache: 917 against 307).
 # A compiler that does not know the switch ends the build with its name; without it the kernel is slow, not wrong.
-FLAGS_OF = {"attn_chunk.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+FLAGS_OF = {s: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for s in ("attn_chunk.hip", "attn_tree.hip")}
 # the host pass reports that it does not know the packed-fp32 feature; that line is noise
 NOISE = "is not a recognized feature for this target"
 

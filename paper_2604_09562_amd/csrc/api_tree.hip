@@ -32,6 +32,31 @@ int32_t check_books(const ss_batch *b, const ss_block_pool *pool)
     return SS_OK;
 }
 
+// Partial results of the kernel of short calls: (reference, sum) of their rows, then their outputs.
+size_t unit_slots(const TreeUnitChoice &u, int batch, int heads) { return u.splits > 1 ? (size_t)batch * u.tiles * u.splits * heads : 0; }
+size_t unit_part_o(const TreeUnitChoice &u, int batch, int heads) { return align_up(unit_slots(u, batch, heads) * kTreeUnitRows * 2 * sizeof(float), 256); }
+
+// Which kernel takes a call.
+struct TreeForm {
+    bool mfma;
+    TreeUnitChoice unit;
+    ChunkShape shape;
+    size_t workspace;
+};
+TreeForm tree_form(const ss_paged_kv *kv, const ss_batch *b, int32_t q_dtype, int32_t num_q_heads, int32_t total_rows)
+{
+    TreeForm f;
+    f.mfma = chunk_mfma_supported(kv->head_dim, kv->dtype, q_dtype);
+    const int64_t nodes = b->max_q_len > 0 && b->max_q_len < total_rows ? b->max_q_len : b->max_q_len > 0 || b->batch == 1 ? total_rows : 0;   // of the widest tree
+    f.unit = f.mfma ? tree_unit_rule(b->batch, kv->num_kv_heads, nodes * (num_q_heads / kv->num_kv_heads), (int64_t)b->max_blocks_per_seq * SS_BLOCK_SIZE, kv->head_dim,
+                                     kv->dtype == SS_FP8_E4M3, attn_chip_waves() / 4)
+                    : TreeUnitChoice{0, 1};
+    f.shape = chunk_shape(f.mfma, b->batch, b->max_blocks_per_seq, num_q_heads, kv->num_kv_heads, total_rows);
+    f.workspace = f.unit.tiles ? unit_part_o(f.unit, b->batch, kv->num_kv_heads) + unit_slots(f.unit, b->batch, kv->num_kv_heads) * kTreeUnitRows * kv->head_dim * sizeof(float) + 256
+                               : chunk_workspace_bytes(f.shape, kv->head_dim);
+    return f;
+}
+
 bool pool_pointers(const ss_block_pool *pool) { return pool->free_count && (pool->num_blocks == 0 || pool->free_ids); }
 
 constexpr int32_t kMaxForks = 1 << 20;
@@ -47,7 +72,7 @@ extern "C" {
 size_t ss_tree_attn_workspace(const ss_paged_kv *kv, const ss_batch *batch, int32_t q_dtype, int32_t num_q_heads, int32_t total_rows)
 {
     if (check_tree_attn(kv, batch, q_dtype, num_q_heads, total_rows) != SS_OK) return 0;
-    return chunk_workspace_bytes(chunk_shape(false, batch->batch, batch->max_blocks_per_seq, num_q_heads, kv->num_kv_heads, total_rows), kv->head_dim);
+    return tree_form(kv, batch, q_dtype, num_q_heads, total_rows).workspace;
 }
 
 int32_t ss_tree_attn(const ss_paged_kv *kv, const ss_batch *batch, const uint32_t *node_mask, int32_t mask_words, const void *q, int64_t q_stride,
@@ -64,8 +89,8 @@ int32_t ss_tree_attn(const ss_paged_kv *kv, const ss_batch *batch, const uint32_
     if (!aligned16(out)) return fail(SS_ERR_INVALID_ARG, "out must be 16-byte aligned");
     if (!(sm_scale > 0.0f) || sm_scale > 2.0e38f)   // (times log2(e) it has to be a float, too)
         return fail(SS_ERR_INVALID_ARG, "sm_scale must be positive and at most 2e38");
-    const ChunkShape s = chunk_shape(false, batch->batch, batch->max_blocks_per_seq, num_q_heads, kv->num_kv_heads, total_rows);
-    if ((rc = check_workspace(workspace, workspace_bytes, chunk_workspace_bytes(s, kv->head_dim))) != SS_OK) return rc;
+    const TreeForm f = tree_form(kv, batch, q_dtype, num_q_heads, total_rows);
+    if ((rc = check_workspace(workspace, workspace_bytes, f.workspace)) != SS_OK) return rc;
     if (option_validate()) {
         rc = validate_chunk(batch->block_table, batch->kv_len, batch->q_indptr, batch->batch, batch->max_blocks_per_seq, kv->num_blocks, total_rows,
                             batch->max_q_len ? batch->max_q_len : total_rows, static_cast<hipStream_t>(stream), "ss_tree_attn");
@@ -78,8 +103,13 @@ int32_t ss_tree_attn(const ss_paged_kv *kv, const ss_batch *batch, const uint32_
     a.block_table = batch->block_table; a.kv_len = batch->kv_len; a.q_indptr = batch->q_indptr;
     a.q = q; a.q_stride = q_stride; a.out = out; a.lse = lse; a.q_dtype = q_dtype; a.num_q_heads = num_q_heads; a.sm_scale = sm_scale;
     a.node_mask = node_mask; a.mask_words = mask_words;
-    chunk_carve(a, s, workspace);
-    return tree_f32_launch(a, static_cast<hipStream_t>(stream));
+    if (f.unit.tiles) {
+        a.part_ml = static_cast<float *>(workspace);
+        a.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace) + unit_part_o(f.unit, batch->batch, kv->num_kv_heads));
+        return tree_unit_launch(a, f.unit, static_cast<hipStream_t>(stream));
+    }
+    chunk_carve(a, f.shape, workspace);
+    return f.mfma ? tree_mfma_launch(a, static_cast<hipStream_t>(stream)) : tree_f32_launch(a, static_cast<hipStream_t>(stream));
 }
 
 size_t ss_tree_verify_workspace(int32_t batch, int32_t total_rows, int32_t vocab)

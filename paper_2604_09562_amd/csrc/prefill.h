@@ -3,6 +3,7 @@
 #pragma once
 
 #include "common.h"
+#include "tree_rule.h"
 
 namespace ss {
 
@@ -79,6 +80,8 @@ void chunk_carve(ChunkArgs &a, const ChunkShape &s, void *workspace);
 int32_t chunk_mfma_launch(const ChunkArgs &a, hipStream_t stream);
 int32_t chunk_f32_launch(const ChunkArgs &a, hipStream_t stream);
 int32_t tree_f32_launch(const ChunkArgs &a, hipStream_t stream);
+int32_t tree_mfma_launch(const ChunkArgs &a, hipStream_t stream);
+int32_t tree_unit_launch(const ChunkArgs &a, const TreeUnitChoice &how, hipStream_t stream);
 
 // ---- optional checks of device-resident metadata -----------------------------------------------
 int32_t validate_chunk(const int32_t *block_table, const int32_t *kv_len, const int32_t *q_indptr, int batch, int max_blocks,

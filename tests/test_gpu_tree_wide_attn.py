@@ -248,7 +248,7 @@ def test_binding_refuses():
     with pytest.raises(binding.SpecVerifyError):
         binding.ss_tree_attn(inp, out, lse.double(), ws)
     with pytest.raises(binding.SpecVerifyError):
-        binding.ss_tree_attn(inp, out, lse, ws[:256])
+        binding.ss_tree_attn(inp, out, lse, ws[:128])
     binding.ss_set_option("validate", 1)
     try:
         with pytest.raises(binding.SpecVerifyError, match="out of range"):
