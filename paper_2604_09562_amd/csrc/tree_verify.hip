@@ -6,7 +6,10 @@
 // the formula.  An exponential's argument is formed from the difference of two logits, which is exact to 2^-53, so that blocks with different
 // references agree to 1e-15.
 //
-// One pass over all rows, one workgroup a row for the draw, and the walk through the drawn tokens.
+// Two forms.  Few rows: one pass over all of them, a workgroup a row for the draws, and the walk through the drawn tokens, three launches.  Many rows: only those on the paths are
+// read, a round after the other; in a round every workgroup of a request first finds, each for itself, what was drawn at the node before and the child that the walk goes on with, and
+// then takes its blocks of that child's row.  Bound by latency: a round is a chain of state, masses, one block, the tree and the new row (9 us, 13 where 64 rows of 128 256 entries are
+// summed; the exponentials of those are half of that).
 #include "accept_common.h"
 #include "tree_verify.h"
 
@@ -17,27 +20,17 @@ struct Draw {           // of a row
     int32_t token;
     float logprob;
 };
-
-struct VerifyWorkspace {
-    float *top;         // [rows][nsub] the blocks' largest logits
-    double *sum;        // [rows][nsub]
-    Draw *draw;         // [rows]
-    int32_t *request;   // [rows] whose row it is, -1: no one's
-    int nsub;
+struct Walk {           // where a request's walk is
+    int32_t cur, n;     // node, -1 at its end; accepted nodes
 };
 
-__host__ VerifyWorkspace carve_verify(void *ws, int total_rows, int vocab)
-{
-    VerifyWorkspace w;
-    w.nsub = num_sub(vocab);
-    char *p = static_cast<char *>(ws);
-    const size_t n = (size_t)total_rows * w.nsub;
-    w.sum = reinterpret_cast<double *>(p); p += align_up(sizeof(double) * n, 256);
-    w.top = reinterpret_cast<float *>(p); p += align_up(sizeof(float) * n, 256);
-    w.draw = reinterpret_cast<Draw *>(p); p += align_up(sizeof(Draw) * (size_t)total_rows, 256);
-    w.request = reinterpret_cast<int32_t *>(p);
-    return w;
-}
+struct VerifyWorkspace {
+    double *sum;        // [rows][nsub], in rounds [2][batch][nsub]
+    float *top;         // the same: the blocks' largest logits
+    Draw *draw;         // [rows]
+    Walk *walk;         // in rounds [2][batch]
+    int nsub;
+};
 
 // Arguments of exponentials, (x - max) / T in steps of the table.
 struct DiffArg {
@@ -76,29 +69,10 @@ __device__ __forceinline__ bool rows_of(const TreeVerifyArgs &a, int b, int &r0,
     return r0 >= 0 && r1 > r0 && r1 <= a.total_rows;
 }
 
-__global__ __launch_bounds__(kThreads) void verify_rows_kernel(TreeVerifyArgs a, VerifyWorkspace w)
-{
-    const int row = blockIdx.x * kThreads + threadIdx.x;
-    if (row < a.total_rows) w.request[row] = -1;
-}
-__global__ __launch_bounds__(kThreads) void verify_requests_kernel(TreeVerifyArgs a, VerifyWorkspace w)
-{
-    int r0, rows;
-    if (!rows_of(a, blockIdx.x, r0, rows)) return;
-    for (int i = threadIdx.x; i < rows; i += kThreads) w.request[r0 + i] = blockIdx.x;
-}
-
-// grid: rows * blocks
+// The sums of block c of a row.
 template <int DT>
-__global__ __launch_bounds__(kThreads) void verify_sums_kernel(TreeVerifyArgs a, VerifyWorkspace w)
+__device__ __forceinline__ void block_sums(const TreeVerifyArgs &a, int64_t row, int c, double inv_t, const ExpTable &ex, float *top, double *sum, float *sh_m, double *sh_s)
 {
-    __shared__ ExpTable ex;
-    __shared__ float sh_m[4];
-    __shared__ double sh_s[4];
-    const int row = blockIdx.x / w.nsub, c = blockIdx.x % w.nsub, b = w.request[row];
-    if (b < 0) return;
-    const double inv_t = inverse_temperature(a, b);
-    ex.init();
     Raw8<DT> raw;
     float x[8];
     load8<DT>(row_ptr(a.target, row, a.row_stride, DT), a.vocab, c * kSub + threadIdx.x * 8, raw);
@@ -116,30 +90,55 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(TreeVerifyArgs a,
         s = block_sum(s, sh_s);
     }
     if (threadIdx.x == 0) {
-        w.top[(int64_t)row * w.nsub + c] = m;
-        w.sum[(int64_t)row * w.nsub + c] = s;
+        top[c] = m;
+        sum[c] = s;
     }
+}
+
+// The lowest token of a row whose logit is m, the row's largest; in every lane of a workgroup.
+template <int DT>
+__device__ __forceinline__ int lowest_with(const TreeVerifyArgs &a, int nsub, const float *top, int row, float m, int *sh)
+{
+    auto least = [&](int x) {
+        for (int off = 32; off; off >>= 1) x = min(x, __shfl_xor(x, off));
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
+        __syncthreads();
+        return min(min(sh[0], sh[1]), min(sh[2], sh[3]));
+    };
+    int c = 0x7fffffff;
+    for (int i = threadIdx.x; i < nsub; i += kThreads)
+        if (top[i] == m) { c = i; break; }
+    c = least(c);
+    Raw8<DT> raw;
+    float x[8];
+    const int i0 = c * kSub + threadIdx.x * 8;
+    load8<DT>(row_ptr(a.target, row, a.row_stride, DT), a.vocab, i0, raw);
+    unpack8<DT>(raw, x);
+    int y = 0x7fffffff;
+#pragma unroll
+    for (int i = 7; i >= 0; --i)
+        if (x[i] == m) y = i0 + i;
+    return least(y);
 }
 
 // The token of a row, in every lane of a workgroup.
 template <int DT>
-__device__ Draw draw_of(const TreeVerifyArgs &a, const VerifyWorkspace &w, int row, double inv_t, const ExpTable &ex, DrawShared &sh, float *sh_m, double *sh_s)
+__device__ Draw draw_of(const TreeVerifyArgs &a, int nsub, const float *top, const double *sum, int row, double inv_t, const ExpTable &ex, DrawShared &sh, float *sh_m, double *sh_s)
 {
-    const float *top = w.top + (int64_t)row * w.nsub;
-    const double *sum = w.sum + (int64_t)row * w.nsub;
     float m = -INFINITY;
-    for (int c = threadIdx.x; c < w.nsub; c += kThreads) m = fmaxf(m, top[c]);
+    for (int c = threadIdx.x; c < nsub; c += kThreads) m = fmaxf(m, top[c]);
     m = block_max(m, sh_m);
     Draw d = {-1, 0.f};
     if (inv_t > 0.0 && m < INFINITY && m > -INFINITY) {
         const DiffArg arg(inv_t, m);
         auto mass_of = [&](int c) { return top[c] == -INFINITY ? 0.0 : sum[c] * ex(arg(top[c])); };
         double part = 0.0;
-        for (int c = threadIdx.x; c < w.nsub; c += kThreads) part += mass_of(c);
+        for (int c = threadIdx.x; c < nsub; c += kThreads) part += mass_of(c);
         const double all = block_sum(part, sh_s);
         __syncthreads();
         const void *p = row_ptr(a.target, row, a.row_stride, DT);
-        d.token = draw_token(w.nsub, a.uniforms[row], sh, mass_of, [&](int c, double (&r)[kSubPer]) {
+        d.token = draw_token(nsub, a.uniforms[row], sh, mass_of, [&](int c, double (&r)[kSubPer]) {
             Raw8<DT> raw;
             float x[8];
             load8<DT>(p, a.vocab, c * kSub + threadIdx.x * 8, raw);
@@ -151,23 +150,8 @@ __device__ Draw draw_of(const TreeVerifyArgs &a, const VerifyWorkspace &w, int r
         });
         if (d.token >= 0) d.logprob = (float)(((double)load_logit(a.target, row, a.row_stride, DT, d.token) - (double)m) * inv_t - log(all));
     }
-    if (d.token < 0) d.token = m > -INFINITY ? lowest_index_of(a.target, row, a.row_stride, DT, a.vocab, m, sh) : 0;
+    if (d.token < 0) d.token = m > -INFINITY ? lowest_with<DT>(a, nsub, top, row, m, sh.first) : 0;
     return d;
-}
-
-// grid: rows
-template <int DT>
-__global__ __launch_bounds__(kThreads) void verify_draw_kernel(TreeVerifyArgs a, VerifyWorkspace w)
-{
-    __shared__ ExpTable ex;
-    __shared__ DrawShared sh;
-    __shared__ float sh_m[4];
-    __shared__ double sh_s[4];
-    const int row = blockIdx.x, b = w.request[row];
-    if (b < 0) return;
-    ex.init();
-    const Draw d = draw_of<DT>(a, w, row, inverse_temperature(a, b), ex, sh, sh_m, sh_s);
-    if (threadIdx.x == 0) w.draw[row] = d;
 }
 
 // The lowest child of node cur that carries token y, INT_MAX if there is none; in every lane of a workgroup.
@@ -183,74 +167,209 @@ __device__ __forceinline__ int child_with(const TreeVerifyArgs &a, int r0, int r
     return min(min(sh[0], sh[1]), min(sh[2], sh[3]));
 }
 
+// What a request has before anything is drawn; whether it has rows.
+__device__ __forceinline__ void clear_outputs(const TreeVerifyArgs &a, int b)
+{
+    const int tid = threadIdx.x;
+    if (tid == 0) a.accepted_len[b] = 0;
+    if (tid < SS_OUT_WIDTH) {
+        a.out_tokens[(int64_t)b * SS_OUT_WIDTH + tid] = -1;
+        if (a.logprobs) a.logprobs[(int64_t)b * SS_OUT_WIDTH + tid] = 0.f;
+        if (tid < SS_MAX_DEPTH) a.accepted_nodes[(int64_t)b * SS_MAX_DEPTH + tid] = -1;
+    }
+}
+__device__ __forceinline__ void emit(const TreeVerifyArgs &a, int b, int n, const Draw &d)
+{
+    a.out_tokens[(int64_t)b * SS_OUT_WIDTH + n] = d.token;
+    if (a.logprobs) a.logprobs[(int64_t)b * SS_OUT_WIDTH + n] = d.logprob;
+}
+
+// ---- few rows ----------------------------------------------------------------------------------------------------------
+// The request that a row belongs to, -1 if none does; in every lane of a workgroup.
+__device__ __forceinline__ int request_of(const TreeVerifyArgs &a, int row, int *sh)
+{
+    int at = 0x7fffffff;
+    for (int b = threadIdx.x; b < a.batch; b += kThreads) {
+        int r0, rows;
+        if (rows_of(a, b, r0, rows) && row >= r0 && row < r0 + rows) at = min(at, b);
+    }
+    for (int off = 32; off; off >>= 1) at = min(at, __shfl_xor(at, off));
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = at;
+    __syncthreads();
+    at = min(min(sh[0], sh[1]), min(sh[2], sh[3]));
+    __syncthreads();
+    return at == 0x7fffffff ? -1 : at;
+}
+
+// grid: rows * blocks
+template <int DT>
+__global__ __launch_bounds__(kThreads) void verify_sums_kernel(TreeVerifyArgs a, VerifyWorkspace w)
+{
+    __shared__ ExpTable ex;
+    __shared__ float sh_m[4];
+    __shared__ double sh_s[4];
+    __shared__ int sh_b[4];
+    const int row = blockIdx.x / w.nsub, c = blockIdx.x % w.nsub, b = request_of(a, row, sh_b);
+    if (b < 0) return;
+    ex.init();
+    block_sums<DT>(a, row, c, inverse_temperature(a, b), ex, w.top + (int64_t)row * w.nsub, w.sum + (int64_t)row * w.nsub, sh_m, sh_s);
+}
+
+// grid: rows
+template <int DT>
+__global__ __launch_bounds__(kThreads) void verify_draw_kernel(TreeVerifyArgs a, VerifyWorkspace w)
+{
+    __shared__ ExpTable ex;
+    __shared__ DrawShared sh;
+    __shared__ float sh_m[4];
+    __shared__ double sh_s[4];
+    __shared__ int sh_b[4];
+    const int row = blockIdx.x, b = request_of(a, row, sh_b);
+    if (b < 0) return;
+    ex.init();
+    const Draw d = draw_of<DT>(a, w.nsub, w.top + (int64_t)row * w.nsub, w.sum + (int64_t)row * w.nsub, row, inverse_temperature(a, b), ex, sh, sh_m, sh_s);
+    if (threadIdx.x == 0) w.draw[row] = d;
+}
+
 // grid: batch
 __global__ __launch_bounds__(kThreads) void verify_walk_kernel(TreeVerifyArgs a, VerifyWorkspace w)
 {
     __shared__ int sh[4];
     const int b = blockIdx.x, tid = threadIdx.x;
-    int r0, rows, n = 0, cur = 0, emitted = 0;
-    int32_t *out = a.out_tokens + (int64_t)b * SS_OUT_WIDTH, *nodes = a.accepted_nodes + (int64_t)b * SS_MAX_DEPTH;
-    float *lp = a.logprobs ? a.logprobs + (int64_t)b * SS_OUT_WIDTH : nullptr;
-    if (rows_of(a, b, r0, rows)) {
-        for (;;) {
-            const Draw d = w.draw[r0 + cur];
-            if (tid == 0) {
-                out[emitted] = d.token;
-                if (lp) lp[emitted] = d.logprob;
-            }
-            ++emitted;
-            if (n == a.max_depth) break;
-            const int c = child_with(a, r0, rows, cur, d.token, sh);
-            if (c == 0x7fffffff) break;
-            if (tid == 0) nodes[n] = c;
-            ++n;
-            cur = c;
-        }
+    int r0, rows, n = 0, cur = 0;
+    clear_outputs(a, b);
+    if (!rows_of(a, b, r0, rows)) return;
+    __syncthreads();   // (outputs are one lane's from here on)
+    for (;;) {
+        const Draw d = w.draw[r0 + cur];
+        if (tid == 0) emit(a, b, n, d);
+        if (n == a.max_depth) break;
+        const int c = child_with(a, r0, rows, cur, d.token, sh);
+        if (c == 0x7fffffff) break;
+        if (tid == 0) a.accepted_nodes[(int64_t)b * SS_MAX_DEPTH + n] = c;
+        ++n;
+        cur = c;
     }
     if (tid == 0) a.accepted_len[b] = n;
-    if (tid < SS_OUT_WIDTH) {
-        if (tid >= emitted) {
-            out[tid] = -1;
-            if (lp) lp[tid] = 0.f;
-        }
-        if (tid < SS_MAX_DEPTH && tid >= n) nodes[tid] = -1;
+}
+
+// ---- many rows ---------------------------------------------------------------------------------------------------------
+// Round r: the draw at the node that round r - 1 has summed, the child, the sums of its row.  grid: batch * groups of `each` blocks
+template <int DT>
+__global__ __launch_bounds__(kThreads) void verify_round_kernel(TreeVerifyArgs a, VerifyWorkspace w, int r, int each)
+{
+    __shared__ ExpTable ex;
+    __shared__ DrawShared sh;
+    __shared__ float sh_m[4];
+    __shared__ double sh_s[4];
+    __shared__ int sh_c[4];
+    const int groups = (w.nsub + each - 1) / each, b = blockIdx.x / groups, group = blockIdx.x % groups;
+    const bool first = group == 0 && threadIdx.x == 0;   // whose the outputs are
+    Walk *walk = w.walk + (int64_t)(r & 1) * a.batch + b;
+    int r0, rows;
+    Walk at = {0, 0};
+    if (r == 0) {
+        if (group == 0) clear_outputs(a, b);
+        if (!rows_of(a, b, r0, rows)) at.cur = -1;
+    } else {
+        at = w.walk[(int64_t)((r - 1) & 1) * a.batch + b];
     }
+    if (at.cur < 0) {
+        if (first) *walk = at;
+        return;
+    }
+    if (r > 0) rows_of(a, b, r0, rows);
+    const double inv_t = inverse_temperature(a, b);
+    ex.init();
+    if (r > 0) {
+        const int64_t front = ((int64_t)((r - 1) & 1) * a.batch + b) * w.nsub;
+        const Draw d = draw_of<DT>(a, w.nsub, w.top + front, w.sum + front, r0 + at.cur, inv_t, ex, sh, sh_m, sh_s);
+        if (first) emit(a, b, at.n, d);
+        const int c = at.n < a.max_depth ? child_with(a, r0, rows, at.cur, d.token, sh_c) : 0x7fffffff;
+        if (c == 0x7fffffff) {
+            if (first) {
+                a.accepted_len[b] = at.n;
+                *walk = {-1, at.n};
+            }
+            return;
+        }
+        if (first) a.accepted_nodes[(int64_t)b * SS_MAX_DEPTH + at.n] = c;
+        at = {c, at.n + 1};
+    }
+    if (first) *walk = at;
+    const int64_t back = ((int64_t)(r & 1) * a.batch + b) * w.nsub;
+    for (int c = group * each; c < min(group * each + each, w.nsub); ++c)
+        block_sums<DT>(a, r0 + at.cur, c, inv_t, ex, w.top + back, w.sum + back, sh_m, sh_s);
+}
+
+// Whether all rows at once are the faster form.
+bool few_rows(int batch, int total_rows, int vocab, int max_depth)
+{
+    const double all = 11.0 + (double)total_rows * vocab / 1.1e6;
+    const double rounds = 8.0 + 10.0 * (max_depth < 4 ? max_depth + 1 : 5) + 3.0 * (max_depth < 4 ? 0 : max_depth - 4);
+    return all <= rounds;
+}
+
+__host__ VerifyWorkspace carve_verify(void *ws, int batch, int total_rows, int vocab, size_t *bytes)
+{
+    VerifyWorkspace w;
+    w.nsub = num_sub(vocab);
+    // (any max_depth's: a workspace serves them all)
+    const size_t rows = few_rows(batch, total_rows, vocab, SS_MAX_DEPTH) && total_rows > 2 * batch ? total_rows : 2 * (size_t)batch, n = rows * w.nsub;
+    char *p = static_cast<char *>(ws);
+    w.sum = reinterpret_cast<double *>(p); p += align_up(sizeof(double) * n, 256);
+    w.top = reinterpret_cast<float *>(p); p += align_up(sizeof(float) * n, 256);
+    w.draw = reinterpret_cast<Draw *>(p); p += align_up(sizeof(Draw) * rows, 256);
+    w.walk = reinterpret_cast<Walk *>(p); p += align_up(2 * sizeof(Walk) * (size_t)batch, 256);
+    *bytes = (size_t)(p - static_cast<char *>(ws)) + 256;
+    return w;
+}
+
+constexpr int kRoundWgs = 768;   // workgroups of a round: three to a compute unit
+
+template <int DT>
+int32_t launch(const TreeVerifyArgs &a, hipStream_t stream)
+{
+    size_t unused;
+    const VerifyWorkspace w = carve_verify(a.workspace, a.batch, a.total_rows, a.vocab, &unused);
+    const dim3 wg(kThreads);
+    if (few_rows(a.batch, a.total_rows, a.vocab, a.max_depth)) {
+        if (a.total_rows > 0) {
+            hipLaunchKernelGGL(verify_sums_kernel<DT>, dim3((unsigned)a.total_rows * (unsigned)w.nsub), wg, 0, stream, a, w);
+            hipLaunchKernelGGL(verify_draw_kernel<DT>, dim3((unsigned)a.total_rows), wg, 0, stream, a, w);
+        }
+        hipLaunchKernelGGL(verify_walk_kernel, dim3((unsigned)a.batch), wg, 0, stream, a, w);
+        SS_HIP_CHECK(hipGetLastError(), "launch tree_verify kernels");
+        return SS_OK;
+    }
+    const int64_t blocks = (int64_t)a.batch * w.nsub;
+    int each = (int)((blocks + kRoundWgs - 1) / kRoundWgs);
+    each = each < w.nsub ? each : w.nsub;
+    const unsigned groups = (unsigned)((w.nsub + each - 1) / each);
+    for (int r = 0; r <= a.max_depth; ++r) hipLaunchKernelGGL(verify_round_kernel<DT>, dim3(groups * (unsigned)a.batch), wg, 0, stream, a, w, r, each);
+    hipLaunchKernelGGL(verify_round_kernel<DT>, dim3((unsigned)a.batch), wg, 0, stream, a, w, a.max_depth + 1, w.nsub);   // (the draws at the deepest nodes)
+    SS_HIP_CHECK(hipGetLastError(), "launch verify_round_kernel");
+    return SS_OK;
 }
 
 }  // namespace
 
 int64_t tree_verify_workgroups(int batch, int total_rows, int vocab)
 {
-    const int64_t n = (int64_t)total_rows * num_sub(vocab);
+    const int64_t rows = few_rows(batch, total_rows, vocab, SS_MAX_DEPTH) ? total_rows : 0, n = rows * num_sub(vocab);
     return n > batch ? n : batch;
 }
 
 size_t tree_verify_workspace_bytes(int batch, int total_rows, int vocab)
 {
-    const size_t n = (size_t)total_rows * num_sub(vocab);
-    return align_up(sizeof(double) * n, 256) + align_up(sizeof(float) * n, 256) + align_up(sizeof(Draw) * (size_t)total_rows, 256) +
-           align_up(sizeof(int32_t) * (size_t)total_rows, 256) + 256;
+    size_t bytes;
+    carve_verify(nullptr, batch, total_rows, vocab, &bytes);
+    return bytes;
 }
 
 int32_t tree_verify_launch(const TreeVerifyArgs &a, hipStream_t stream)
 {
-    const VerifyWorkspace w = carve_verify(a.workspace, a.total_rows, a.vocab);
-    const dim3 wg(kThreads);
-    if (a.total_rows > 0) {
-        hipLaunchKernelGGL(verify_rows_kernel, dim3((unsigned)(a.total_rows + kThreads - 1) / kThreads), wg, 0, stream, a, w);
-        hipLaunchKernelGGL(verify_requests_kernel, dim3((unsigned)a.batch), wg, 0, stream, a, w);
-        const dim3 sums((unsigned)a.total_rows * (unsigned)w.nsub), rows((unsigned)a.total_rows);
-        if (a.logit_dtype == SS_BF16) {
-            hipLaunchKernelGGL(verify_sums_kernel<SS_BF16>, sums, wg, 0, stream, a, w);
-            hipLaunchKernelGGL(verify_draw_kernel<SS_BF16>, rows, wg, 0, stream, a, w);
-        } else {
-            hipLaunchKernelGGL(verify_sums_kernel<SS_F32>, sums, wg, 0, stream, a, w);
-            hipLaunchKernelGGL(verify_draw_kernel<SS_F32>, rows, wg, 0, stream, a, w);
-        }
-    }
-    hipLaunchKernelGGL(verify_walk_kernel, dim3((unsigned)a.batch), wg, 0, stream, a, w);
-    SS_HIP_CHECK(hipGetLastError(), "launch tree_verify kernels");
-    return SS_OK;
+    return a.logit_dtype == SS_BF16 ? launch<SS_BF16>(a, stream) : launch<SS_F32>(a, stream);
 }
 
 }  // namespace ss
