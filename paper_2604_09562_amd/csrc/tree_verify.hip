@@ -69,102 +69,198 @@ __device__ __forceinline__ bool rows_of(const TreeVerifyArgs &a, int b, int &r0,
     return r0 >= 0 && r1 > r0 && r1 <= a.total_rows;
 }
 
-// The sums of block c of a row.
-template <int DT>
-__device__ __forceinline__ void block_sums(const TreeVerifyArgs &a, int64_t row, int c, double inv_t, const ExpTable &ex, float *top, double *sum, float *sh_m, double *sh_s)
+// Sums and maxima over a wavefront, in every lane.
+__device__ __forceinline__ float wave_max(float x)
 {
-    Raw8<DT> raw;
-    float x[8];
-    load8<DT>(row_ptr(a.target, row, a.row_stride, DT), a.vocab, c * kSub + threadIdx.x * 8, raw);
-    unpack8<DT>(raw, x);
+    for (int off = 32; off; off >>= 1) x = fmaxf(x, __shfl_xor(x, off));
+    return x;
+}
+__device__ __forceinline__ int wave_min(int x)
+{
+    for (int off = 32; off; off >>= 1) x = min(x, __shfl_xor(x, off));
+    return x;
+}
+__device__ __forceinline__ double lane_of(double x, int lane)
+{
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), lane), __builtin_amdgcn_readlane(__double2loint(x), lane));
+}
+
+// The sums of block c of a row: a wavefront's, by itself.
+template <int DT>
+__device__ __forceinline__ void block_sums(const TreeVerifyArgs &a, int64_t row, int c, double inv_t, const ExpTable &ex, float *top, double *sum)
+{
+    constexpr int EACH = kSub / (64 * 8);
+    const int lane = threadIdx.x & 63;
+    const void *p = row_ptr(a.target, row, a.row_stride, DT);
+    Raw8<DT> raw[EACH];
+    if (c * kSub + kSub <= a.vocab) {   // (plain loads, all under way together)
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const uint4 *from = reinterpret_cast<const uint4 *>(static_cast<const char *>(p) + (int64_t)(c * kSub + i * 512 + lane * 8) * (DT == SS_BF16 ? 2 : 4));
+#pragma unroll
+            for (int j = 0; j < (DT == SS_BF16 ? 1 : 2); ++j) raw[i].w[j] = from[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) load8<DT>(p, a.vocab, c * kSub + i * 512 + lane * 8, raw[i]);
+    }
     float m = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = fmaxf(m, x[i]);   // (a NaN is masked)
-    m = block_max(m, sh_m);
+    for (int i = 0; i < EACH; ++i) {
+        float x[8];
+        unpack8<DT>(raw[i], x);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m = fmaxf(m, x[k]);   // (a NaN is masked)
+    }
+    m = wave_max(m);
     double s = 0.0;
     if (inv_t > 0.0) {
-        double e[8];
-        exp8(ex, DiffArg(inv_t, m), x, e);
+        const DiffArg arg(inv_t, m);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s += e[i];
-        s = block_sum(s, sh_s);
+        for (int i = 0; i < EACH; ++i) {
+            float x[8];
+            double e[8];
+            unpack8<DT>(raw[i], x);
+            exp8(ex, arg, x, e);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += e[k];
+        }
+        s = wave_scan(s);
     }
-    if (threadIdx.x == 0) {
+    if (lane == 63) {
         top[c] = m;
         sum[c] = s;
     }
 }
 
-// The lowest token of a row whose logit is m, the row's largest; in every lane of a workgroup.
-template <int DT>
-__device__ __forceinline__ int lowest_with(const TreeVerifyArgs &a, int nsub, const float *top, int row, float m, int *sh)
-{
-    auto least = [&](int x) {
-        for (int off = 32; off; off >>= 1) x = min(x, __shfl_xor(x, off));
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
-        __syncthreads();
-        return min(min(sh[0], sh[1]), min(sh[2], sh[3]));
-    };
-    int c = 0x7fffffff;
-    for (int i = threadIdx.x; i < nsub; i += kThreads)
-        if (top[i] == m) { c = i; break; }
-    c = least(c);
-    Raw8<DT> raw;
-    float x[8];
-    const int i0 = c * kSub + threadIdx.x * 8;
-    load8<DT>(row_ptr(a.target, row, a.row_stride, DT), a.vocab, i0, raw);
-    unpack8<DT>(raw, x);
-    int y = 0x7fffffff;
-#pragma unroll
-    for (int i = 7; i >= 0; --i)
-        if (x[i] == m) y = i0 + i;
-    return least(y);
-}
+struct DrawLds {
+    double entry[4];
+    int last[4], first[4], tok, child[4];
+};
 
-// The token of a row, in every lane of a workgroup.
+// The token of a row, in every lane of a workgroup.  Every wavefront scans the blocks for itself, a lane a run of them; the entries of the block are the workgroup's.
 template <int DT>
-__device__ Draw draw_of(const TreeVerifyArgs &a, int nsub, const float *top, const double *sum, int row, double inv_t, const ExpTable &ex, DrawShared &sh, float *sh_m, double *sh_s)
+__device__ Draw draw_of(const TreeVerifyArgs &a, int nsub, const float *top, const double *sum, int row, double inv_t, const ExpTable &ex, DrawLds &sh)
 {
-    float m = -INFINITY;
-    for (int c = threadIdx.x; c < nsub; c += kThreads) m = fmaxf(m, top[c]);
-    m = block_max(m, sh_m);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int per = (nsub + 63) / 64, c0 = lane * per, c1 = min(c0 + per, nsub);
+    const void *p = row_ptr(a.target, row, a.row_stride, DT);
+    const float u = inv_t > 0.0 ? a.uniforms[row] : 0.f;
+    float own_top = -INFINITY;
+    for (int c = c0; c < c1; ++c) own_top = fmaxf(own_top, top[c]);
+    const float m = wave_max(own_top);
+    auto entries = [&](int c, float (&x)[8]) {
+        Raw8<DT> raw;
+        load8<DT>(p, a.vocab, c * kSub + tid * 8, raw);
+        unpack8<DT>(raw, x);
+    };
     Draw d = {-1, 0.f};
     if (inv_t > 0.0 && m < INFINITY && m > -INFINITY) {
         const DiffArg arg(inv_t, m);
         auto mass_of = [&](int c) { return top[c] == -INFINITY ? 0.0 : sum[c] * ex(arg(top[c])); };
-        double part = 0.0;
-        for (int c = threadIdx.x; c < nsub; c += kThreads) part += mass_of(c);
-        const double all = block_sum(part, sh_s);
-        __syncthreads();
-        const void *p = row_ptr(a.target, row, a.row_stride, DT);
-        d.token = draw_token(nsub, a.uniforms[row], sh, mass_of, [&](int c, double (&r)[kSubPer]) {
-            Raw8<DT> raw;
-            float x[8];
-            load8<DT>(p, a.vocab, c * kSub + threadIdx.x * 8, raw);
-            unpack8<DT>(raw, x);
-            exp8(ex, DiffArg(inv_t, top[c]), x, r);
-            const double level = ex(arg(top[c]));
+        double own = 0.0;
+        int own_last = -1;   // last block of this lane with mass
+        for (int c = c0; c < c1; ++c) {
+            const double v = mass_of(c);
+            own += v;
+            if (v > 0.0) own_last = c;
+        }
+        const double cum = wave_scan(own), all = lane_of(cum, 63), thr = (double)u * all;
+        const uint64_t over = __ballot(own > 0.0 && cum > thr), some = __ballot(own > 0.0);   // (there is mass: the block of the largest logit has)
+        const bool take_last = over == 0;   // rounding left u times the sum at or past it: the last entry with mass
+        const int owner = take_last ? 63 - __builtin_clzll(some) : __builtin_ctzll(over);
+        double pre = cum - own;
+        int cs = own_last;
+        if (per > 1 && lane == owner) {   // inside the lane's run: the first with mass whose running sum crosses (rounding may leave none: then the last with mass)
+            double run = pre;
+            bool found = false;
+            for (int c = c0; c < c1; ++c) {
+                const double v = mass_of(c);
+                if (v > 0.0 && !found) {
+                    cs = c;
+                    pre = run;
+                    found = !take_last && run + v > thr;
+                }
+                run += v;
+            }
+        }
+        const int block = __builtin_amdgcn_readlane(cs, owner);
+        const double prefix = lane_of(pre, owner);
+        float x[8];
+        double r[8];
+        entries(block, x);
+        exp8(ex, DiffArg(inv_t, top[block]), x, r);
+        const double level = ex(arg(top[block]));
+        double local = 0.0;
+        int my_last = -1;
 #pragma unroll
-            for (int i = 0; i < kSubPer; ++i) r[i] *= level;
-        });
-        if (d.token >= 0) d.logprob = (float)(((double)load_logit(a.target, row, a.row_stride, DT, d.token) - (double)m) * inv_t - log(all));
+        for (int i = 0; i < 8; ++i) {
+            r[i] *= level;
+            local += r[i];
+            if (r[i] > 0.0) my_last = i;
+        }
+        const double incl = wave_scan(local);
+        const uint64_t mass = __ballot(my_last >= 0);
+        if (lane == 63) sh.entry[wave] = incl;
+        if (lane == 0) sh.last[wave] = mass ? wave * 64 + 63 - __builtin_clzll(mass) : -1;
+        __syncthreads();
+        double before = prefix;
+        for (int w = 0; w < wave; ++w) before += sh.entry[w];
+        const double excl = before + (incl - local);
+        // (the scan groups its additions differently for every lane, so the sum at a lane without mass may lie an ulp above that of the lane in front of it)
+        const uint64_t bal = __ballot(!take_last && local > 0.0 && excl + local > thr);
+        if (lane == 0) sh.first[wave] = bal ? wave * 64 + __builtin_ctzll(bal) : 0x7fffffff;
+        __syncthreads();
+        const int first = min(min(sh.first[0], sh.first[1]), min(sh.first[2], sh.first[3]));
+        const int at = first != 0x7fffffff ? first : max(max(sh.last[0], sh.last[1]), max(sh.last[2], sh.last[3]));
+        if (tid == at) {
+            double c = excl;
+            int y = -1;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (r[i] > 0.0) {
+                    c += r[i];
+                    if (first != 0x7fffffff && y < 0 && c > thr) y = i;
+                }
+            y = y >= 0 ? y : my_last;   // (the lane's total crossed but the sum entry by entry may round differently: its last entry with mass)
+            sh.tok = block * kSub + tid * 8 + y;
+        }
+        __syncthreads();
+        d.token = sh.tok;
+        d.logprob = (float)(((double)load_logit(a.target, row, a.row_stride, DT, d.token) - (double)m) * inv_t - log(all));
+        return d;
     }
-    if (d.token < 0) d.token = m > -INFINITY ? lowest_with<DT>(a, nsub, top, row, m, sh.first) : 0;
+    d.token = 0;
+    if (m > -INFINITY) {   // the lowest token whose logit is the largest
+        int c = 0x7fffffff;
+        for (int i = c0; i < c1; ++i)
+            if (top[i] == m) { c = i; break; }
+        c = wave_min(c);
+        float x[8];
+        entries(c, x);
+        int y = 0x7fffffff;
+#pragma unroll
+        for (int i = 7; i >= 0; --i)
+            if (x[i] == m) y = c * kSub + tid * 8 + i;
+        y = wave_min(y);
+        if (lane == 0) sh.first[wave] = y;
+        __syncthreads();
+        d.token = min(min(sh.first[0], sh.first[1]), min(sh.first[2], sh.first[3]));
+    }
     return d;
 }
 
 // The lowest child of node cur that carries token y, INT_MAX if there is none; in every lane of a workgroup.
-__device__ __forceinline__ int child_with(const TreeVerifyArgs &a, int r0, int rows, int cur, int y, int *sh)
+__device__ __forceinline__ int child_with(const TreeVerifyArgs &a, int r0, int rows, int cur, int y, DrawLds &sh)
 {
     int c = 0x7fffffff;
     for (int i = cur + 1 + threadIdx.x; i < rows; i += kThreads)
         if (a.parent[r0 + i] == cur && a.tokens[r0 + i] == y) { c = i; break; }
-    for (int off = 32; off; off >>= 1) c = min(c, __shfl_xor(c, off));
+    c = wave_min(c);
+    __syncthreads();   // (a step in front may still read)
+    if ((threadIdx.x & 63) == 0) sh.child[threadIdx.x >> 6] = c;
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = c;
-    __syncthreads();
-    return min(min(sh[0], sh[1]), min(sh[2], sh[3]));
+    return min(min(sh.child[0], sh.child[1]), min(sh.child[2], sh.child[3]));
 }
 
 // What a request has before anything is drawn; whether it has rows.
@@ -201,18 +297,16 @@ __device__ __forceinline__ int request_of(const TreeVerifyArgs &a, int row, int 
     return at == 0x7fffffff ? -1 : at;
 }
 
-// grid: rows * blocks
+// grid: rows * fours of blocks
 template <int DT>
 __global__ __launch_bounds__(kThreads) void verify_sums_kernel(TreeVerifyArgs a, VerifyWorkspace w)
 {
     __shared__ ExpTable ex;
-    __shared__ float sh_m[4];
-    __shared__ double sh_s[4];
     __shared__ int sh_b[4];
-    const int row = blockIdx.x / w.nsub, c = blockIdx.x % w.nsub, b = request_of(a, row, sh_b);
+    const int fours = (w.nsub + 3) / 4, row = blockIdx.x / fours, c = blockIdx.x % fours * 4 + (threadIdx.x >> 6), b = request_of(a, row, sh_b);
     if (b < 0) return;
     ex.init();
-    block_sums<DT>(a, row, c, inverse_temperature(a, b), ex, w.top + (int64_t)row * w.nsub, w.sum + (int64_t)row * w.nsub, sh_m, sh_s);
+    if (c < w.nsub) block_sums<DT>(a, row, c, inverse_temperature(a, b), ex, w.top + (int64_t)row * w.nsub, w.sum + (int64_t)row * w.nsub);
 }
 
 // grid: rows
@@ -220,21 +314,19 @@ template <int DT>
 __global__ __launch_bounds__(kThreads) void verify_draw_kernel(TreeVerifyArgs a, VerifyWorkspace w)
 {
     __shared__ ExpTable ex;
-    __shared__ DrawShared sh;
-    __shared__ float sh_m[4];
-    __shared__ double sh_s[4];
+    __shared__ DrawLds sh;
     __shared__ int sh_b[4];
     const int row = blockIdx.x, b = request_of(a, row, sh_b);
     if (b < 0) return;
     ex.init();
-    const Draw d = draw_of<DT>(a, w.nsub, w.top + (int64_t)row * w.nsub, w.sum + (int64_t)row * w.nsub, row, inverse_temperature(a, b), ex, sh, sh_m, sh_s);
+    const Draw d = draw_of<DT>(a, w.nsub, w.top + (int64_t)row * w.nsub, w.sum + (int64_t)row * w.nsub, row, inverse_temperature(a, b), ex, sh);
     if (threadIdx.x == 0) w.draw[row] = d;
 }
 
 // grid: batch
 __global__ __launch_bounds__(kThreads) void verify_walk_kernel(TreeVerifyArgs a, VerifyWorkspace w)
 {
-    __shared__ int sh[4];
+    __shared__ DrawLds sh;
     const int b = blockIdx.x, tid = threadIdx.x;
     int r0, rows, n = 0, cur = 0;
     clear_outputs(a, b);
@@ -254,16 +346,13 @@ __global__ __launch_bounds__(kThreads) void verify_walk_kernel(TreeVerifyArgs a,
 }
 
 // ---- many rows ---------------------------------------------------------------------------------------------------------
-// Round r: the draw at the node that round r - 1 has summed, the child, the sums of its row.  grid: batch * groups of `each` blocks
+// Round r: the draw at the node that round r - 1 has summed, the child, the sums of its row.  grid: batch * groups of 4 `each` blocks
 template <int DT>
 __global__ __launch_bounds__(kThreads) void verify_round_kernel(TreeVerifyArgs a, VerifyWorkspace w, int r, int each)
 {
     __shared__ ExpTable ex;
-    __shared__ DrawShared sh;
-    __shared__ float sh_m[4];
-    __shared__ double sh_s[4];
-    __shared__ int sh_c[4];
-    const int groups = (w.nsub + each - 1) / each, b = blockIdx.x / groups, group = blockIdx.x % groups;
+    __shared__ DrawLds sh;
+    const int groups = (w.nsub + 4 * each - 1) / (4 * each), b = blockIdx.x / groups, group = blockIdx.x % groups;
     const bool first = group == 0 && threadIdx.x == 0;   // whose the outputs are
     Walk *walk = w.walk + (int64_t)(r & 1) * a.batch + b;
     int r0, rows;
@@ -283,9 +372,9 @@ __global__ __launch_bounds__(kThreads) void verify_round_kernel(TreeVerifyArgs a
     ex.init();
     if (r > 0) {
         const int64_t front = ((int64_t)((r - 1) & 1) * a.batch + b) * w.nsub;
-        const Draw d = draw_of<DT>(a, w.nsub, w.top + front, w.sum + front, r0 + at.cur, inv_t, ex, sh, sh_m, sh_s);
+        const Draw d = draw_of<DT>(a, w.nsub, w.top + front, w.sum + front, r0 + at.cur, inv_t, ex, sh);
         if (first) emit(a, b, at.n, d);
-        const int c = at.n < a.max_depth ? child_with(a, r0, rows, at.cur, d.token, sh_c) : 0x7fffffff;
+        const int c = at.n < a.max_depth ? child_with(a, r0, rows, at.cur, d.token, sh) : 0x7fffffff;
         if (c == 0x7fffffff) {
             if (first) {
                 a.accepted_len[b] = at.n;
@@ -298,8 +387,10 @@ __global__ __launch_bounds__(kThreads) void verify_round_kernel(TreeVerifyArgs a
     }
     if (first) *walk = at;
     const int64_t back = ((int64_t)(r & 1) * a.batch + b) * w.nsub;
-    for (int c = group * each; c < min(group * each + each, w.nsub); ++c)
-        block_sums<DT>(a, r0 + at.cur, c, inv_t, ex, w.top + back, w.sum + back, sh_m, sh_s);
+    for (int i = 0; i < each; ++i) {
+        const int c = (group * each + i) * 4 + (threadIdx.x >> 6);
+        if (c < w.nsub) block_sums<DT>(a, r0 + at.cur, c, inv_t, ex, w.top + back, w.sum + back);
+    }
 }
 
 // Whether all rows at once are the faster form.
@@ -325,7 +416,7 @@ __host__ VerifyWorkspace carve_verify(void *ws, int batch, int total_rows, int v
     return w;
 }
 
-constexpr int kRoundWgs = 768;   // workgroups of a round: three to a compute unit
+constexpr int kRoundWgs = 1280;   // workgroups of a round: five to a compute unit, as many as it runs at a time
 
 template <int DT>
 int32_t launch(const TreeVerifyArgs &a, hipStream_t stream)
@@ -335,19 +426,20 @@ int32_t launch(const TreeVerifyArgs &a, hipStream_t stream)
     const dim3 wg(kThreads);
     if (few_rows(a.batch, a.total_rows, a.vocab, a.max_depth)) {
         if (a.total_rows > 0) {
-            hipLaunchKernelGGL(verify_sums_kernel<DT>, dim3((unsigned)a.total_rows * (unsigned)w.nsub), wg, 0, stream, a, w);
+            hipLaunchKernelGGL(verify_sums_kernel<DT>, dim3((unsigned)a.total_rows * (unsigned)((w.nsub + 3) / 4)), wg, 0, stream, a, w);
             hipLaunchKernelGGL(verify_draw_kernel<DT>, dim3((unsigned)a.total_rows), wg, 0, stream, a, w);
         }
         hipLaunchKernelGGL(verify_walk_kernel, dim3((unsigned)a.batch), wg, 0, stream, a, w);
         SS_HIP_CHECK(hipGetLastError(), "launch tree_verify kernels");
         return SS_OK;
     }
-    const int64_t blocks = (int64_t)a.batch * w.nsub;
-    int each = (int)((blocks + kRoundWgs - 1) / kRoundWgs);
-    each = each < w.nsub ? each : w.nsub;
-    const unsigned groups = (unsigned)((w.nsub + each - 1) / each);
+    const int fours = (w.nsub + 3) / 4;
+    const int64_t all = (int64_t)a.batch * fours;
+    int each = (int)((all + kRoundWgs - 1) / kRoundWgs);
+    each = each < fours ? each : fours;
+    const unsigned groups = (unsigned)((fours + each - 1) / each);
     for (int r = 0; r <= a.max_depth; ++r) hipLaunchKernelGGL(verify_round_kernel<DT>, dim3(groups * (unsigned)a.batch), wg, 0, stream, a, w, r, each);
-    hipLaunchKernelGGL(verify_round_kernel<DT>, dim3((unsigned)a.batch), wg, 0, stream, a, w, a.max_depth + 1, w.nsub);   // (the draws at the deepest nodes)
+    hipLaunchKernelGGL(verify_round_kernel<DT>, dim3((unsigned)a.batch), wg, 0, stream, a, w, a.max_depth + 1, fours);   // (the draws at the deepest nodes)
     SS_HIP_CHECK(hipGetLastError(), "launch verify_round_kernel");
     return SS_OK;
 }
