@@ -136,11 +136,19 @@ __device__ __forceinline__ void block_sums(const TreeVerifyArgs &a, int64_t row,
 struct DrawLds {
     double entry[4];
     int last[4], first[4], tok, child[4];
+    float x;
+};
+// A drawn token, and what its log-probability is made of.
+struct Drawn {
+    int token;
+    float x, m;     // its logit, the row's largest
+    double all;     // the sum of the exponentials, 0 if the token was not drawn from a distribution
+    __device__ Draw result(double inv_t) const { return {token, all > 0.0 ? (float)(((double)x - (double)m) * inv_t - log(all)) : 0.f}; }
 };
 
 // The token of a row, in every lane of a workgroup.  Every wavefront scans the blocks for itself, a lane a run of them; the entries of the block are the workgroup's.
 template <int DT>
-__device__ Draw draw_of(const TreeVerifyArgs &a, int nsub, const float *top, const double *sum, int row, double inv_t, const ExpTable &ex, DrawLds &sh)
+__device__ Drawn draw_of(const TreeVerifyArgs &a, int nsub, const float *top, const double *sum, int row, double inv_t, const ExpTable &ex, DrawLds &sh)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int per = (nsub + 63) / 64, c0 = lane * per, c1 = min(c0 + per, nsub);
@@ -154,7 +162,7 @@ __device__ Draw draw_of(const TreeVerifyArgs &a, int nsub, const float *top, con
         load8<DT>(p, a.vocab, c * kSub + tid * 8, raw);
         unpack8<DT>(raw, x);
     };
-    Draw d = {-1, 0.f};
+    Drawn d = {0, 0.f, m, 0.0};
     if (inv_t > 0.0 && m < INFINITY && m > -INFINITY) {
         const DiffArg arg(inv_t, m);
         auto mass_of = [&](int c) { return top[c] == -INFINITY ? 0.0 : sum[c] * ex(arg(top[c])); };
@@ -224,13 +232,16 @@ __device__ Draw draw_of(const TreeVerifyArgs &a, int nsub, const float *top, con
                 }
             y = y >= 0 ? y : my_last;   // (the lane's total crossed but the sum entry by entry may round differently: its last entry with mass)
             sh.tok = block * kSub + tid * 8 + y;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i == y) sh.x = x[i];
         }
         __syncthreads();
         d.token = sh.tok;
-        d.logprob = (float)(((double)load_logit(a.target, row, a.row_stride, DT, d.token) - (double)m) * inv_t - log(all));
+        d.x = sh.x;
+        d.all = all;
         return d;
     }
-    d.token = 0;
     if (m > -INFINITY) {   // the lowest token whose logit is the largest
         int c = 0x7fffffff;
         for (int i = c0; i < c1; ++i)
@@ -250,12 +261,22 @@ __device__ Draw draw_of(const TreeVerifyArgs &a, int nsub, const float *top, con
     return d;
 }
 
-// The lowest child of node cur that carries token y, INT_MAX if there is none; in every lane of a workgroup.
-__device__ __forceinline__ int child_with(const TreeVerifyArgs &a, int r0, int rows, int cur, int y, DrawLds &sh)
+// The lowest child of node cur that carries token y, INT_MAX if there is none; in every lane of a workgroup.  A lane's first node behind cur has been asked for before the draw.
+struct Candidate {
+    int parent, token;
+};
+__device__ __forceinline__ Candidate candidate(const TreeVerifyArgs &a, int r0, int rows, int cur)
 {
-    int c = 0x7fffffff;
-    for (int i = cur + 1 + threadIdx.x; i < rows; i += kThreads)
-        if (a.parent[r0 + i] == cur && a.tokens[r0 + i] == y) { c = i; break; }
+    const int i = cur + 1 + threadIdx.x;
+    return i < rows ? Candidate{a.parent[r0 + i], a.tokens[r0 + i]} : Candidate{-1, -1};
+}
+__device__ __forceinline__ int child_with(const TreeVerifyArgs &a, const Candidate &mine, int r0, int rows, int cur, int y, DrawLds &sh)
+{
+    int c = 0x7fffffff, i = cur + 1 + threadIdx.x;
+    if (mine.parent == cur && mine.token == y) c = i;
+    else
+        for (i += kThreads; i < rows; i += kThreads)
+            if (a.parent[r0 + i] == cur && a.tokens[r0 + i] == y) { c = i; break; }
     c = wave_min(c);
     __syncthreads();   // (a step in front may still read)
     if ((threadIdx.x & 63) == 0) sh.child[threadIdx.x >> 6] = c;
@@ -319,8 +340,9 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(TreeVerifyArgs a,
     const int row = blockIdx.x, b = request_of(a, row, sh_b);
     if (b < 0) return;
     ex.init();
-    const Draw d = draw_of<DT>(a, w.nsub, w.top + (int64_t)row * w.nsub, w.sum + (int64_t)row * w.nsub, row, inverse_temperature(a, b), ex, sh);
-    if (threadIdx.x == 0) w.draw[row] = d;
+    const double inv_t = inverse_temperature(a, b);
+    const Drawn d = draw_of<DT>(a, w.nsub, w.top + (int64_t)row * w.nsub, w.sum + (int64_t)row * w.nsub, row, inv_t, ex, sh);
+    if (threadIdx.x == 0) w.draw[row] = d.result(inv_t);
 }
 
 // grid: batch
@@ -336,7 +358,7 @@ __global__ __launch_bounds__(kThreads) void verify_walk_kernel(TreeVerifyArgs a,
         const Draw d = w.draw[r0 + cur];
         if (tid == 0) emit(a, b, n, d);
         if (n == a.max_depth) break;
-        const int c = child_with(a, r0, rows, cur, d.token, sh);
+        const int c = child_with(a, candidate(a, r0, rows, cur), r0, rows, cur, d.token, sh);
         if (c == 0x7fffffff) break;
         if (tid == 0) a.accepted_nodes[(int64_t)b * SS_MAX_DEPTH + n] = c;
         ++n;
@@ -356,34 +378,37 @@ __global__ __launch_bounds__(kThreads) void verify_round_kernel(TreeVerifyArgs a
     const bool first = group == 0 && threadIdx.x == 0;   // whose the outputs are
     Walk *walk = w.walk + (int64_t)(r & 1) * a.batch + b;
     int r0, rows;
-    Walk at = {0, 0};
+    const bool has = rows_of(a, b, r0, rows);
+    const double inv_t = inverse_temperature(a, b);
+    Walk at = {has ? 0 : -1, 0};
     if (r == 0) {
         if (group == 0) clear_outputs(a, b);
-        if (!rows_of(a, b, r0, rows)) at.cur = -1;
     } else {
         at = w.walk[(int64_t)((r - 1) & 1) * a.batch + b];
     }
+    ex.init();
     if (at.cur < 0) {
         if (first) *walk = at;
         return;
     }
-    if (r > 0) rows_of(a, b, r0, rows);
-    const double inv_t = inverse_temperature(a, b);
-    ex.init();
+    Drawn d = {};
+    int n = -1;   // whose draw that is
     if (r > 0) {
         const int64_t front = ((int64_t)((r - 1) & 1) * a.batch + b) * w.nsub;
-        const Draw d = draw_of<DT>(a, w.nsub, w.top + front, w.sum + front, r0 + at.cur, inv_t, ex, sh);
-        if (first) emit(a, b, at.n, d);
-        const int c = at.n < a.max_depth ? child_with(a, r0, rows, at.cur, d.token, sh) : 0x7fffffff;
+        const Candidate mine = candidate(a, r0, rows, at.cur);
+        n = at.n;
+        d = draw_of<DT>(a, w.nsub, w.top + front, w.sum + front, r0 + at.cur, inv_t, ex, sh);
+        const int c = n < a.max_depth ? child_with(a, mine, r0, rows, at.cur, d.token, sh) : 0x7fffffff;
         if (c == 0x7fffffff) {
             if (first) {
-                a.accepted_len[b] = at.n;
-                *walk = {-1, at.n};
+                emit(a, b, n, d.result(inv_t));
+                a.accepted_len[b] = n;
+                *walk = {-1, n};
             }
             return;
         }
-        if (first) a.accepted_nodes[(int64_t)b * SS_MAX_DEPTH + at.n] = c;
-        at = {c, at.n + 1};
+        if (first) a.accepted_nodes[(int64_t)b * SS_MAX_DEPTH + n] = c;
+        at = {c, n + 1};
     }
     if (first) *walk = at;
     const int64_t back = ((int64_t)(r & 1) * a.batch + b) * w.nsub;
@@ -391,6 +416,7 @@ __global__ __launch_bounds__(kThreads) void verify_round_kernel(TreeVerifyArgs a
         const int c = (group * each + i) * 4 + (threadIdx.x >> 6);
         if (c < w.nsub) block_sums<DT>(a, r0 + at.cur, c, inv_t, ex, w.top + back, w.sum + back);
     }
+    if (first && n >= 0) emit(a, b, n, d.result(inv_t));
 }
 
 // Whether all rows at once are the faster form.
