@@ -525,7 +525,7 @@ int32_t ss_block_fork(const ss_batch *batch, const ss_block_pool *pool, int32_t 
  *   status      device int32 [1]: 0; s < 0: request -1-s has impossible lengths (kv_len or held below 0, held beyond the table's columns), s = -1-batch: the free
  *               list's length is.  Then nothing else changed
  */
-size_t ss_block_release_workspace(int32_t batch, int32_t max_blocks_per_seq);
+size_t ss_block_release_workspace(int32_t batch, int32_t max_blocks_per_seq, int32_t num_blocks);
 int32_t ss_block_release(const ss_batch *batch, const ss_block_pool *pool, int32_t *shares, int32_t *held, int32_t *status, void *workspace,
                          size_t workspace_bytes, void *stream);
 

@@ -147,7 +147,7 @@ def lib() -> ctypes.CDLL:
             fn = getattr(L, name)
             fn.restype, fn.argtypes = i32, args
         for name, args in (("ss_tree_attn_workspace", [kv_p, batch_p, i32, i32, i32]), ("ss_tree_verify_workspace", [i32] * 3),
-                           ("ss_block_fork_workspace", [i32] * 2), ("ss_block_release_workspace", [i32] * 2), ("ss_block_compact_workspace", [i32])):
+                           ("ss_block_fork_workspace", [i32] * 2), ("ss_block_release_workspace", [i32] * 3), ("ss_block_compact_workspace", [i32])):
             fn = getattr(L, name)
             fn.restype, fn.argtypes = size, args
         L.ss_kv_commit.argtypes = [ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
@@ -494,11 +494,9 @@ def alloc_tree_verify_outputs(d: Dict[str, object], device="cuda:0"):
 
 
 def _books(d: Dict[str, object]):
-    """Descriptors of a batch's table and of its cache's free blocks, looked at each time: these calls write where they point."""
-    B, W, N = d["batch"], d["max_blocks_per_seq"], d["num_blocks"]
-    kv_len = d.get("kv_len")
-    bt = ss_batch(B, W, 0, 0, _ints("block_table", d["block_table"], B * W), 0 if kv_len is None else _ints("kv_len", kv_len, B), 0, 0)
-    return bt, ss_block_pool(N, _ints("free_ids", d["free_ids"], N), _ints("free_count", d["free_count"], 1))
+    """Descriptors of a batch's table and of its cache's free blocks, which are looked at where their workspace is allocated."""
+    bt = ss_batch(d["batch"], d["max_blocks_per_seq"], 0, 0, d["block_table"].data_ptr(), d["kv_len"].data_ptr(), 0, 0)
+    return bt, ss_block_pool(d["num_blocks"], d["free_ids"].data_ptr(), d["free_count"].data_ptr())
 
 
 def ss_block_fork(d: Dict[str, object], parent: torch.Tensor, child: torch.Tensor, length: Optional[torch.Tensor], copy_src: torch.Tensor,
@@ -507,7 +505,7 @@ def ss_block_fork(d: Dict[str, object], parent: torch.Tensor, child: torch.Tenso
     place, and the blocks that ss_block_copy is to copy."""
     bt, pool = _books(d)
     n = parent.numel()
-    _check(lib().ss_block_fork(ctypes.byref(bt), ctypes.byref(pool), _ints("shares", d["shares"], d["num_blocks"]), _ints("held", d["held"], d["batch"]), n,
+    _check(lib().ss_block_fork(ctypes.byref(bt), ctypes.byref(pool), d["shares"].data_ptr(), d["held"].data_ptr(), n,
                                _ints("parent", parent, n), _ints("child", child, n), 0 if length is None else _ints("length", length, n),
                                _ints("copy_src", copy_src, n), _ints("copy_dst", copy_dst, n), _ints("status", status, 1), workspace.data_ptr(),
                                workspace.nbytes, _stream()))
@@ -516,7 +514,7 @@ def ss_block_fork(d: Dict[str, object], parent: torch.Tensor, child: torch.Tenso
 def ss_block_release(d: Dict[str, object], status: torch.Tensor, workspace: torch.Tensor) -> None:
     """Enqueue the return of what requests hold beyond their `kv_len`: `held`, `shares`, `free_ids` and `free_count` in place."""
     bt, pool = _books(d)
-    _check(lib().ss_block_release(ctypes.byref(bt), ctypes.byref(pool), _ints("shares", d["shares"], d["num_blocks"]), _ints("held", d["held"], d["batch"]),
+    _check(lib().ss_block_release(ctypes.byref(bt), ctypes.byref(pool), d["shares"].data_ptr(), d["held"].data_ptr(),
                                   _ints("status", status, 1), workspace.data_ptr(), workspace.nbytes, _stream()))
 
 
@@ -525,14 +523,18 @@ def ss_block_compact(d: Dict[str, object], remap: Optional[torch.Tensor], copy_s
     """Enqueue the renumbering of the blocks in use to the front of the cache (`block_table`, `shares` and `free_ids` in place), and what ss_block_copy is to copy."""
     bt, pool = _books(d)
     N, shares = d["num_blocks"], d["shares"]
-    _check(lib().ss_block_compact(ctypes.byref(bt), ctypes.byref(pool), 0 if shares is None else _ints("shares", shares, N), _ints("held", d["held"], d["batch"]),
+    _check(lib().ss_block_compact(ctypes.byref(bt), ctypes.byref(pool), _ptr(shares), d["held"].data_ptr(),
                                   0 if remap is None else _ints("remap", remap, N), _ints("copy_src", copy_src, N // 2), _ints("copy_dst", copy_dst, N // 2),
                                   _ints("num_copies", num_copies, 1), _ints("status", status, 1), workspace.data_ptr(), workspace.nbytes, _stream()))
 
 
 def alloc_block_share_workspace(d: Dict[str, object], device="cuda:0", num_forks: int = 0) -> torch.Tensor:
-    """A workspace that ss_block_fork (of up to num_forks), ss_block_release and ss_block_compact can take in turn."""
-    sizes = (lib().ss_block_fork_workspace(d["batch"], num_forks), lib().ss_block_release_workspace(d["batch"], d["max_blocks_per_seq"]),
+    """A workspace that ss_block_fork (of up to num_forks), ss_block_release and ss_block_compact can take in turn, for a batch whose arrays are looked at here."""
+    B, N = d["batch"], d["num_blocks"]
+    for name, n in (("block_table", B * d["max_blocks_per_seq"]), ("kv_len", B), ("held", B), ("shares", N if d["shares"] is not None else 0), ("free_ids", N), ("free_count", 1)):
+        if d[name] is not None:
+            _ints(name, d[name], n)
+    sizes = (lib().ss_block_fork_workspace(d["batch"], num_forks), lib().ss_block_release_workspace(d["batch"], d["max_blocks_per_seq"], d["num_blocks"]),
              lib().ss_block_compact_workspace(d["num_blocks"]))
     if 0 in sizes:
         raise SpecVerifyError(lib().ss_last_error().decode())

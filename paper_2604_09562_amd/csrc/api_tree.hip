@@ -138,8 +138,7 @@ int32_t ss_tree_verify(int32_t batch, int32_t vocab, int64_t row_stride, int32_t
         return fail(SS_ERR_INVALID_ARG, "uniforms are required unless the temperature of all requests is 0");
     if (!aligned16(target_logits) || row_stride * (logit_dtype == SS_F32 ? 4 : 2) % 16)
         return fail(SS_ERR_INVALID_ARG, "logits rows must start 16-byte aligned (base and row_stride)");
-    if (tree_verify_workgroups(batch, total_rows, vocab) > (1 << 24) - 1)
-        return fail(SS_ERR_UNSUPPORTED, "total_rows * vocab too large for one launch");
+    if (batch >= 1 << 24) return fail(SS_ERR_UNSUPPORTED, "batch too large for one launch");
     const int32_t rc = check_workspace(workspace, workspace_bytes, tree_verify_workspace_bytes(batch, total_rows, vocab));
     if (rc != SS_OK) return rc;
     TreeVerifyArgs a{};
@@ -180,13 +179,13 @@ int32_t ss_block_fork(const ss_batch *batch, const ss_block_pool *pool, int32_t 
     return block_fork_launch(a, static_cast<hipStream_t>(stream));
 }
 
-size_t ss_block_release_workspace(int32_t batch, int32_t max_blocks_per_seq)
+size_t ss_block_release_workspace(int32_t batch, int32_t max_blocks_per_seq, int32_t num_blocks)
 {
-    if (batch < 0 || max_blocks_per_seq < 0) {
-        fail(SS_ERR_INVALID_ARG, "negative batch or max_blocks_per_seq");
+    if (batch < 0 || max_blocks_per_seq < 0 || num_blocks < 0) {
+        fail(SS_ERR_INVALID_ARG, "negative batch, max_blocks_per_seq or num_blocks");
         return 0;
     }
-    return align_up(block_release_scratch_ints(batch, max_blocks_per_seq) * sizeof(int32_t), 256);
+    return align_up(block_release_scratch_ints(batch, max_blocks_per_seq, num_blocks) * sizeof(int32_t), 256);
 }
 
 int32_t ss_block_release(const ss_batch *batch, const ss_block_pool *pool, int32_t *shares, int32_t *held, int32_t *status, void *workspace,
@@ -196,7 +195,7 @@ int32_t ss_block_release(const ss_batch *batch, const ss_block_pool *pool, int32
     if (rc != SS_OK) return rc;
     if (!status || !pool_pointers(pool) || (pool->num_blocks > 0 && !shares) || (batch->batch > 0 && (!batch->block_table || !batch->kv_len || !held)))
         return fail(SS_ERR_INVALID_ARG, "a required device pointer is NULL");
-    if ((rc = check_workspace(workspace, workspace_bytes, ss_block_release_workspace(batch->batch, batch->max_blocks_per_seq))) != SS_OK) return rc;
+    if ((rc = check_workspace(workspace, workspace_bytes, ss_block_release_workspace(batch->batch, batch->max_blocks_per_seq, pool->num_blocks))) != SS_OK) return rc;
     BlockReleaseArgs a{};
     a.batch = batch->batch; a.max_blocks = batch->max_blocks_per_seq; a.num_blocks = pool->num_blocks;
     a.block_table = batch->block_table; a.kv_len = batch->kv_len; a.held = held; a.shares = shares;

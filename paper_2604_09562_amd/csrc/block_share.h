@@ -24,7 +24,7 @@ struct BlockReleaseArgs {
     int32_t *held, *shares, *free_ids, *free_count, *status;
     int32_t *scratch;                         // block_release_scratch_ints()
 };
-size_t block_release_scratch_ints(int batch, int max_blocks);
+size_t block_release_scratch_ints(int batch, int max_blocks, int num_blocks);
 int32_t block_release_launch(const BlockReleaseArgs &a, hipStream_t stream);
 
 struct BlockCompactArgs {

@@ -144,20 +144,37 @@ __global__ __launch_bounds__(kForkThreads) void block_fork_rows_kernel(BlockFork
 }
 
 // ---- releases ----------------------------------------------------------------------------------------------------------
-// Release r (they are counted in the order of request, logical block) takes one from its block's shares.  What is below zero then has no holder left, and its releases
-// leave there the last one's number; that release puts the block on the list, behind those of lower number.
-constexpr int kReleaseHead = 4;       // scratch: length of the free list, releases, status; then the releases in front of each request, then freed blocks by pieces
+// Releases are counted in the order of request, logical block.  Release r takes one from its block's shares and leaves its number in the block's entry of `last`, if no later one
+// does; what is below zero then has no holder left, and goes to the list at its last release's place, behind those of lower number.
+// One workgroup does a small table; else the sums are one workgroup's, while others clear `last`, and the releases many workgroups', in three launches: taken and named, those that free
+// a block counted by pieces, put on the list (2.7 + 5 + 4.5 + 5 us for 3500 releases; with names in a launch of their own 26 us, tables followed anew in each launch).
+constexpr int kReleaseHead = 4;       // scratch: length of the free list, releases
 constexpr int kReleasePiece = 1024;   // releases whose freed blocks are counted together
 constexpr int kReleaseLds = 1024;     // requests whose sums a workgroup keeps in LDS
 constexpr int kReleaseThreads = 256;
+constexpr int64_t kReleaseKept = 1 << 24;   // entries of a table up to which releases' blocks are kept in the workspace (64 MB)
 
-__device__ __forceinline__ int claim_of(int r) { return INT32_MIN + (int)(kMaxReleased - 1 - r); }   // the lower the later; far below any count
+struct ReleaseScratch {
+    int32_t *head, *given, *freed_in, *last, *ids;   // ids: nullptr in large tables
+};
+__host__ __device__ inline ReleaseScratch release_scratch(int32_t *p, int batch, int max_blocks, int num_blocks)
+{
+    ReleaseScratch s;
+    const int64_t entries = (int64_t)batch * max_blocks;
+    s.head = p;
+    s.given = p + kReleaseHead;                       // [batch + 1] releases in front of each request
+    s.freed_in = s.given + batch + 1;                 // [pieces]
+    s.last = s.freed_in + (entries + kReleasePiece - 1) / kReleasePiece;   // [num_blocks]
+    s.ids = entries <= kReleaseKept ? s.last + num_blocks : nullptr;       // [entries]
+    return s;
+}
 
 struct Releases {
     const BlockReleaseArgs &a;
-    const int32_t *given;             // [batch + 1]
+    const ReleaseScratch &s;
+    const int32_t *given;
     // the block of release r, -1 if it is none
-    __device__ int id(int r) const
+    __device__ int find(int r) const
     {
         int lo = 0, hi = a.batch;     // the last request with given[lo] <= r
         while (hi - lo > 1) {
@@ -167,21 +184,20 @@ struct Releases {
         const int x = a.block_table[(int64_t)lo * a.max_blocks + blocks_of(a.kv_len[lo]) + r - given[lo]];
         return (unsigned)x < (unsigned)a.num_blocks ? x : -1;
     }
-    __device__ void give(int r) const
+    __device__ void take(int r) const
     {
-        const int x = id(r);
-        if (x >= 0) atomicSub(&a.shares[x], 1);
-    }
-    __device__ void claim(int r) const
-    {
-        const int x = id(r);
-        if (x >= 0 && current(&a.shares[x]) < 0) atomicMin(&a.shares[x], claim_of(r));
+        const int x = find(r);
+        if (s.ids) s.ids[r] = x;
+        if (x >= 0) {
+            atomicSub(&a.shares[x], 1);
+            atomicMax(&s.last[x], r);
+        }
     }
     // the block that release r puts on the list, or -1
     __device__ int freed(int r) const
     {
-        const int x = id(r);
-        return x >= 0 && current(&a.shares[x]) == claim_of(r) ? x : -1;
+        const int x = s.ids ? s.ids[r] : find(r);
+        return x >= 0 && current(&s.last[x]) == r && current(&a.shares[x]) < 0 ? x : -1;
     }
 };
 
@@ -227,16 +243,26 @@ __device__ bool release_sums(const BlockReleaseArgs &a, ReleaseLds &lds, int32_t
 __global__ __launch_bounds__(kThreads) void block_release_kernel(BlockReleaseArgs a)
 {
     __shared__ ReleaseLds lds;
-    int32_t *given = a.scratch + kReleaseHead;
+    const ReleaseScratch w = release_scratch(a.scratch, a.batch, a.max_blocks, a.num_blocks);
     int count, releases;
-    if (!release_sums(a, lds, given, count, releases)) return;
+    if (!release_sums(a, lds, w.given, count, releases)) return;
     __threadfence_block();
     __syncthreads();
-    const Releases s = {a, given};
-    for (int r = threadIdx.x; r < releases; r += kThreads) s.give(r);
+    const Releases s = {a, w, w.given};
+    for (int r = threadIdx.x; r < releases; r += kThreads) {
+        const int x = s.find(r);
+        w.ids[r] = x;
+        if (x >= 0) __hip_atomic_store(&w.last[x], -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
     __threadfence_block();
     __syncthreads();
-    for (int r = threadIdx.x; r < releases; r += kThreads) s.claim(r);
+    for (int r = threadIdx.x; r < releases; r += kThreads) {
+        const int x = w.ids[r];
+        if (x >= 0) {
+            atomicSub(&a.shares[x], 1);
+            atomicMax(&w.last[x], r);
+        }
+    }
     __threadfence_block();
     __syncthreads();
     int at = count;
@@ -246,26 +272,31 @@ __global__ __launch_bounds__(kThreads) void block_release_kernel(BlockReleaseArg
         const int place = at + group_scan<kThreads>(x >= 0, lds.part, total) - 1;
         if (x >= 0) {
             if (place < a.num_blocks) a.free_ids[place] = x;
-            a.shares[x] = 0;    // (no other release's claim, either)
+            a.shares[x] = 0;    // (this release alone has found it below zero)
         }
         at += total;
     }
     if (threadIdx.x == 0) a.free_count[0] = min(at, a.num_blocks);
 }
 
+// The first workgroup sums, the others clear.
 __global__ __launch_bounds__(kThreads) void block_release_sum_kernel(BlockReleaseArgs a)
 {
     __shared__ ReleaseLds lds;
+    const ReleaseScratch w = release_scratch(a.scratch, a.batch, a.max_blocks, a.num_blocks);
+    if (blockIdx.x > 0) {
+        for (int64_t x = (int64_t)(blockIdx.x - 1) * kThreads + threadIdx.x; x < a.num_blocks; x += (int64_t)(gridDim.x - 1) * kThreads) w.last[x] = -1;
+        return;
+    }
     int count, releases;
-    const bool ok = release_sums(a, lds, a.scratch + kReleaseHead, count, releases);
+    const bool ok = release_sums(a, lds, w.given, count, releases);
     if (threadIdx.x == 0) {
-        a.scratch[0] = count;
-        a.scratch[1] = ok ? releases : 0;
-        a.scratch[2] = !ok;
+        w.head[0] = count;
+        w.head[1] = ok ? releases : 0;
     }
 }
 
-enum { kGive, kClaim, kCount, kPlace };
+enum { kTake, kCount, kPlace };
 
 template <int PHASE>
 __global__ __launch_bounds__(kReleaseThreads) void block_release_phase_kernel(BlockReleaseArgs a)
@@ -273,24 +304,21 @@ __global__ __launch_bounds__(kReleaseThreads) void block_release_phase_kernel(Bl
     constexpr int EACH = kReleasePiece / kReleaseThreads;
     __shared__ int32_t sums[kReleaseLds + 1];
     __shared__ int part[kReleaseThreads / 64];
-    const int tid = threadIdx.x, count = a.scratch[0], releases = a.scratch[1];
-    int32_t *given = a.scratch + kReleaseHead, *freed_in = given + a.batch + 1;
-    if (a.batch <= kReleaseLds) {
-        for (int b = tid; b <= a.batch; b += kReleaseThreads) sums[b] = given[b];
+    const ReleaseScratch w = release_scratch(a.scratch, a.batch, a.max_blocks, a.num_blocks);
+    const int tid = threadIdx.x, count = w.head[0], releases = w.head[1];
+    const bool search = PHASE == kTake || !w.ids, lds = search && a.batch <= kReleaseLds;
+    if (blockIdx.x * (PHASE == kTake ? kReleaseThreads : kReleasePiece) >= (unsigned)releases) return;
+    if (lds) {
+        for (int b = tid; b <= a.batch; b += kReleaseThreads) sums[b] = w.given[b];
         __syncthreads();
     }
-    const Releases s = {a, a.batch <= kReleaseLds ? sums : given};
-    const int pieces = (releases + kReleasePiece - 1) / kReleasePiece;
-    for (int piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
-        const int first = piece * kReleasePiece + tid * EACH;
-        if constexpr (PHASE == kGive || PHASE == kClaim) {
-#pragma unroll
-            for (int k = 0; k < EACH; ++k)
-                if (first + k < releases) {
-                    if (PHASE == kGive) s.give(first + k);
-                    else s.claim(first + k);
-                }
-        } else {
+    const Releases s = {a, w, lds ? sums : w.given};
+    if constexpr (PHASE == kTake) {
+        for (int64_t r = (int64_t)blockIdx.x * kReleaseThreads + tid; r < releases; r += (int64_t)gridDim.x * kReleaseThreads) s.take((int)r);
+    } else {
+        const int pieces = (releases + kReleasePiece - 1) / kReleasePiece;
+        for (int piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+            const int first = piece * kReleasePiece + tid * EACH;
             int x[EACH], mine = 0, total;
 #pragma unroll
             for (int k = 0; k < EACH; ++k) {
@@ -299,17 +327,17 @@ __global__ __launch_bounds__(kReleaseThreads) void block_release_phase_kernel(Bl
             }
             const int incl = group_scan<kReleaseThreads>(mine, part, total);
             if constexpr (PHASE == kCount) {
-                if (tid == 0) freed_in[piece] = total;
+                if (tid == 0) w.freed_in[piece] = total;
             } else {
                 int front = 0, before;
-                for (int i = tid; i < piece; i += kReleaseThreads) front += freed_in[i];
+                for (int i = tid; i < piece; i += kReleaseThreads) front += w.freed_in[i];
                 group_scan<kReleaseThreads>(front, part, before);
                 int place = count + before + incl - mine;
 #pragma unroll
                 for (int k = 0; k < EACH; ++k)
                     if (x[k] >= 0) {
                         if (place < a.num_blocks) a.free_ids[place] = x[k];
-                        a.shares[x[k]] = 0;   // (no other release's claim, either)
+                        a.shares[x[k]] = 0;   // (this release alone has found it below zero)
                         ++place;
                     }
                 if (piece == pieces - 1 && tid == 0) a.free_count[0] = min(count + before + total, a.num_blocks);
@@ -473,9 +501,10 @@ int32_t block_fork_launch(const BlockForkArgs &a, hipStream_t stream)
     return SS_OK;
 }
 
-size_t block_release_scratch_ints(int batch, int max_blocks)
+size_t block_release_scratch_ints(int batch, int max_blocks, int num_blocks)
 {
-    return kReleaseHead + (size_t)batch + 1 + ((size_t)batch * max_blocks + kReleasePiece - 1) / kReleasePiece;
+    const int64_t entries = (int64_t)batch * max_blocks;
+    return kReleaseHead + (size_t)batch + 1 + (entries + kReleasePiece - 1) / kReleasePiece + num_blocks + (entries <= kReleaseKept ? entries : 0);
 }
 
 int32_t block_release_launch(const BlockReleaseArgs &a, hipStream_t stream)
@@ -486,11 +515,11 @@ int32_t block_release_launch(const BlockReleaseArgs &a, hipStream_t stream)
         SS_HIP_CHECK(hipGetLastError(), "launch block_release_kernel");
         return SS_OK;
     }
-    const int64_t pieces = (entries + kReleasePiece - 1) / kReleasePiece;
+    const int64_t pieces = (entries + kReleasePiece - 1) / kReleasePiece, clear = ((int64_t)a.num_blocks + kThreads - 1) / kThreads;
+    const int64_t each = (entries + kReleaseThreads - 1) / kReleaseThreads;
     const dim3 grid((unsigned)(pieces < 1024 ? pieces : 1024)), wg(kReleaseThreads);
-    hipLaunchKernelGGL(block_release_sum_kernel, dim3(1), dim3(kThreads), 0, stream, a);
-    hipLaunchKernelGGL(block_release_phase_kernel<kGive>, grid, wg, 0, stream, a);
-    hipLaunchKernelGGL(block_release_phase_kernel<kClaim>, grid, wg, 0, stream, a);
+    hipLaunchKernelGGL(block_release_sum_kernel, dim3(1 + (unsigned)(clear < 255 ? clear : 255)), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL(block_release_phase_kernel<kTake>, dim3((unsigned)(each < 1024 ? each : 1024)), wg, 0, stream, a);
     hipLaunchKernelGGL(block_release_phase_kernel<kCount>, grid, wg, 0, stream, a);
     hipLaunchKernelGGL(block_release_phase_kernel<kPlace>, grid, wg, 0, stream, a);
     SS_HIP_CHECK(hipGetLastError(), "launch block_release kernels");

@@ -38,7 +38,7 @@ inline double tree_tile_time(double units, double rows, double steps, int head_d
 {
     const double tiles = units * (double)(int64_t)((rows + 255) / 256), each = tiles * steps / cus;
     const double step = head_dim == 64 ? 0.6 : kv8 ? 1.3 : rows <= 128 ? 0.8 : 1.0;
-    return 20.0 + 6.0 * (each < 5.0 ? each / 5.0 : 1.0) + step * each;
+    return 20.0 + 6.0 * (each < 5.0 ? each / 5.0 : 1.0) + step * 0.6 * each;   // (lengths taken to be 0.6 of the bound in the mean)
 }
 
 // rows: of the widest tree and a KV head, 0 if no bound of them is known

@@ -16,7 +16,6 @@ struct TreeVerifyArgs {
     float *logprobs;                       // may be nullptr
     void *workspace;
 };
-int64_t tree_verify_workgroups(int batch, int total_rows, int vocab);   // of the largest launch
 size_t tree_verify_workspace_bytes(int batch, int total_rows, int vocab);
 int32_t tree_verify_launch(const TreeVerifyArgs &a, hipStream_t stream);
 

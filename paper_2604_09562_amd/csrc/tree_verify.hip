@@ -472,12 +472,6 @@ int32_t launch(const TreeVerifyArgs &a, hipStream_t stream)
 
 }  // namespace
 
-int64_t tree_verify_workgroups(int batch, int total_rows, int vocab)
-{
-    const int64_t rows = few_rows(batch, total_rows, vocab, SS_MAX_DEPTH) ? total_rows : 0, n = rows * num_sub(vocab);
-    return n > batch ? n : batch;
-}
-
 size_t tree_verify_workspace_bytes(int batch, int total_rows, int vocab)
 {
     size_t bytes;

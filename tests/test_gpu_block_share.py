@@ -383,7 +383,7 @@ def test_binding_refuses():
     for name in ("block_table", "kv_len", "held", "shares", "free_ids", "free_count"):
         for bad in (d[name].long(), d[name].cpu(), d[name].reshape(-1)[:0]):
             with pytest.raises(binding.SpecVerifyError):
-                binding.ss_block_release(dict(d, **{name: bad}), status, ws)
+                binding.alloc_block_share_workspace(dict(d, **{name: bad}), DEV)
     with pytest.raises(binding.SpecVerifyError):
         binding.ss_block_fork(d, z, z[:1], None, src, src, status, ws)
     with pytest.raises(binding.SpecVerifyError):

@@ -73,7 +73,7 @@ def _verify(L, batch=3, vocab=100, stride=104, dt=1, rows=9, depth=0, indptr=P, 
     (1, b"logit_dtype", dict(dt=2)), (1, b"temperature", dict(t=-1.0)), (1, b"temperature", dict(t=float("nan"))), (1, b"NULL", dict(indptr=None)),
     (1, b"NULL", dict(parent=None)), (1, b"NULL", dict(tokens=None)), (1, b"NULL", dict(logits=None)), (1, b"NULL", dict(n=None)), (1, b"NULL", dict(out=None)),
     (1, b"NULL", dict(nodes=None)), (1, b"uniforms", dict(u=None)), (1, b"uniforms", dict(u=None, temp=P, t=0.0)), (1, b"aligned", dict(stride=101)),
-    (1, b"aligned", dict(logits=P + 2)), (1, b"workspace", dict(ws=None)), (3, b"needed", dict(nbytes=8)), (2, b"too large", dict(rows=1 << 30))])
+    (1, b"aligned", dict(logits=P + 2)), (1, b"workspace", dict(ws=None)), (3, b"needed", dict(nbytes=8)), (2, b"too large", dict(batch=1 << 24))])
 def test_tree_verify_refuses(L, code, text, args):
     assert _verify(L, **args) == code and text in L.ss_last_error(), L.ss_last_error()
 
@@ -123,7 +123,7 @@ def test_release_and_compact_refuse(L):
     assert _release(L, shares=None) == 1 and b"NULL" in L.ss_last_error()
     assert _compact(L, num=None) == 1 and b"NULL" in L.ss_last_error()
     assert _compact(L, dst=None) == 1 and b"NULL" in L.ss_last_error()
-    for f, args in ((L.ss_block_fork_workspace, (-1, 0)), (L.ss_block_fork_workspace, (0, -1)), (L.ss_block_release_workspace, (-1, 3)),
+    for f, args in ((L.ss_block_fork_workspace, (-1, 0)), (L.ss_block_fork_workspace, (0, -1)), (L.ss_block_release_workspace, (-1, 3, 4)), (L.ss_block_release_workspace, (1, 3, -4)),
                     (L.ss_block_compact_workspace, (-1,))):
         assert f(*args) == 0 and b"negative" in L.ss_last_error()
 
