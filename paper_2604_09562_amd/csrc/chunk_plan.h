@@ -20,6 +20,7 @@ constexpr int kOpenFew = 1;          // a tile's cost beside its steps where the
 // Steps of a tile that no cut is made for.  With 0 | 1 | 2, us: 33 tokens behind 700 21.0 | 21.0 | 22.1, a prompt of 2048 64.2 | 63.2 | 63.2; fp32, four requests
 // of 20 .. 150 tokens, 24.6 | 24.9 | 33.9.
 constexpr int kSnap = 1;
+constexpr double kNarrowStep = 0.75;   // what a step costs a tile of a draft tree with half of the rows or less, against one of more
 
 template <typename T>
 __device__ __forceinline__ T wave_incl_sum(T x)
@@ -77,12 +78,20 @@ struct ChunkUnit {                   // a request
         last = tiles ? steps(tiles - 1) : 0;
         slope = tiles > 1 ? (last - first) / (2.0 * (tiles - 1)) : 0.0;
     }
+    // TREE: whether a tile, a request's last one, has half of the rows or less, with steps that cost less
+    __device__ __forceinline__ bool narrow(int t) const { return TREE && q_len * G - t * ROWS <= ROWS / 2; }
     // cost of the tiles in front of tile t
-    __device__ __forceinline__ double before(int t) const { return (double)t * (open + first) + __builtin_floor(slope * t * (t - 1.0)); }
+    __device__ __forceinline__ double before(int t) const
+    {
+        const double all = (double)t * (open + first) + __builtin_floor(slope * t * (t - 1.0));
+        if constexpr (TREE) return t == tiles && t > 0 && narrow(t - 1) ? all - __builtin_floor((1.0 - kNarrowStep) * first) : all;
+        else return all;
+    }
     // the step of tile t at which a cut of this cost (counted from the request's first tile) falls: 0 and steps(t) are no cuts
     __device__ __forceinline__ int cut(double x, int t, int n) const
     {
-        const double off = x - before(t) - open;
+        double off = x - before(t) - open;
+        if constexpr (TREE) off = narrow(t) ? off / kNarrowStep : off;
         return off <= kSnap ? 0 : off >= n - kSnap ? n : (int)off;
     }
 };

@@ -14,6 +14,10 @@ MIXED = [(1, 1), (0, 0), (25, 325), (33, 33), (64, 1500), (0, 40), (7, 4000), (1
 TYPES = [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32"), ("bf16", "f32"), ("f32", "bf16"), ("f32", "fp8")]
 
 
+# With a bound of the rows short calls take a kernel of their own; without one all of bf16 queries are the other kernel's.
+BOTH = pytest.mark.parametrize("most", [None, 0], ids=["bound", "no_bound"])
+
+
 def run(inp, most=None, lse=True):
     if most is None:
         q = inp["q_indptr"]
@@ -29,20 +33,22 @@ def run(inp, most=None, lse=True):
     return out, l
 
 
+@BOTH
 @pytest.mark.parametrize("q,kv", TYPES)
 @pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (4, 2, 64), (8, 8, 128), (10, 2, 128), (16, 2, 64), (16, 1, 128), (7, 1, 64)])
-def test_mixed_batch(q, kv, hq, hkv, d):
+def test_mixed_batch(q, kv, hq, hkv, d, most):
     inp = ref.tree_batch(MIXED, hq, hkv, d, q=q, kv=kv, seed=hq + d, spare_rows=3, spare_columns=5, spare_words=1, stray_bits=True, row_pad=16)
-    ref.check_tree(inp, *run(inp))
+    ref.check_tree(inp, *run(inp, most))
 
 
+@BOTH
 @pytest.mark.parametrize("q,kv", TYPES[:3])
 @pytest.mark.parametrize("pattern", ["tree", "chain", "all", "none", "random"])
 @pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (8, 1, 64)])
-def test_patterns(q, kv, pattern, hq, hkv, d):
+def test_patterns(q, kv, pattern, hq, hkv, d, most):
     lengths = [(31, 31), (32, 64), (65, 200), (96, 96), (5, 5), (1, 1), (257, 700)]
     inp = ref.tree_batch(lengths, hq, hkv, d, pattern=pattern, q=q, kv=kv, seed=3)
-    ref.check_tree(inp, *run(inp), pattern)
+    ref.check_tree(inp, *run(inp, most), pattern)
 
 
 @pytest.mark.parametrize("q,kv", TYPES[:3])
@@ -53,50 +59,56 @@ def test_any_bound_of_the_rows(q, kv, most):
     ref.check_tree(inp, *run(inp, most))
 
 
+@BOTH
 @pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129])
 @pytest.mark.parametrize("kv", ["bf16", "fp8", "f32"])
-def test_every_place_in_a_block(n, kv):
+def test_every_place_in_a_block(n, kv, most):
     """Trees that begin and end at every place of blocks and steps."""
     inp = ref.tree_batch([(n, n + c) for c in (0, 1, 15, 16, 17, 31, 32, 33, 47, 63, 64, 65)], 4, 1, 128, kv=kv, q="f32" if kv == "f32" else "bf16", seed=n)
-    ref.check_tree(inp, *run(inp))
+    ref.check_tree(inp, *run(inp, most))
 
 
+@BOTH
 @pytest.mark.parametrize("kv,q", [("bf16", "bf16"), ("fp8", "bf16"), ("f32", "f32")])
-def test_long_and_many(kv, q):
+def test_long_and_many(kv, q, most):
     for lengths, hq, hkv in (([(48, 20000)], 8, 2), ([(30, 30 + 37 * i) for i in range(130)], 4, 1), ([(600, 1500)], 4, 4), ([(64, 64 + 5000), (64, 70)], 32, 8)):
         inp = ref.tree_batch(lengths, hq, hkv, 128, kv=kv, q=q, seed=11)
-        ref.check_tree(inp, *run(inp), str(lengths[:2]))
+        ref.check_tree(inp, *run(inp, most), str(lengths[:2]))
 
 
+@BOTH
 @pytest.mark.parametrize("kv,q", [("bf16", "bf16"), ("fp8", "bf16"), ("f32", "f32")])
-def test_more_nodes_than_positions(kv, q):
+def test_more_nodes_than_positions(kv, q, most):
     """kv_len below the request's rows: nodes in front of position 0 are no keys, and rows that see none are empty."""
     inp = ref.tree_batch([(20, 9), (40, 400), (33, 1), (5, 0)], 8, 2, 128, kv=kv, q=q, pattern="tree", seed=2)
-    ref.check_tree(inp, *run(inp))
+    ref.check_tree(inp, *run(inp, most))
 
 
-def test_without_log_sum_exp():
+@BOTH
+def test_without_log_sum_exp(most):
     for kv, q in (("bf16", "bf16"), ("fp8", "bf16"), ("f32", "f32")):
         inp = ref.tree_batch(MIXED, 8, 2, 128, kv=kv, q=q, seed=4)
-        out, lse = run(inp)
-        again, untouched = run(inp, lse=False)
+        out, lse = run(inp, most)
+        again, untouched = run(inp, most, lse=False)
         assert (untouched == 7).all()
         ref.check_tree(inp, again, lse)
 
 
+@BOTH
 @pytest.mark.parametrize("kv,q", [("bf16", "bf16"), ("fp8", "bf16"), ("f32", "f32")])
-def test_chain_is_the_chunks_attention(kv, q):
+def test_chain_is_the_chunks_attention(kv, q, most):
     inp = ref.tree_batch([(70, 300), (33, 2000), (1, 50)], 8, 2, 128, pattern="chain", kv=kv, q=q, seed=6)
-    out, lse = run(inp)
+    out, lse = run(inp, most)
     check_chunk(inp, out, lse)
     chunk, clse, ws = binding.alloc_chunk_outputs(inp, DEV)
     binding.ss_chunk_attn(inp, chunk, clse, ws)
     ref.check_tree(inp, chunk, clse)
 
 
+@BOTH
 @pytest.mark.parametrize("kv,q", [("bf16", "bf16"), ("fp8", "bf16"), ("f32", "f32")])
 @pytest.mark.parametrize("bad", ["key", "value", "both"])
-def test_what_is_not_finite_stays_with_the_rows_that_see_it(kv, q, bad):
+def test_what_is_not_finite_stays_with_the_rows_that_see_it(kv, q, bad, most):
     """Two nodes hold NaN or infinities; rows that do not see them are as if they were not there, the others are not finite."""
     n, m = 90, 400
     inp = ref.tree_batch([(n, m), (30, 60)], 8, 2, 128, kv=kv, q=q, seed=8)
@@ -109,7 +121,7 @@ def test_what_is_not_finite_stays_with_the_rows_that_see_it(kv, q, bad):
                 inp[name].view(torch.uint8)[block, :, slot] = 0x7F
             else:
                 inp[name][block, :, slot] = float("nan") if name == "k_cache" or node == 13 else float("inf")
-    out, lse = run(inp)
+    out, lse = run(inp, most)
     sees = inp["sees"][0]
     hit = torch.zeros(inp["total_rows"], dtype=torch.bool)
     for node in nodes:
@@ -126,13 +138,14 @@ def test_what_is_not_finite_stays_with_the_rows_that_see_it(kv, q, bad):
     ref.check_tree(clean, out, lse, rows=(~hit).nonzero()[:, 0])
 
 
+@BOTH
 @pytest.mark.parametrize("kv,q", [("bf16", "bf16"), ("fp8", "bf16"), ("f32", "f32")])
-def test_scores_of_any_size(kv, q):
+def test_scores_of_any_size(kv, q, most):
     """A scale that takes scores far beyond an exponential's range: the largest score's value, whatever stands in front."""
     for scale in (1e-30, 30.0, 1e12, 1e30):
         inp = ref.tree_batch([(40, 300), (7, 7)], 4, 1, 128, kv=kv, q=q, seed=9)
         inp["sm_scale"] = float(np.float32(scale))
-        out, lse = run(inp)
+        out, lse = run(inp, most)
         got = (out if out.dtype == torch.float32 else out.view(torch.bfloat16)).double()
         assert got.isfinite().all() and lse.isfinite().all()
         if scale < 1:
