@@ -118,9 +118,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_unit_kernel(ChunkArgs a, 
         const int n = t * kRows + r32, i_row = min(n, rows - 1) / G;
         const uint32_t *mask = a.node_mask + (int64_t)(u.q0 + i_row) * a.mask_words;
         u32x4 in_k[2][FP8 ? LOADS : 1], in_v[2][FP8 ? LOADS : 1];
-        int id[2], ks[2] = {}, vs[2] = {};
+        int id[2], next[2] = {}, ks[2] = {}, vs[2] = {};   // next: blocks of the wavefront's next step
         if (first + wave < steps) {
             ids_of(first + wave, id);
+            ids_of(first + wave + kWaves, next);
             bring(k_base, id, k_tile, in_k);
             bring(v_base, id, v_tile, in_v);
             scales_of(k_scale, id, ks);
@@ -149,12 +150,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_unit_kernel(ChunkArgs a, 
             uint32_t window = ~0u;
             if (step >= full) window = tree_window(mask, a.mask_words, u.q_len, step * kKeys - ctx) >> (4 * half);
             const bool more = step + kWaves < steps;
-            int next[2], ks_next[2] = {}, vs_next[2] = {};
-            if (more) {
-                ids_of(step + kWaves, next);
-                scales_of(k_scale, next, ks_next);
-                scales_of(v_scale, next, vs_next);
-            }
+            int after[2], ks_next[2] = {}, vs_next[2] = {};
+            ids_of(step + 2 * kWaves, after);   // (scalar loads, in time for the loads that follow them)
+            scales_of(k_scale, next, ks_next);
+            scales_of(v_scale, next, vs_next);
             // Keys are on their way from this step's scores to the next one's, values from the end of one step to the middle of the next.
             put(in_k, k_tile, ks);
             if constexpr (FP8) {
@@ -298,6 +297,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_unit_kernel(ChunkArgs a, 
                 for (int j = 0; j < 2; ++j) {
                     ks[j] = ks_next[j];
                     vs[j] = vs_next[j];
+                    next[j] = after[j];
                 }
             }
         }

@@ -7,12 +7,11 @@
 // behind 300 | 1000 | 4000 | 10000 tokens 10.2 | 14.4 | 30 | 59 (10 | 14 | 30 | 62); 16 requests behind 300 | 4000 20 | 76 (21 | 77); 16 of 64 nodes behind 4000 151 (153); e4m3 with 8
 // query heads, one of 25 nodes behind 10000 87 (88), 16 behind 4000 163 (174); 64-wide heads, 16 of 64 nodes behind 10000 94 (95).
 //
-// The other kernel: what a call costs it without keys, as soon as tiles are cut 6 more (openings, partial results and their merge), and steps of 32 keys for 256 rows.  The same:
-// one request of 25 nodes 18 | 21 | 26 | 31 (20 | 21 | 25 | 34); 16 of them 29 | 77 (30 | 77); 16 of 64 nodes 101 (90); e4m3, one of 25 nodes 39 (39), 16 behind 4000
-// 103 (108); 64-wide heads, 16 of 64 nodes behind 10000 70 (73).
+// The other kernel: what a call costs it without keys, as soon as tiles are cut 6 more (openings, partial results and their merge), and steps of 32 keys for 256 rows: of bf16 1.06, of
+// e4m3 1.27, of 64-wide heads 0.6 to each compute unit, three quarters of that where a tile has 128 rows or less.
 //
 // Of 282 calls of 1 .. 64 requests with 6 .. 150 nodes behind up to 30000 tokens (lengths from half of the bound on; 32 heads over 8 of 128 in bf16, 64 over 8 in e4m3, 16 over 2 of
-// 64 in bf16) the rule takes the fastest form that was measured, or one within 15 %, in 279, and 1.1 % more time than the fastest in the mean.
+// 64 in bf16) the rule takes the fastest form that was measured, or one within 15 %, in 274, and 2 % more time than the fastest in the mean.
 #pragma once
 
 #include <stdint.h>
@@ -34,10 +33,11 @@ inline double tree_unit_time(double tiles, double steps, int splits, int head_di
     const double round = head_dim == 64 ? 1.0 : kv8 ? 2.0 + 0.1 * full : 1.3 + 0.6 * full;
     return 1.5 + turns * (5.7 + round * rounds) + (splits > 1 ? 3.5 : 0.0);
 }
-inline double tree_tile_time(double units, double rows, double steps, int head_dim, bool kv8, int cus)
+inline double tree_tile_time(double units, int64_t rows, double steps, int head_dim, bool kv8, int cus)
 {
-    const double tiles = units * (double)(int64_t)((rows + 255) / 256), each = tiles * steps / cus;
-    const double step = head_dim == 64 ? 0.6 : kv8 ? 1.3 : rows <= 128 ? 0.8 : 1.0;
+    // (a last tile of half the rows or less takes three quarters)
+    const double tiles = (double)(rows / 256) + (rows % 256 == 0 ? 0.0 : rows % 256 <= 128 ? 0.75 : 1.0), each = units * tiles * steps / cus;
+    const double step = head_dim == 64 ? 0.6 : kv8 ? 1.25 : 1.0;
     return 20.0 + 6.0 * (each < 5.0 ? each / 5.0 : 1.0) + step * 0.6 * each;   // (lengths taken to be 0.6 of the bound in the mean)
 }
 
@@ -47,7 +47,7 @@ inline TreeUnitChoice tree_unit_rule(int batch, int num_kv_heads, int64_t rows, 
     const int64_t each = (rows + kTreeUnitRows - 1) / kTreeUnitRows, tiles = each * batch * num_kv_heads;
     if (rows <= 0 || tiles > 65536) return {0, 1};
     const double steps = (double)((max_keys + 31) / 32);
-    double best = tree_tile_time((double)batch * num_kv_heads, (double)rows, steps, head_dim, kv8, cus);
+    double best = tree_tile_time((double)batch * num_kv_heads, rows, steps, head_dim, kv8, cus);
     TreeUnitChoice c = {0, 1};
     for (int splits = 1; splits <= 16 && (splits == 1 || steps >= 8.0 * splits); splits *= 2) {
         const double t = tree_unit_time((double)tiles, steps, splits, head_dim, kv8, cus);
