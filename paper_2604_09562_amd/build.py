@@ -22,7 +22,7 @@ LIB = os.path.join(HERE, "libspecverify.so")
 # the per-grouping attention units take longest: start them first
 SOURCES = ["attn_mfma_g8.hip", "attn_mfma_g4.hip", "attn_mfma_g2.hip", "attn_mfma_g1.hip", "attn_unit.hip", "accept.hip", "accept_tree.hip", "accept_static.hip", "api.hip",
            "attn_chunk.hip", "attn_mfma.hip", "attn_generic.hip", "kvcache.hip", "block_map.hip", "kv_write.hip", "attn_chunk_f32.hip", "api_prefill.hip", "validate.hip",
-           "attn_tree.hip", "attn_tree_unit.hip", "api_tree.hip", "block_share.hip", "block_copy.hip", "tree_verify.hip",
+           "attn_tree.hip", "attn_tree_unit.hip", "attn_tree_unit_f32.hip", "api_tree.hip", "block_share.hip", "block_copy.hip", "tree_verify.hip",
            "depth_controller.cpp", "router.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

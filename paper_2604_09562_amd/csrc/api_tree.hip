@@ -48,9 +48,10 @@ TreeForm tree_form(const ss_paged_kv *kv, const ss_batch *b, int32_t q_dtype, in
     TreeForm f;
     f.mfma = chunk_mfma_supported(kv->head_dim, kv->dtype, q_dtype);
     const int64_t nodes = b->max_q_len > 0 && b->max_q_len < total_rows ? b->max_q_len : b->max_q_len > 0 || b->batch == 1 ? total_rows : 0;   // of the widest tree
-    f.unit = f.mfma ? tree_unit_rule(b->batch, kv->num_kv_heads, nodes * (num_q_heads / kv->num_kv_heads), (int64_t)b->max_blocks_per_seq * SS_BLOCK_SIZE, kv->head_dim,
-                                     kv->dtype == SS_FP8_E4M3, attn_chip_waves() / 4)
-                    : TreeUnitChoice{0, 1};
+    const int64_t rows = nodes * (num_q_heads / kv->num_kv_heads), keys = (int64_t)b->max_blocks_per_seq * SS_BLOCK_SIZE;
+    const int cus = attn_chip_waves() / 4;
+    f.unit = f.mfma ? tree_unit_rule(b->batch, kv->num_kv_heads, rows, keys, kv->head_dim, kv->dtype == SS_FP8_E4M3, cus)
+                    : TreeUnitChoice{tree_unit_f32_rule(b->batch, kv->num_kv_heads, rows, keys, kv->head_dim, cus), 1};
     f.shape = chunk_shape(f.mfma, b->batch, b->max_blocks_per_seq, num_q_heads, kv->num_kv_heads, total_rows);
     f.workspace = f.unit.tiles ? unit_part_o(f.unit, b->batch, kv->num_kv_heads) + unit_slots(f.unit, b->batch, kv->num_kv_heads) * kTreeUnitRows * kv->head_dim * sizeof(float) + 256
                                : chunk_workspace_bytes(f.shape, kv->head_dim);
@@ -106,7 +107,7 @@ int32_t ss_tree_attn(const ss_paged_kv *kv, const ss_batch *batch, const uint32_
     if (f.unit.tiles) {
         a.part_ml = static_cast<float *>(workspace);
         a.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace) + unit_part_o(f.unit, batch->batch, kv->num_kv_heads));
-        return tree_unit_launch(a, f.unit, static_cast<hipStream_t>(stream));
+        return f.mfma ? tree_unit_launch(a, f.unit, static_cast<hipStream_t>(stream)) : tree_unit_f32_launch(a, f.unit.tiles, static_cast<hipStream_t>(stream));
     }
     chunk_carve(a, f.shape, workspace);
     return f.mfma ? tree_mfma_launch(a, static_cast<hipStream_t>(stream)) : tree_f32_launch(a, static_cast<hipStream_t>(stream));

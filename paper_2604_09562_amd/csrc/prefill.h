@@ -81,6 +81,7 @@ int32_t chunk_mfma_launch(const ChunkArgs &a, hipStream_t stream);
 int32_t chunk_f32_launch(const ChunkArgs &a, hipStream_t stream);
 int32_t tree_f32_launch(const ChunkArgs &a, hipStream_t stream);
 int32_t tree_mfma_launch(const ChunkArgs &a, hipStream_t stream);
+int32_t tree_unit_f32_launch(const ChunkArgs &a, int tiles, hipStream_t stream);
 int32_t tree_unit_launch(const ChunkArgs &a, const TreeUnitChoice &how, hipStream_t stream);
 
 // ---- optional checks of device-resident metadata -----------------------------------------------

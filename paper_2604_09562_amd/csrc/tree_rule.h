@@ -1,4 +1,4 @@
-// Which calls of wide trees' attention the kernel of short calls (attn_tree_unit.hip) takes, and how it cuts them.  Plain host code, with a test of its own.
+// Which calls of wide trees' attention the kernels of short calls (attn_tree_unit.hip, attn_tree_unit_f32.hip) take, and how it cuts them.  Plain host code, with a test of its own.
 //
 // Both kernels' times, in us, from the sizes that the host knows: batch, heads, the widest tree, and the width of the table as the bound of the lengths.
 //
@@ -18,7 +18,7 @@
 
 namespace ss {
 
-constexpr int kTreeUnitRows = 32;   // query rows of a tile
+constexpr int kTreeUnitRows = 32, kTreeUnitRowsF32 = 16;   // query rows of a tile
 struct TreeUnitChoice {
     int32_t tiles;    // of a request and KV head, that are taken side by side; 0: the call is another kernel's
     int32_t splits;   // workgroups that share a tile's keys
@@ -57,6 +57,25 @@ inline TreeUnitChoice tree_unit_rule(int batch, int num_kv_heads, int64_t rows, 
         }
     }
     return c;
+}
+
+// The same choice for calls in fp32 (attn_tree_unit_f32.hip): tiles that are taken side by side, 0 for the other kernel, whose tiles have 64 rows that share its steps of 64 keys.
+// Both are bound by the fp32 matrix rate where they are large.  Short calls: 7 us, and 3.15 us a round of 256 keys (64-wide heads: two requests of 25 nodes behind 0 | 300 | 1000 |
+// 4000 | 10000 tokens 8.6 | 11.0 | 20 | 57 | 134) or 3.4 of 128 (128-wide: 7.8 | 17.4 | 36 | 114 | 271), once for every workgroup to a compute unit; the other kernel on the same 17 |
+// 24.5 | 23 | 28 | 39 and 23.5 | 38 | 35 | 67 | 142, sixteen of 64 nodes behind 300 36 | 90 (here 22.5 | 128).  Of 293 calls of 2 .. 64 requests with 6 .. 150 nodes behind up to 10000
+// tokens of one length (three types, both widths) the choice is within 15 % of the faster in 279, and 2.5 % above it in the mean.
+inline int32_t tree_unit_f32_rule(int batch, int num_kv_heads, int64_t rows, int64_t max_keys, int head_dim, int cus)
+{
+    const int64_t each = (rows + kTreeUnitRowsF32 - 1) / kTreeUnitRowsF32, wgs = each * batch * num_kv_heads;
+    if (rows <= 0 || wgs > 65536) return 0;
+    const bool narrow = head_dim == 64;
+    const int keys_of_round = narrow ? 256 : 128;   // (one block to each of 16 or 8 wavefronts)
+    const double turns = (double)((wgs + cus - 1) / cus), rounds = (double)((max_keys + keys_of_round - 1) / keys_of_round);
+    const double unit = 7.0 + turns * (1.0 + (narrow ? 3.15 : 3.4) * rounds);
+    const double steps = (double)((max_keys + 63) / 64), tiles = (double)((rows + 63) / 64) * batch * num_kv_heads;
+    const double few = steps < 3.0 ? steps : 3.0, spread = 0.75 * tiles * steps / cus;   // (lengths taken to be 0.75 of the bound in the mean)
+    const double other = 15.0 + (narrow ? 3.3 : 7.5) * (spread > few ? spread : few);
+    return unit < other ? (int32_t)each : 0;
 }
 
 }  // namespace ss

@@ -12,7 +12,8 @@ def rule(tmp_path_factory):
     d = tmp_path_factory.mktemp("rule")
     (d / "r.cpp").write_text('#include "tree_rule.h"\n'
                              'extern "C" void rule(int b, int h, long long rows, long long keys, int dim, int kv8, int cus, int *o)\n'
-                             '{\n    const ss::TreeUnitChoice c = ss::tree_unit_rule(b, h, rows, keys, dim, kv8 != 0, cus);\n    o[0] = c.tiles;\n    o[1] = c.splits;\n}\n')
+                             '{\n    const ss::TreeUnitChoice c = ss::tree_unit_rule(b, h, rows, keys, dim, kv8 != 0, cus);\n    o[0] = c.tiles;\n    o[1] = c.splits;\n}\n'
+                             'extern "C" int rule_f32(int b, int h, long long rows, long long keys, int dim, int cus) { return ss::tree_unit_f32_rule(b, h, rows, keys, dim, cus); }\n')
     subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Werror", "-shared", "-fPIC", "-I", CSRC, str(d / "r.cpp"), "-o", str(d / "r.so")], check=True)
     fn = ctypes.CDLL(str(d / "r.so")).rule
     fn.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.c_longlong, ctypes.c_longlong] + [ctypes.c_int] * 3 + [ctypes.c_void_p]
@@ -21,6 +22,8 @@ def rule(tmp_path_factory):
         o = (ctypes.c_int * 2)()
         fn(batch, heads, rows, keys, dim, int(kv8), cus, o)
         return o[0], o[1]
+    call.f32 = lambda batch, heads, rows, keys, dim=128, cus=256: ctypes.CDLL(str(d / "r.so")).rule_f32(
+        batch, heads, ctypes.c_longlong(rows), ctypes.c_longlong(keys), dim, cus)
     return call
 
 
@@ -46,3 +49,20 @@ def test_cuts_of_any_call(rule, dim, kv8):
                     assert splits == 1 or -(-keys // 32) >= 8 * splits
                     assert tiles * batch * heads <= 65536
     assert rule(1, 8, 0, 100, dim, kv8) == (0, 1)
+
+
+def test_short_calls_in_fp32(rule):
+    assert rule.f32(4, 2, 160, 560, 64) == 10 and rule.f32(1, 8, 100, 336) == 7 and rule.f32(2, 8, 24, 300) == 2
+    assert rule.f32(2, 2, 100, 10000, 64) == 0 and rule.f32(16, 8, 256, 364) == 0 and rule.f32(64, 8, 600, 450) == 0
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_cuts_of_any_call_in_fp32(rule, dim):
+    for batch in (0, 1, 3, 64, 5000, 2 ** 31 - 1):
+        for heads in (1, 2, 8, 128):
+            for rows in (0, 1, 15, 16, 17, 100, 4096, 2 ** 31 - 1):
+                for keys in (0, 16, 500, 70000, 2 ** 31 - 16):
+                    if batch * heads > 2 ** 31:
+                        continue
+                    tiles = rule.f32(batch, heads, rows, keys, dim)
+                    assert tiles == 0 or (rows > 0 and tiles == -(-rows // 16) and tiles * batch * heads <= 65536)
