@@ -276,7 +276,7 @@ def bits(x):
 
 
 @pytest.mark.parametrize("kv", ["f32", "bf16", "fp8"])
-@pytest.mark.parametrize("layers,hkv,d,n", [(1, 1, 64, 5), (3, 8, 128, 40), (70, 2, 64, 9), (2, 3, 128, 200)])
+@pytest.mark.parametrize("layers,hkv,d,n", [(1, 1, 64, 5), (3, 8, 128, 40), (70, 2, 64, 9), (2, 3, 128, 200), (3, 16, 128, 1400)])   # (the last: past the caches)
 def test_copies(kv, layers, hkv, d, n):
     c = caches(layers, n, hkv, d, kv)
     rng = np.random.default_rng(n)
