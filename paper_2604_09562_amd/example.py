@@ -1,6 +1,6 @@
 """A decode lane driven end to end through the library, on synthetic model outputs.
 
-    python -m paper_2604_09562_amd.example [--steps N] [--batch B] [--layers L] [--tree] [--chunk C]
+    python -m paper_2604_09562_amd.example [--steps N] [--batch B] [--layers L] [--tree] [--chunk C] [--wide N [--samples S]]
 
 First the prompts are put into the empty cache, C new tokens of every request at a time:
 
@@ -21,7 +21,15 @@ for by seeded random tensors, there being no weights here):
                                                                               ss_spec_accept_tree_greedy / _sample + ss_kv_compact
   commit      new valid lengths                                               ss_kv_commit
 
-and prints the accepted tokens per step.  Every device step runs in the library's kernels; this file
+and prints the accepted tokens per step.  With --wide every request is continued S times, in trees of up to N new tokens:
+
+  forks       S requests that share the blocks of one prompt                  ss_block_fork, ss_block_copy
+  blocks, write                                                               ss_block_map, ss_kv_write
+  attention   of the trees' nodes, once per layer                             ss_tree_attn
+  accept      the target's own draws, walked while a child carries them       ss_tree_verify
+  commit      paths to their places, lengths, blocks of the rest back         ss_kv_compact, ss_kv_commit, ss_block_release
+
+and half-way the last continuation of every request is dropped and the cache made whole again (ss_block_release, ss_block_compact, ss_block_copy).  Every device step runs in the library's kernels; this file
 only moves arguments.
 """
 from __future__ import annotations
@@ -33,6 +41,50 @@ import numpy as np
 import torch
 
 from . import binding, synth
+
+
+def open_books(cache: dict, dev: str):
+    """The cache's blocks, all free, and what the requests hold of them; returns the call that takes blocks for a step's new tokens."""
+    i32 = lambda x: binding.to_device(np.asarray(x, dtype=np.int32), dev)  # noqa: E731
+    cache.update(free_ids=i32(np.arange(cache["num_blocks"])), free_count=i32([cache["num_blocks"]]), held=i32(np.zeros(cache["batch"])),
+                 block_table=torch.zeros_like(cache["block_table"]))
+    status, ws = i32([0]), binding.alloc_block_map_workspace(cache, dev)
+
+    def blocks(d, rows):
+        slots = torch.empty(rows, dtype=torch.int32, device=dev)
+        binding.ss_block_map(d, slots, None, status, ws)
+        if int(status):      # (known before anything follows the table)
+            raise RuntimeError(f"ss_block_map: status {int(status)}")
+        return slots
+    return blocks
+
+
+def fill_prompts(cache: dict, lengths: np.ndarray, layers: int, chunk: int, blocks, rng, dev: str, verbose: bool) -> None:
+    """Put prompts of these lengths into the empty cache, `chunk` tokens of every request at a time."""
+    i32 = lambda x: binding.to_device(np.asarray(x, dtype=np.int32), dev)  # noqa: E731
+    Hq, Hkv, D = cache["num_q_heads"], cache["num_kv_heads"], cache["head_dim"]
+    done, chunks, t_prompt = np.zeros_like(lengths), 0, 0.0
+    while (done < lengths).any():
+        new = np.minimum(lengths - done, chunk)
+        done += new
+        q_indptr = np.concatenate([[0], np.cumsum(new)])
+        R = int(q_indptr[-1])
+        d = dict(cache, total_rows=R, q_dtype="bf16", new_dtype="bf16", kv_len=i32(done), q_indptr=i32(q_indptr))
+        # queries, keys and values of a layer are parts of one product's rows
+        wide = torch.from_numpy(rng.standard_normal((R, (Hq + 2 * Hkv) * D), dtype=np.float32)).to(dev, torch.bfloat16)
+        d["q"], d["k_new"], d["v_new"] = (x.unflatten(1, (-1, D)) for x in wide.split([Hq * D, Hkv * D, Hkv * D], 1))
+        out, lse, ws_c = binding.alloc_chunk_outputs(d, dev)
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        slots = blocks(d, R)
+        for _ in range(layers):
+            binding.ss_kv_write(d, slots)
+            binding.ss_chunk_attn(d, out, lse, ws_c)
+        torch.cuda.synchronize()
+        t_prompt += time.perf_counter() - t0
+        chunks += 1
+    if verbose:
+        print(f"{int(lengths.sum())} prompt tokens in {chunks} chunks, {1e3 * t_prompt / max(chunks, 1):.3f} ms of device work per chunk ({layers} layers)")
 
 
 def run(steps: int = 6, batch: int = 8, layers: int = 4, tree: bool = False, vocab: int = 32000, seed: int = 0,
@@ -58,45 +110,9 @@ def run(steps: int = 6, batch: int = 8, layers: int = 4, tree: bool = False, voc
     depth = np.full(batch, 4, dtype=np.int32)
     emitted, t_dev = 0, 0.0
     start_len = cur.copy()
-    sm_scale = cache["sm_scale"]
 
-    # the cache's blocks, all free, and what the requests hold of them
-    i32 = lambda x: binding.to_device(np.asarray(x, dtype=np.int32), dev)  # noqa: E731
-    cache.update(free_ids=i32(np.arange(cache["num_blocks"])), free_count=i32([cache["num_blocks"]]), held=i32(np.zeros(batch)),
-                 block_table=torch.zeros_like(cache["block_table"]))
-    status, ws_b = i32([0]), binding.alloc_block_map_workspace(cache, dev)
-
-    def blocks(d, rows):
-        slots = torch.empty(rows, dtype=torch.int32, device=dev)
-        binding.ss_block_map(d, slots, None, status, ws_b)
-        if int(status):      # (known before anything follows the table)
-            raise RuntimeError(f"ss_block_map: status {int(status)}")
-        return slots
-
-    # ---- the prompts
-    prompt_rng = np.random.default_rng(seed + 1)
-    done, chunks, t_prompt = np.zeros_like(cur), 0, 0.0
-    while (done < cur).any():
-        new = np.minimum(cur - done, chunk)
-        done += new
-        q_indptr = np.concatenate([[0], np.cumsum(new)])
-        R = int(q_indptr[-1])
-        d = dict(cache, total_rows=R, q_dtype="bf16", new_dtype="bf16", sm_scale=sm_scale, kv_len=i32(done), q_indptr=i32(q_indptr))
-        # queries, keys and values of a layer are parts of one product's rows
-        wide = torch.from_numpy(prompt_rng.standard_normal((R, (Hq + 2 * Hkv) * D), dtype=np.float32)).to(dev, torch.bfloat16)
-        d["q"], d["k_new"], d["v_new"] = (x.unflatten(1, (-1, D)) for x in wide.split([Hq * D, Hkv * D, Hkv * D], 1))
-        out, lse, ws_c = binding.alloc_chunk_outputs(d, dev)
-        torch.cuda.synchronize()
-        t0 = time.perf_counter()
-        slots = blocks(d, R)
-        for _ in range(layers):
-            binding.ss_kv_write(d, slots)
-            binding.ss_chunk_attn(d, out, lse, ws_c)
-        torch.cuda.synchronize()
-        t_prompt += time.perf_counter() - t0
-        chunks += 1
-    if verbose:
-        print(f"{int(cur.sum())} prompt tokens in {chunks} chunks, {1e3 * t_prompt / max(chunks, 1):.3f} ms of device work per chunk ({layers} layers)")
+    blocks = open_books(cache, dev)
+    fill_prompts(cache, cur, layers, chunk, blocks, np.random.default_rng(seed + 1), dev, verbose)
 
     for step in range(steps):
         # ---- what the models would hand over: draft tokens/logits, queries and new keys/values per layer
@@ -156,6 +172,115 @@ def run(steps: int = 6, batch: int = 8, layers: int = 4, tree: bool = False, voc
     return dict(chosen=chosen, emitted=emitted, depths=depth.copy(), kv_len=cur, start_len=start_len)
 
 
+def wide_trees(rng, live, nodes, drawn, vocab):
+    """Trees of up to `nodes` new tokens for the requests in `live`, `drawn` at their roots: (new tokens of each, q_indptr, parents, tokens, masks)."""
+    new = np.where(live, rng.integers(min(2, nodes), nodes + 1, len(live)), 0)
+    q_indptr = np.concatenate([[0], np.cumsum(new)])
+    R, words = int(q_indptr[-1]), -(-nodes // 32)
+    parent, tokens, mask = np.full(R, -1, np.int32), rng.integers(0, vocab, R).astype(np.int32), np.zeros((R, words), np.uint32)
+    for b, r0 in enumerate(q_indptr[:-1]):
+        for i in range(new[b]):
+            if i == 0:
+                tokens[r0] = drawn[b]
+            else:
+                parent[r0 + i] = rng.integers(max(i - 8, 0), i)
+                mask[r0 + i] = mask[r0 + parent[r0 + i]]      # a node attends its ancestors
+            mask[r0 + i, i // 32] |= np.uint32(1 << i % 32)   # and itself
+    return new, q_indptr, parent, tokens, mask
+
+
+def run_wide(steps: int = 6, batch: int = 4, layers: int = 4, nodes: int = 48, samples: int = 3, vocab: int = 32000, seed: int = 0, chunk: int = 512,
+             temperature: float = 0.8, verbose: bool = True) -> dict:
+    """`samples` continuations of each of `batch` prompts, in draft trees of up to `nodes` new tokens."""
+    dev = "cuda:0"
+    torch.cuda.set_device(0)
+    i32 = lambda x: binding.to_device(np.asarray(x, dtype=np.int32), dev)  # noqa: E731
+    rows = batch * samples
+    cfg = synth.CONFIGS[1].scaled(batch=rows, vocab=vocab, ctx=("uniform", 200, 1500))
+    rng = np.random.default_rng(seed)
+    host = synth.make_attention_inputs(cfg, seed=seed)
+    room = nodes + steps * (binding.SS_MAX_DEPTH + 1)
+    prompts = np.where(np.arange(rows) % samples == 0, np.maximum(host["kv_len"].astype(np.int32) - room, 1), 0).astype(np.int32)
+    cache = binding.attention_to_device(host, dev)
+    columns = -(-(int(prompts.max()) + room) // 16)
+    cache.update(max_blocks_per_seq=columns, block_table=torch.zeros((rows, columns), dtype=torch.int32, device=dev))
+    Hq, Hkv, D, N = cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim, cache["num_blocks"]
+    blocks = open_books(cache, dev)
+    fill_prompts(cache, prompts, layers, chunk, blocks, np.random.default_rng(seed + 1), dev, verbose)
+    cache.update(kv_len=i32(prompts), shares=i32(np.zeros(N)))
+    handle = binding.cache_layers([cache])      # (one cache stands in for every layer's)
+    status, ws = i32([0]), binding.alloc_block_share_workspace(cache, dev, num_forks=rows)
+
+    def ok(call):
+        if int(status):
+            raise RuntimeError(f"{call}: status {int(status)}")
+
+    # ---- the continuations share their prompt's blocks; a block that is not full is copied
+    children = np.flatnonzero(prompts == 0)
+    if len(children):
+        src, dst = i32(np.zeros(len(children))), i32(np.zeros(len(children)))
+        binding.ss_block_fork(cache, i32(children // samples * samples), i32(children), None, src, dst, status, ws)
+        binding.ss_block_copy(handle, src, dst)
+        ok("ss_block_fork")
+    start_len = cache["kv_len"].cpu().numpy()
+    live, drawn = np.ones(rows, bool), rng.integers(0, vocab, rows)
+    emitted, moved, t_dev = np.zeros(rows, int), 0, 0.0
+    for step in range(steps):
+        if step == steps // 2 and samples > 1:
+            live[samples - 1::samples] = False
+            cache["kv_len"] *= i32(live)
+            binding.ss_block_release(cache, status, ws)
+            ok("ss_block_release")
+            src, dst, moves = i32(np.zeros(N // 2)), i32(np.zeros(N // 2)), i32([0])
+            binding.ss_block_compact(cache, None, src, dst, moves, status, ws)
+            binding.ss_block_copy(handle, src, dst, moves)
+            ok("ss_block_compact")
+            moved = int(moves)
+        # ---- what the models would hand over
+        new, q_indptr, parent, tokens, mask = wide_trees(rng, live, nodes, drawn, vocab)
+        R = int(q_indptr[-1])
+        d = dict(cache, total_rows=R, q_dtype="bf16", new_dtype="bf16", kv_len=cache["kv_len"] + i32(new), q_indptr=i32(q_indptr),
+                 node_mask=binding.to_device(mask.view(np.int32), dev))
+        wide = torch.from_numpy(rng.standard_normal((R, (Hq + 2 * Hkv) * D), dtype=np.float32)).to(dev, torch.bfloat16)
+        d["q"], d["k_new"], d["v_new"] = (x.unflatten(1, (-1, D)) for x in wide.split([Hq * D, Hkv * D, Hkv * D], 1))
+        logits = torch.from_numpy(rng.standard_normal((R, vocab), dtype=np.float32)).to(dev, torch.bfloat16)
+        has_child = np.flatnonzero(parent >= 0)      # the target thinks well of some of the drafts
+        below = has_child[rng.random(len(has_child)) < 0.3]
+        root = np.repeat(q_indptr[:-1], new)
+        logits[torch.from_numpy(root[below] + parent[below]).to(dev), torch.from_numpy(tokens[below].astype(np.int64)).to(dev)] = 12.0
+        v = dict(batch=rows, vocab=vocab, row_stride=vocab, logit_dtype="bf16", total_rows=R, q_indptr=d["q_indptr"], tree_parent=i32(parent), node_tokens=i32(tokens),
+                 target_logits=logits, uniforms=torch.from_numpy(rng.random(R, dtype=np.float32)).to(dev), temperature=None, temperature_scalar=temperature)
+        out, lse, ws_t = binding.alloc_tree_outputs(d, dev, max_q_len=nodes)
+        n_acc, toks, accepted, logp, ws_v = binding.alloc_tree_verify_outputs(v, dev)
+
+        # ---- the device side of the step
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        slots = blocks(d, R)
+        for _ in range(layers):
+            binding.ss_kv_write(d, slots)
+            binding.ss_tree_attn(d, out, lse, ws_t, max_q_len=nodes)
+        binding.ss_tree_verify(v, n_acc, toks, accepted, logp, ws_v)
+        binding.ss_kv_compact(d, accepted, n_acc, max_q_len=nodes)      # (once: one cache stands in for every layer's)
+        binding.ss_kv_commit(d["q_indptr"], n_acc, d["kv_len"])
+        binding.ss_block_release(d, status, ws)
+        torch.cuda.synchronize()
+        t_dev += time.perf_counter() - t0
+        ok("ss_block_release")
+
+        cache["kv_len"] = d["kv_len"]
+        n = np.where(live, n_acc.cpu().numpy(), 0)
+        drawn = toks.cpu().numpy()[np.arange(rows), n]
+        emitted += np.where(live, n + 1, 0)
+        if verbose:
+            print(f"step {step}: {R} nodes, accepted {n[live].tolist()}, mean log-probability {float(logp[torch.from_numpy(live).to(dev), 0].mean()):.2f}")
+    held = int(cache["held"].sum())
+    if verbose:
+        print(f"{int(emitted.sum())} tokens emitted in {steps} steps, {1e3 * t_dev / max(steps, 1):.3f} ms of device work per step ({layers} layers); "
+              f"{held} blocks held, {N - int(cache['free_count'])} in use, {moved} moved")
+    return dict(emitted=emitted, live=live, kv_len=cache["kv_len"].cpu().numpy(), start_len=start_len, held=held, used=N - int(cache["free_count"]))
+
+
 def main() -> None:
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--steps", type=int, default=6)
@@ -164,7 +289,12 @@ def main() -> None:
     ap.add_argument("--tree", action="store_true", help="tree-shaped drafts (greedy acceptance unless --sample)")
     ap.add_argument("--chunk", type=int, default=512, help="new tokens of a request's prompt at a time")
     ap.add_argument("--sample", action="store_true", help="with --tree: the sampled acceptance walk")
+    ap.add_argument("--wide", type=int, default=0, metavar="N", help="draft trees of up to N new tokens, verified by the target's own draws")
+    ap.add_argument("--samples", type=int, default=3, help="with --wide: continuations of each prompt, which share its blocks")
     a = ap.parse_args()
+    if a.wide:
+        run_wide(a.steps, a.batch, a.layers, a.wide, a.samples, chunk=a.chunk)
+        return
     run(a.steps, a.batch, a.layers, a.tree, sample=a.sample, chunk=a.chunk)
 
 
