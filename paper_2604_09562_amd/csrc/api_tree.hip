@@ -115,7 +115,7 @@ int32_t ss_tree_attn(const ss_paged_kv *kv, const ss_batch *batch, const uint32_
 
 size_t ss_tree_verify_workspace(int32_t batch, int32_t total_rows, int32_t vocab)
 {
-    if (batch < 0 || total_rows < 0 || vocab <= 0) {
+    if (batch < 0 || total_rows < 0 || vocab <= 0 || vocab > 1 << 30) {
         fail(SS_ERR_INVALID_ARG, "bad batch/total_rows/vocab (%d, %d, %d)", batch, total_rows, vocab);
         return 0;
     }
@@ -127,7 +127,7 @@ int32_t ss_tree_verify(int32_t batch, int32_t vocab, int64_t row_stride, int32_t
                        float temperature_scalar, int32_t *accepted_len, int32_t *out_tokens, int32_t *accepted_nodes, float *logprobs, void *workspace,
                        size_t workspace_bytes, void *stream)
 {
-    if (batch < 0 || total_rows < 0 || vocab <= 0) return fail(SS_ERR_INVALID_ARG, "bad batch/total_rows/vocab (%d, %d, %d)", batch, total_rows, vocab);
+    if (batch < 0 || total_rows < 0 || vocab <= 0 || vocab > 1 << 30) return fail(SS_ERR_INVALID_ARG, "bad batch/total_rows/vocab (%d, %d, %d)", batch, total_rows, vocab);
     if (max_depth < 0 || max_depth > SS_MAX_DEPTH) return fail(SS_ERR_INVALID_ARG, "max_depth must be 0 (%d is meant) or in [1, %d]", SS_MAX_DEPTH, SS_MAX_DEPTH);
     if (row_stride < vocab) return fail(SS_ERR_INVALID_ARG, "row_stride (%lld) < vocab (%d)", (long long)row_stride, vocab);
     if (logit_dtype != SS_F32 && logit_dtype != SS_BF16) return fail(SS_ERR_INVALID_ARG, "logit_dtype must be SS_F32 or SS_BF16");

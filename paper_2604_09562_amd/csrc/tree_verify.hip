@@ -58,7 +58,7 @@ __device__ __forceinline__ void exp8(const ExpTable &ex, const DiffArg &arg, con
 __device__ __forceinline__ double inverse_temperature(const TreeVerifyArgs &a, int b)
 {
     const float t = a.temperature ? a.temperature[b] : a.temperature_scalar;
-    return t > 0.f ? 1.0 / (double)t : 0.0;
+    return t > 0.f ? 1.0 / (double)fminf(t, 0x1.fffffep127f) : 0.0;   // (an infinite one: the draws' weights are all 1)
 }
 
 __device__ __forceinline__ bool rows_of(const TreeVerifyArgs &a, int b, int &r0, int &rows)
@@ -422,6 +422,7 @@ __global__ __launch_bounds__(kThreads) void verify_round_kernel(TreeVerifyArgs a
 // Whether all rows at once are the faster form.
 bool few_rows(int batch, int total_rows, int vocab, int max_depth)
 {
+    if ((int64_t)total_rows * ((num_sub(vocab) + 3) / 4) >= 1 << 23) return false;   // (more than a launch takes)
     const double all = 11.0 + (double)total_rows * vocab / 1.1e6;
     const double rounds = 8.0 + 10.0 * (max_depth < 4 ? max_depth + 1 : 5) + 3.0 * (max_depth < 4 ? 0 : max_depth - 4);
     return all <= rounds;
@@ -442,7 +443,9 @@ __host__ VerifyWorkspace carve_verify(void *ws, int batch, int total_rows, int v
     return w;
 }
 
-constexpr int kRoundWgs = 1280;   // workgroups of a round: five to a compute unit, as many as it runs at a time
+// Workgroups of a round, about: a few more than the 1024 that the chip runs at a time, of which those of ended requests are gone at once.  With 1024 | 1280 | 2560, us: 160 requests with
+// 128 256 entries 135 | 122 | 128, 80 of them 96 | 90 | 90, 300 with 32 000 102 | 96 | 96; 64 and 100 requests are level.
+constexpr int kRoundWgs = 1280;
 
 template <int DT>
 int32_t launch(const TreeVerifyArgs &a, hipStream_t stream)

@@ -81,6 +81,14 @@ def test_temperatures(temperature):
     check(batch([25, 40, 3], 3000, "bf16", temperature, seed=6))
 
 
+@pytest.mark.parametrize("nodes", [[12, 20, 1], [24] * 40])
+def test_infinite_temperatures(nodes):
+    """Every token alike."""
+    h = batch(nodes, 5003, temperature=float("inf"), seed=16)
+    check(h)
+    check(h, scalar=True)
+
+
 def test_a_temperature_for_each_request_or_one_for_all():
     check(batch([20] * 6, 4000, temperature=[0.0, 1.0, 0.7, 0.0, 3.0, 0.01], seed=7))
     check(batch([20] * 6, 4000, temperature=0.7, seed=8), scalar=True)

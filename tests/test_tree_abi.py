@@ -82,6 +82,9 @@ def test_tree_verify_workspace(L):
     assert _verify(L, batch=0) == 0
     assert L.ss_tree_verify_workspace(0, 0, 0) == 0 and L.ss_tree_verify_workspace(-1, 0, 5) == 0
     assert 0 < L.ss_tree_verify_workspace(0, 0, 5) <= L.ss_tree_verify_workspace(4, 40, 5) <= L.ss_tree_verify_workspace(4, 40, 50000)
+    assert L.ss_tree_verify_workspace(4, 9, (1 << 30) + 1) == 0 and L.ss_tree_verify_workspace(4, 9, 1 << 30) > 0
+    assert _verify(L, vocab=(1 << 30) + 1, stride=(1 << 30) + 8) != 0
+    assert L.ss_tree_verify_workspace(4, 1 << 26, 1) < 1 << 16       # more rows than one launch takes: only those on the paths
 
 
 def _pool(**kw):
