@@ -146,8 +146,10 @@ __global__ __launch_bounds__(kForkThreads) void block_fork_rows_kernel(BlockFork
 // ---- releases ----------------------------------------------------------------------------------------------------------
 // Releases are counted in the order of request, logical block.  Release r takes one from its block's shares and leaves its number in the block's entry of `last`, if no later one
 // does; what is below zero then has no holder left, and goes to the list at its last release's place, behind those of lower number.
-// One workgroup does a small table; else the sums are one workgroup's, while others clear `last`, and the releases many workgroups', in three launches: taken and named, those that free
-// a block counted by pieces, put on the list (2.7 + 5 + 4.5 + 5 us for 3500 releases; with names in a launch of their own 26 us, tables followed anew in each launch).
+// One workgroup does a table of up to 2^14 entries; else the sums are one workgroup's, while others clear `last`, and the releases many workgroups', in three launches: taken and named,
+// those that free a block counted by pieces, put on the list (2.5 + 5.7 + 6.5 + 5 us for 240 000 entries; with names in a launch of their own 26 us in all). A workgroup by itself is
+// bound by six scattered accesses a release: with 64 requests of 256 entries, by number of releases, 0 | 256 | 1024 | 2048 | 4096 | 16384, 6 | 6 | 10 | 18 | 32 | 118 us, and 14.5 to 16.5
+// in four launches. A step gives back some blocks of drafts and those of a request or two that have ended.
 constexpr int kReleaseHead = 4;       // scratch: length of the free list, releases
 constexpr int kReleasePiece = 1024;   // releases whose freed blocks are counted together
 constexpr int kReleaseLds = 1024;     // requests whose sums a workgroup keeps in LDS
@@ -242,38 +244,56 @@ __device__ bool release_sums(const BlockReleaseArgs &a, ReleaseLds &lds, int32_t
 
 __global__ __launch_bounds__(kThreads) void block_release_kernel(BlockReleaseArgs a)
 {
+    constexpr int EACH = 4;   // releases of a thread that are under way together
     __shared__ ReleaseLds lds;
+    __shared__ int32_t sums[kReleaseLds + 1];
     const ReleaseScratch w = release_scratch(a.scratch, a.batch, a.max_blocks, a.num_blocks);
+    int32_t *given = a.batch <= kReleaseLds ? sums : w.given;
     int count, releases;
-    if (!release_sums(a, lds, w.given, count, releases)) return;
+    if (!release_sums(a, lds, given, count, releases)) return;
     __threadfence_block();
     __syncthreads();
-    const Releases s = {a, w, w.given};
-    for (int r = threadIdx.x; r < releases; r += kThreads) {
-        const int x = s.find(r);
-        w.ids[r] = x;
-        if (x >= 0) __hip_atomic_store(&w.last[x], -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    __threadfence_block();
-    __syncthreads();
-    for (int r = threadIdx.x; r < releases; r += kThreads) {
-        const int x = w.ids[r];
-        if (x >= 0) {
-            atomicSub(&a.shares[x], 1);
-            atomicMax(&w.last[x], r);
+    const Releases s = {a, w, given};
+    for (int lo = threadIdx.x; lo < releases; lo += EACH * kThreads) {
+        int x[EACH];
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) x[k] = lo + k * kThreads < releases ? s.find(lo + k * kThreads) : -1;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            if (lo + k * kThreads < releases) w.ids[lo + k * kThreads] = x[k];
+            if (x[k] >= 0) __hip_atomic_store(&w.last[x[k]], -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
     }
+    __threadfence_block();
+    __syncthreads();
+    for (int lo = threadIdx.x; lo < releases; lo += EACH * kThreads)
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int r = lo + k * kThreads, x = r < releases ? w.ids[r] : -1;
+            if (x >= 0) {
+                atomicSub(&a.shares[x], 1);
+                atomicMax(&w.last[x], r);
+            }
+        }
     __threadfence_block();
     __syncthreads();
     int at = count;
-    for (int lo = 0; lo < releases; lo += kThreads) {
-        const int r = lo + threadIdx.x, x = r < releases ? s.freed(r) : -1;
-        int total;
-        const int place = at + group_scan<kThreads>(x >= 0, lds.part, total) - 1;
-        if (x >= 0) {
-            if (place < a.num_blocks) a.free_ids[place] = x;
-            a.shares[x] = 0;    // (this release alone has found it below zero)
+    for (int lo = 0; lo < releases; lo += EACH * kThreads) {
+        const int first = lo + threadIdx.x * EACH;
+        int x[EACH], mine = 0, total;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            x[k] = first + k < releases ? s.freed(first + k) : -1;
+            mine += x[k] >= 0;
         }
+        int place = at + group_scan<kThreads>(mine, lds.part, total) - mine;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k)
+            if (x[k] >= 0) {
+                if (place < a.num_blocks) a.free_ids[place] = x[k];
+                a.shares[x[k]] = 0;    // (this release alone has found it below zero)
+                ++place;
+            }
         at += total;
     }
     if (threadIdx.x == 0) a.free_count[0] = min(at, a.num_blocks);
@@ -481,8 +501,9 @@ __global__ __launch_bounds__(kCompactThreads) void block_compact_rest_kernel(Blo
     compact_rest(a, s, (int64_t)blockIdx.x * kCompactThreads + threadIdx.x, (int64_t)gridDim.x * kCompactThreads);
 }
 
-// Entries up to which one workgroup does a whole call.
+// Entries of the table up to which one workgroup does a whole call.
 constexpr int kFewEntries = 4096;
+constexpr int kFewReleases = 1 << 14;   // of a release
 
 }  // namespace
 
@@ -510,7 +531,7 @@ size_t block_release_scratch_ints(int batch, int max_blocks, int num_blocks)
 int32_t block_release_launch(const BlockReleaseArgs &a, hipStream_t stream)
 {
     const int64_t entries = (int64_t)a.batch * a.max_blocks;
-    if (entries <= kFewEntries) {
+    if (entries <= kFewReleases) {
         hipLaunchKernelGGL(block_release_kernel, dim3(1), dim3(kThreads), 0, stream, a);
         SS_HIP_CHECK(hipGetLastError(), "launch block_release_kernel");
         return SS_OK;

@@ -168,7 +168,7 @@ def test_releases(batch, width, spare, seed):
 def test_many_releases_in_pieces():
     """More given back than a workgroup counts at a time, most of it shared; the last holder decides the place."""
     rng = np.random.default_rng(9)
-    for batch, width in ((300, 200), (30, 3000)):
+    for batch, width in ((300, 200), (30, 3000), (1500, 10), (160, 100), (1639, 10)):
         k = ref.random_books(rng, batch, width, 7, families=6, empty=1)
         k["kv_len"][:] = np.where(rng.random(batch) < 0.8, 0, k["kv_len"])
         got, status = run_release(k)
@@ -187,7 +187,7 @@ def test_releases_that_cannot_be():
         assert run_release(dict(k, count=count))[1] == -10
 
 
-@pytest.mark.parametrize("batch,width", [(16, 9), (80, 90)])
+@pytest.mark.parametrize("batch,width", [(16, 9), (80, 90), (200, 90)])
 def test_blocks_given_back_too_often_and_ids_that_are_none(batch, width):
     """A block twice in a table goes to the list once; what is no block's id is left where it is, and nothing is written outside the arrays."""
     rng = np.random.default_rng(11)
