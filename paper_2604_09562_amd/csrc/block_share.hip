@@ -2,7 +2,8 @@
 //
 // shares[x] counts a block's holders beyond the first.  All three calls are whole numbers in orders that their definitions fix, so the result does not
 // depend on which thread comes first: additions to shares commute, and where an order counts (which block is taken, where one comes to
-// stand in the free list) it is a prefix sum.  Bound by latency: chains of lengths, sums, ids and counts, about 1 us each.
+// stand in the free list) it is a prefix sum.  Bound by latency: chains of lengths, sums, ids and counts, about 1 us each: 96 forks of requests of 256 .. 4096 tokens 4.6 + 3.4 us, a small
+// cache's compaction 5.4, one of 3910 blocks 4.8 + 6.4.
 #include "block_share.h"
 
 namespace ss {
