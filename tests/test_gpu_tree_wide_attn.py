@@ -106,7 +106,7 @@ def test_chain_is_the_chunks_attention(kv, q, most):
 
 
 @BOTH
-@pytest.mark.parametrize("kv,q", [("bf16", "bf16"), ("fp8", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("kv,q", [("bf16", "bf16"), ("fp8", "bf16"), ("f32", "f32"), ("fp8", "f32"), ("f32", "bf16")])
 @pytest.mark.parametrize("bad", ["key", "value", "both"])
 def test_what_is_not_finite_stays_with_the_rows_that_see_it(kv, q, bad, most):
     """Two nodes hold NaN or infinities; rows that do not see them are as if they were not there, the others are not finite."""
@@ -205,10 +205,11 @@ def test_block_ids_outside_the_cache_are_not_followed():
         ref.check_tree(inp, out, lse, rows=torch.arange(30, device=DEV))
 
 
-def test_blocks_behind_four_gigabytes():
+@pytest.mark.parametrize("q", ["bf16", "f32"])
+def test_blocks_behind_four_gigabytes(q):
     """Offsets of keys and values beyond 32 bits."""
     hkv, d, n, m = 8, 128, 40, 700
-    inp = ref.tree_batch([(n, m)], 32, hkv, d, seed=13)
+    inp = ref.tree_batch([(n, m)], 32, hkv, d, q=q, seed=13)
     far = 150000     # blocks of 32 KB
     big = dict(inp, num_blocks=far)
     for name in ("k_cache", "v_cache"):
