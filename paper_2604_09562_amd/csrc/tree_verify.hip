@@ -22,6 +22,7 @@ struct Draw {           // of a row
 };
 struct Walk {           // where a request's walk is
     int32_t cur, n;     // node, -1 at its end; accepted nodes
+    float u;            // the node's uniform
 };
 
 struct VerifyWorkspace {
@@ -146,16 +147,34 @@ struct Drawn {
     __device__ Draw result(double inv_t) const { return {token, all > 0.0 ? (float)(((double)x - (double)m) * inv_t - log(all)) : 0.f}; }
 };
 
+// A row's blocks as the draw takes them: a lane's first one is asked for before the row is known to be needed.
+struct Blocks {
+    const float *top;
+    const double *sum;
+    int nsub, c0, c1;   // this lane's run of blocks
+    float top0;
+    double sum0;
+    __device__ __forceinline__ Blocks(const VerifyWorkspace &w, int64_t at) : top(w.top + at), sum(w.sum + at), nsub(w.nsub)
+    {
+        const int lane = threadIdx.x & 63, per = (nsub + 63) / 64;
+        c0 = lane * per;
+        c1 = min(c0 + per, nsub);
+        top0 = top[min(c0, nsub - 1)];
+        sum0 = sum[min(c0, nsub - 1)];
+    }
+    __device__ __forceinline__ float largest(int c) const { return c == c0 ? top0 : top[c]; }
+    __device__ __forceinline__ double mass(int c) const { return c == c0 ? sum0 : sum[c]; }
+};
+
 // The token of a row, in every lane of a workgroup.  Every wavefront scans the blocks for itself, a lane a run of them; the entries of the block are the workgroup's.
 template <int DT>
-__device__ Drawn draw_of(const TreeVerifyArgs &a, int nsub, const float *top, const double *sum, int row, double inv_t, const ExpTable &ex, DrawLds &sh)
+__device__ __forceinline__ Drawn draw_of(const TreeVerifyArgs &a, const Blocks &blocks, int row, float u, double inv_t, const ExpTable &ex, DrawLds &sh)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int per = (nsub + 63) / 64, c0 = lane * per, c1 = min(c0 + per, nsub);
+    const int c0 = blocks.c0, c1 = blocks.c1;
     const void *p = row_ptr(a.target, row, a.row_stride, DT);
-    const float u = inv_t > 0.0 ? a.uniforms[row] : 0.f;
     float own_top = -INFINITY;
-    for (int c = c0; c < c1; ++c) own_top = fmaxf(own_top, top[c]);
+    for (int c = c0; c < c1; ++c) own_top = fmaxf(own_top, blocks.largest(c));
     const float m = wave_max(own_top);
     auto entries = [&](int c, float (&x)[8]) {
         Raw8<DT> raw;
@@ -165,7 +184,10 @@ __device__ Drawn draw_of(const TreeVerifyArgs &a, int nsub, const float *top, co
     Drawn d = {0, 0.f, m, 0.0};
     if (inv_t > 0.0 && m < INFINITY && m > -INFINITY) {
         const DiffArg arg(inv_t, m);
-        auto mass_of = [&](int c) { return top[c] == -INFINITY ? 0.0 : sum[c] * ex(arg(top[c])); };
+        auto mass_of = [&](int c) {
+            const float top = blocks.largest(c);
+            return top == -INFINITY ? 0.0 : blocks.mass(c) * ex(arg(top));
+        };
         double own = 0.0;
         int own_last = -1;   // last block of this lane with mass
         for (int c = c0; c < c1; ++c) {
@@ -179,7 +201,7 @@ __device__ Drawn draw_of(const TreeVerifyArgs &a, int nsub, const float *top, co
         const int owner = take_last ? 63 - __builtin_clzll(some) : __builtin_ctzll(over);
         double pre = cum - own;
         int cs = own_last;
-        if (per > 1 && lane == owner) {   // inside the lane's run: the first with mass whose running sum crosses (rounding may leave none: then the last with mass)
+        if (c1 - c0 > 1 && lane == owner) {   // inside the lane's run: the first with mass whose running sum crosses (rounding may leave none: then the last with mass)
             double run = pre;
             bool found = false;
             for (int c = c0; c < c1; ++c) {
@@ -197,8 +219,9 @@ __device__ Drawn draw_of(const TreeVerifyArgs &a, int nsub, const float *top, co
         float x[8];
         double r[8];
         entries(block, x);
-        exp8(ex, DiffArg(inv_t, top[block]), x, r);
-        const double level = ex(arg(top[block]));
+        const float top = blocks.top[block];
+        exp8(ex, DiffArg(inv_t, top), x, r);
+        const double level = ex(arg(top));
         double local = 0.0;
         int my_last = -1;
 #pragma unroll
@@ -245,7 +268,7 @@ __device__ Drawn draw_of(const TreeVerifyArgs &a, int nsub, const float *top, co
     if (m > -INFINITY) {   // the lowest token whose logit is the largest
         int c = 0x7fffffff;
         for (int i = c0; i < c1; ++i)
-            if (top[i] == m) { c = i; break; }
+            if (blocks.largest(i) == m) { c = i; break; }
         c = wave_min(c);
         float x[8];
         entries(c, x);
@@ -337,11 +360,13 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(TreeVerifyArgs a,
     __shared__ ExpTable ex;
     __shared__ DrawLds sh;
     __shared__ int sh_b[4];
-    const int row = blockIdx.x, b = request_of(a, row, sh_b);
+    const int row = blockIdx.x;
+    const Blocks blocks(w, (int64_t)row * w.nsub);
+    const int b = request_of(a, row, sh_b);
     if (b < 0) return;
     ex.init();
     const double inv_t = inverse_temperature(a, b);
-    const Drawn d = draw_of<DT>(a, w.nsub, w.top + (int64_t)row * w.nsub, w.sum + (int64_t)row * w.nsub, row, inv_t, ex, sh);
+    const Drawn d = draw_of<DT>(a, blocks, row, inv_t > 0.0 ? a.uniforms[row] : 0.f, inv_t, ex, sh);
     if (threadIdx.x == 0) w.draw[row] = d.result(inv_t);
 }
 
@@ -377,10 +402,12 @@ __global__ __launch_bounds__(kThreads) void verify_round_kernel(TreeVerifyArgs a
     const int groups = (w.nsub + 4 * each - 1) / (4 * each), b = blockIdx.x / groups, group = blockIdx.x % groups;
     const bool first = group == 0 && threadIdx.x == 0;   // whose the outputs are
     Walk *walk = w.walk + (int64_t)(r & 1) * a.batch + b;
+    const Blocks blocks(w, ((int64_t)((r - 1) & 1) * a.batch + b) * w.nsub);   // (in round 0 of nothing)
     int r0, rows;
     const bool has = rows_of(a, b, r0, rows);
     const double inv_t = inverse_temperature(a, b);
-    Walk at = {has ? 0 : -1, 0};
+    auto uniform_of = [&](int node) { return inv_t > 0.0 ? a.uniforms[r0 + node] : 0.f; };
+    Walk at = {has ? 0 : -1, 0, has && r == 0 ? uniform_of(0) : 0.f};
     if (r == 0) {
         if (group == 0) clear_outputs(a, b);
     } else {
@@ -394,21 +421,20 @@ __global__ __launch_bounds__(kThreads) void verify_round_kernel(TreeVerifyArgs a
     Drawn d = {};
     int n = -1;   // whose draw that is
     if (r > 0) {
-        const int64_t front = ((int64_t)((r - 1) & 1) * a.batch + b) * w.nsub;
         const Candidate mine = candidate(a, r0, rows, at.cur);
         n = at.n;
-        d = draw_of<DT>(a, w.nsub, w.top + front, w.sum + front, r0 + at.cur, inv_t, ex, sh);
+        d = draw_of<DT>(a, blocks, r0 + at.cur, at.u, inv_t, ex, sh);
         const int c = n < a.max_depth ? child_with(a, mine, r0, rows, at.cur, d.token, sh) : 0x7fffffff;
         if (c == 0x7fffffff) {
             if (first) {
                 emit(a, b, n, d.result(inv_t));
                 a.accepted_len[b] = n;
-                *walk = {-1, n};
+                *walk = {-1, n, 0.f};
             }
             return;
         }
         if (first) a.accepted_nodes[(int64_t)b * SS_MAX_DEPTH + n] = c;
-        at = {c, n + 1};
+        at = {c, n + 1, first ? uniform_of(c) : 0.f};
     }
     if (first) *walk = at;
     const int64_t back = ((int64_t)(r & 1) * a.batch + b) * w.nsub;
