@@ -176,6 +176,38 @@ def test_many_releases_in_pieces():
         ref.check_books(got)
 
 
+@pytest.mark.parametrize("batch,width,ended", [(2000, 9000, 150), (400, 9000, 130)])
+def test_releases_of_more_entries_than_are_kept_and_of_more_pieces_than_workgroups(batch, width, ended):
+    rng = np.random.default_rng(14)
+    own = ended * width
+    N = own + batch
+    perm = rng.permutation(N).astype(np.int32)
+    held, kv_len = np.ones(batch, np.int32), np.full(batch, 16, np.int32)
+    rows = rng.permutation(batch)[:ended]
+    held[rows], kv_len[rows] = width, rng.integers(0, 40, ended)
+    table = np.full((batch, width), -3, np.int32)
+    table[:, 0] = perm[own:]
+    table[rows] = perm[:own].reshape(ended, width)
+    shares = np.zeros(N, np.int32)
+    twice = table[rows[3], 100:7000].copy()       # what one of them holds, another does, too, and some of it a third one, which goes on
+    table[rows[7], 200:7100] = twice
+    shares[twice] = 1
+    shares[twice[::5]] = 2
+    k = dict(table=table, held=held, kv_len=kv_len, shares=shares, free=np.full(N, -1, np.int32), count=0, num_blocks=N)
+    d, status = device(k), ints(1)
+    binding.ss_block_release(d, status, workspace(d))
+    torch.cuda.synchronize()
+    keep = -(-kv_len // 16)
+    given = np.concatenate([table[b, keep[b]:held[b]] for b in range(batch)])
+    assert len(given) > 1 << 20 and int(status) == 0
+    left, last = shares - np.bincount(given, minlength=N), np.zeros(N, np.int64)
+    last[given] = np.arange(len(given))           # (of several the last one stays)
+    freed = given[(left[given] < 0) & (last[given] == np.arange(len(given)))]
+    free = k["free"].copy()
+    free[:len(freed)] = freed
+    same(d, dict(k, held=np.minimum(held, keep), shares=np.maximum(left, 0).astype(np.int32), free=free, count=len(freed)))
+
+
 def test_releases_that_cannot_be():
     k = ref.random_books(np.random.default_rng(10), 9, 8, 5)
     for name, at, value, want in (("kv_len", 3, -1, -4), ("held", 8, 9, -9), ("held", 0, -2, -1), ("held", 2, 2 ** 31 - 1, -3)):
