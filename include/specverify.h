@@ -328,7 +328,8 @@ int32_t ss_kv_append(const ss_paged_kv *kv, const ss_batch *batch, const void *k
  *   accepted_nodes  device int32 [batch][SS_MAX_DEPTH], as written by ss_spec_accept_tree_greedy or ss_tree_verify
  *   accepted_len    device int32 [batch]
  * A row of accepted_nodes that is not increasing within 1..q_len-1 ends that request's moves at the
- * offending entry (nothing outside the request's new slots is ever touched).
+ * offending entry (nothing outside the request's new slots is ever touched), so does a block id outside the cache; a
+ * request whose kv_len is below q_len or beyond its row of the table is left alone.
  * Errors: SS_ERR_INVALID_ARG (NULL pointers, bad dtypes or sizes), SS_ERR_DEVICE (launch failure).
  */
 int32_t ss_kv_compact(const ss_paged_kv *kv, const ss_batch *batch, const int32_t *accepted_nodes,
@@ -384,7 +385,7 @@ typedef struct ss_block_pool {
  *               lengths (kv_len below its rows, rows outside [0, total_rows], more blocks than the table has columns), s = -1-batch:
  *               the free list's length has.  Then table, held and free list are as they were and every slot is -1, so that
  *               ss_kv_write writes nothing; ss_chunk_attn behind it stays inside its arrays, but what it puts out is of no use.  Calls
- *               that follow the table without bounds (ss_kv_append, ss_spec_verify_attn) must not be made before status is known to be 0.
+ *               that follow the table without bounds (ss_kv_append, ss_spec_verify_attn) or write by it (ss_kv_compact) must not be made before status is known to be 0.
  *   workspace   device, >= ss_block_map_workspace(batch) bytes, 256-byte aligned; contents are scratch
  * One call at a time for one pool.  A block that a request gives back here must be its own alone: where blocks may be shared,
  * ss_block_release stands in front of this call and leaves it nothing to give back.

@@ -428,6 +428,7 @@ static KvAppendArgs kv_write_args(const ss_paged_kv *kv, const ss_batch *batch)
     a.batch = batch->batch; a.max_blocks = batch->max_blocks_per_seq;
     a.block_table = batch->block_table; a.kv_len = batch->kv_len; a.q_indptr = batch->q_indptr;
     a.max_q_len = batch->max_q_len ? batch->max_q_len : SS_OUT_WIDTH;
+    a.num_blocks = kv->num_blocks;
     return a;
 }
 

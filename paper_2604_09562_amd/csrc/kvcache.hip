@@ -121,6 +121,7 @@ __global__ __launch_bounds__(64) void kv_compact_kernel(KvAppendArgs a, const in
     const int h = blockIdx.x % a.num_kv_heads, b = blockIdx.x / a.num_kv_heads;
     const int q_len = a.q_indptr[b + 1] - a.q_indptr[b];
     const int P = a.kv_len[b] - q_len;
+    if (a.kv_len[b] < q_len || a.kv_len[b] > (int64_t)a.max_blocks * kTile) return;   // no request's lengths
     const int n = min(accepted_len[b], min(q_len - 1, SS_MAX_DEPTH));
     const int D = a.head_dim;
     const int32_t *bt = a.block_table + (int64_t)b * a.max_blocks;
@@ -132,6 +133,7 @@ __global__ __launch_bounds__(64) void kv_compact_kernel(KvAppendArgs a, const in
         if (node == j) continue;
         const int ps = P + node, pd = P + j;
         const int64_t blk_s = bt[ps / kTile], blk_d = bt[pd / kTile];
+        if ((uint64_t)blk_s >= (uint64_t)a.num_blocks || (uint64_t)blk_d >= (uint64_t)a.num_blocks) break;   // no block's ids
         const int64_t src = ((blk_s * a.num_kv_heads + h) * kTile + ps % kTile) * D + lane * EPL;
         const int64_t dst = ((blk_d * a.num_kv_heads + h) * kTile + pd % kTile) * D + lane * EPL;
 #pragma unroll
