@@ -55,11 +55,12 @@ __device__ __forceinline__ void exp8(const ExpTable &ex, const DiffArg &arg, con
     }
 }
 
-// 1 / T, or 0 for the largest logit's token
+// 1 / T, or 0 for the largest logit's token.  Of an infinite T something so small that the difference of any two floats, 2^129 at most, times it leaves every exponential at one, and
+// above zero, so that minus infinity is masked as ever.
 __device__ __forceinline__ double inverse_temperature(const TreeVerifyArgs &a, int b)
 {
     const float t = a.temperature ? a.temperature[b] : a.temperature_scalar;
-    return t > 0.f ? 1.0 / (double)fminf(t, 0x1.fffffep127f) : 0.0;   // (an infinite one: the draws' weights are all 1)
+    return t > 0.f ? t < INFINITY ? 1.0 / (double)t : 0x1p-1000 : 0.0;
 }
 
 __device__ __forceinline__ bool rows_of(const TreeVerifyArgs &a, int b, int &r0, int &rows)
