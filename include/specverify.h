@@ -485,7 +485,8 @@ int32_t ss_tree_attn(const ss_paged_kv *kv, const ss_batch *batch, const uint32_
  *   out_tokens      device int32 [batch][SS_OUT_WIDTH]: the n + 1 emitted tokens, then -1
  *   accepted_nodes  device int32 [batch][SS_MAX_DEPTH]: the accepted node numbers in path order, then -1 (what ss_kv_compact takes)
  *   logprobs        device float [batch][SS_OUT_WIDTH] or NULL: ln p of each emitted token (0 where it was not drawn from a distribution), then 0
- *   workspace       device, >= ss_tree_verify_workspace(...) bytes, 256-byte aligned; contents are scratch
+ *   workspace       device, >= ss_tree_verify_workspace(...) bytes, 256-byte aligned; contents are scratch.  One that was sized for a larger batch or
+ *                   more rows (of the same or a larger vocabulary) serves, too
  * Sums and the draw are fp64 with fixed orders, so that the tokens are those of a 64-bit reference.
  */
 size_t ss_tree_verify_workspace(int32_t batch, int32_t total_rows, int32_t vocab);

@@ -140,13 +140,14 @@ int32_t ss_tree_verify(int32_t batch, int32_t vocab, int64_t row_stride, int32_t
     if (!aligned16(target_logits) || row_stride * (logit_dtype == SS_F32 ? 4 : 2) % 16)
         return fail(SS_ERR_INVALID_ARG, "logits rows must start 16-byte aligned (base and row_stride)");
     if (batch >= 1 << 24) return fail(SS_ERR_UNSUPPORTED, "batch too large for one launch");
-    const int32_t rc = check_workspace(workspace, workspace_bytes, tree_verify_workspace_bytes(batch, total_rows, vocab));
+    const int32_t rc = check_workspace(workspace, workspace_bytes, tree_verify_least_bytes(batch, vocab));
     if (rc != SS_OK) return rc;
     TreeVerifyArgs a{};
     a.batch = batch; a.vocab = vocab; a.logit_dtype = logit_dtype; a.total_rows = total_rows; a.max_depth = max_depth ? max_depth : SS_MAX_DEPTH;
     a.row_stride = row_stride; a.q_indptr = q_indptr; a.parent = tree_parent; a.tokens = node_tokens; a.target = target_logits;
     a.uniforms = uniforms; a.temperature = temperature; a.temperature_scalar = temperature_scalar;
-    a.accepted_len = accepted_len; a.out_tokens = out_tokens; a.accepted_nodes = accepted_nodes; a.logprobs = logprobs; a.workspace = workspace;
+    a.accepted_len = accepted_len; a.out_tokens = out_tokens; a.accepted_nodes = accepted_nodes; a.logprobs = logprobs;
+    a.workspace = workspace; a.workspace_bytes = workspace_bytes;
     return tree_verify_launch(a, static_cast<hipStream_t>(stream));
 }
 

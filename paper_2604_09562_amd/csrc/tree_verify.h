@@ -15,7 +15,9 @@ struct TreeVerifyArgs {
     int32_t *accepted_len, *out_tokens, *accepted_nodes;
     float *logprobs;                       // may be nullptr
     void *workspace;
+    size_t workspace_bytes;
 };
+size_t tree_verify_least_bytes(int batch, int vocab);
 size_t tree_verify_workspace_bytes(int batch, int total_rows, int vocab);
 int32_t tree_verify_launch(const TreeVerifyArgs &a, hipStream_t stream);
 

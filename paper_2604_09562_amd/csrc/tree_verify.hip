@@ -12,6 +12,7 @@
 // summed; the exponentials of those are half of that).
 #include "accept_common.h"
 #include "tree_verify.h"
+#include "tree_verify_rule.h"
 
 namespace ss {
 namespace {
@@ -446,29 +447,28 @@ __global__ __launch_bounds__(kThreads) void verify_round_kernel(TreeVerifyArgs a
     if (first && n >= 0) emit(a, b, n, d.result(inv_t));
 }
 
-// Whether all rows at once are the faster form.
-bool few_rows(int batch, int total_rows, int vocab, int max_depth)
-{
-    if ((int64_t)total_rows * ((num_sub(vocab) + 3) / 4) >= 1 << 23) return false;   // (more than a launch takes)
-    const double all = 11.0 + (double)total_rows * vocab / 1.1e6;
-    const double rounds = 8.0 + 10.0 * (max_depth < 4 ? max_depth + 1 : 5) + 3.0 * (max_depth < 4 ? 0 : max_depth - 4);
-    return all <= rounds;
-}
-
-__host__ VerifyWorkspace carve_verify(void *ws, int batch, int total_rows, int vocab, size_t *bytes)
+// Room for the sums and draws of so many rows.
+__host__ VerifyWorkspace carve_verify(void *ws, int batch, int64_t rows, int vocab, size_t *bytes)
 {
     VerifyWorkspace w;
     w.nsub = num_sub(vocab);
-    // (any max_depth's: a workspace serves them all)
-    const size_t rows = few_rows(batch, total_rows, vocab, SS_MAX_DEPTH) && total_rows > 2 * batch ? total_rows : 2 * (size_t)batch, n = rows * w.nsub;
+    const size_t n = (size_t)rows * w.nsub;
     char *p = static_cast<char *>(ws);
     w.sum = reinterpret_cast<double *>(p); p += align_up(sizeof(double) * n, 256);
     w.top = reinterpret_cast<float *>(p); p += align_up(sizeof(float) * n, 256);
-    w.draw = reinterpret_cast<Draw *>(p); p += align_up(sizeof(Draw) * rows, 256);
+    w.draw = reinterpret_cast<Draw *>(p); p += align_up(sizeof(Draw) * (size_t)rows, 256);
     w.walk = reinterpret_cast<Walk *>(p); p += align_up(2 * sizeof(Walk) * (size_t)batch, 256);
     *bytes = (size_t)(p - static_cast<char *>(ws)) + 256;
     return w;
 }
+size_t verify_bytes(int batch, int64_t rows, int vocab)
+{
+    size_t bytes;
+    carve_verify(nullptr, batch, rows, vocab, &bytes);
+    return bytes;
+}
+// Rounds have two rows a request, which is the least room that either form is given.
+int64_t round_rows(int batch) { return 2 * (int64_t)batch; }
 
 // Workgroups of a round, about: a few more than the 1024 that the chip runs at a time, of which those of ended requests are gone at once.  With 1024 | 1280 | 2560, us: 160 requests with
 // 128 256 entries 135 | 122 | 128, 80 of them 96 | 90 | 90, 300 with 32 000 102 | 96 | 96; 64 and 100 requests are level.
@@ -477,10 +477,12 @@ constexpr int kRoundWgs = 1280;
 template <int DT>
 int32_t launch(const TreeVerifyArgs &a, hipStream_t stream)
 {
+    const int64_t rows = a.total_rows > round_rows(a.batch) ? a.total_rows : round_rows(a.batch);
+    const bool at_once = verify_all_rows(a.batch, a.total_rows, a.vocab, a.max_depth) && verify_bytes(a.batch, rows, a.vocab) <= a.workspace_bytes;
     size_t unused;
-    const VerifyWorkspace w = carve_verify(a.workspace, a.batch, a.total_rows, a.vocab, &unused);
+    const VerifyWorkspace w = carve_verify(a.workspace, a.batch, at_once ? rows : round_rows(a.batch), a.vocab, &unused);
     const dim3 wg(kThreads);
-    if (few_rows(a.batch, a.total_rows, a.vocab, a.max_depth)) {
+    if (at_once) {
         if (a.total_rows > 0) {
             hipLaunchKernelGGL(verify_sums_kernel<DT>, dim3((unsigned)a.total_rows * (unsigned)((w.nsub + 3) / 4)), wg, 0, stream, a, w);
             hipLaunchKernelGGL(verify_draw_kernel<DT>, dim3((unsigned)a.total_rows), wg, 0, stream, a, w);
@@ -502,11 +504,18 @@ int32_t launch(const TreeVerifyArgs &a, hipStream_t stream)
 
 }  // namespace
 
+size_t tree_verify_least_bytes(int batch, int vocab) { return verify_bytes(batch, round_rows(batch), vocab); }
+
+// What any max_depth takes, of this call and of those with fewer rows or requests: a program has one workspace for its largest step.  (Calls of more rows than a launch takes are no
+// bound that a program would have: they get what they need.)
 size_t tree_verify_workspace_bytes(int batch, int total_rows, int vocab)
 {
-    size_t bytes;
-    carve_verify(nullptr, batch, total_rows, vocab, &bytes);
-    return bytes;
+    int64_t rows = 0;
+    if (total_rows * verify_fours(vocab) < kVerifyGroups) {
+        const int64_t most = verify_most_rows(batch, vocab, SS_MAX_DEPTH);
+        rows = total_rows < most ? total_rows : most;
+    }
+    return verify_bytes(batch, rows > round_rows(batch) ? rows : round_rows(batch), vocab);
 }
 
 int32_t tree_verify_launch(const TreeVerifyArgs &a, hipStream_t stream)
