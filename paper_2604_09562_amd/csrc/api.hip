@@ -460,7 +460,7 @@ int32_t ss_kv_compact(const ss_paged_kv *kv, const ss_batch *batch, const int32_
     if (!accepted_nodes || !accepted_len) return fail(SS_ERR_INVALID_ARG, "a required device pointer is NULL");
     if (g_validate) {
         const int32_t rc = validate_chunk(batch->block_table, batch->kv_len, batch->q_indptr, batch->batch, batch->max_blocks_per_seq, kv->num_blocks,
-                                          total_rows, batch->max_q_len ? batch->max_q_len : total_rows, static_cast<hipStream_t>(stream), "ss_kv_compact");
+                                          total_rows, batch->max_q_len ? batch->max_q_len : total_rows, true, static_cast<hipStream_t>(stream), "ss_kv_compact");
         if (rc != SS_OK) return rc;
     }
     return kv_compact_launch(kv_write_args(kv, batch), accepted_nodes, accepted_len, static_cast<hipStream_t>(stream));

@@ -130,7 +130,7 @@ int32_t ss_chunk_attn(const ss_paged_kv *kv, const ss_batch *batch, const void *
     if (workspace_bytes < need) return fail(SS_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
     if (option_validate()) {
         rc = validate_chunk(batch->block_table, batch->kv_len, batch->q_indptr, batch->batch, batch->max_blocks_per_seq, kv->num_blocks, total_rows,
-                            batch->max_q_len ? batch->max_q_len : total_rows, static_cast<hipStream_t>(stream), "ss_chunk_attn");
+                            batch->max_q_len ? batch->max_q_len : total_rows, false, static_cast<hipStream_t>(stream), "ss_chunk_attn");
         if (rc != SS_OK) return rc;
     }
     ChunkArgs a{};

@@ -94,7 +94,7 @@ int32_t ss_tree_attn(const ss_paged_kv *kv, const ss_batch *batch, const uint32_
     if ((rc = check_workspace(workspace, workspace_bytes, f.workspace)) != SS_OK) return rc;
     if (option_validate()) {
         rc = validate_chunk(batch->block_table, batch->kv_len, batch->q_indptr, batch->batch, batch->max_blocks_per_seq, kv->num_blocks, total_rows,
-                            batch->max_q_len ? batch->max_q_len : total_rows, static_cast<hipStream_t>(stream), "ss_tree_attn");
+                            batch->max_q_len ? batch->max_q_len : total_rows, false, static_cast<hipStream_t>(stream), "ss_tree_attn");
         if (rc != SS_OK) return rc;
     }
     ChunkArgs a{};

@@ -86,7 +86,7 @@ int32_t tree_unit_launch(const ChunkArgs &a, const TreeUnitChoice &how, hipStrea
 
 // ---- optional checks of device-resident metadata -----------------------------------------------
 int32_t validate_chunk(const int32_t *block_table, const int32_t *kv_len, const int32_t *q_indptr, int batch, int max_blocks,
-                       int num_blocks, int total_rows, int max_q_len, hipStream_t stream, const char *what);
+                       int num_blocks, int total_rows, int max_q_len, bool cached, hipStream_t stream, const char *what);
 int32_t validate_slots(const int32_t *slot_map, int total_rows, int64_t slots, bool runs, hipStream_t stream, const char *what);
 
 }  // namespace ss

@@ -114,9 +114,9 @@ __global__ __launch_bounds__(256) void validate_accept_kernel(const int32_t *dra
     __threadfence_system();
 }
 
-// Chunks of any length, requests without new tokens, rows behind the last request's.
+// Chunks of any length, requests without new tokens, rows behind the last request's.  cached: the new tokens stand in the cache, whose lengths count them.
 __global__ __launch_bounds__(256) void validate_chunk_kernel(const int32_t *block_table, const int32_t *kv_len, const int32_t *q_indptr, int batch,
-                                                             int max_blocks, int num_blocks, int total_rows, int max_q_len, CheckRecord *out)
+                                                             int max_blocks, int num_blocks, int total_rows, int max_q_len, int cached, CheckRecord *out)
 {
     __shared__ int bad_req, bad_block;
     const int tid = threadIdx.x;
@@ -126,7 +126,8 @@ __global__ __launch_bounds__(256) void validate_chunk_kernel(const int32_t *bloc
     for (int b = tid; b < batch; b += 256) {
         const int q0 = q_indptr[b], q1 = q_indptr[b + 1], L = kv_len[b];
         const long long nblk = ((long long)L + kTile - 1) / kTile;
-        if (q0 < 0 || q1 < q0 || q1 > total_rows || q1 - q0 > max_q_len || (b == 0 && q0 != 0) || L < 0 || nblk > max_blocks) atomicMin(&bad_req, b);
+        if (q0 < 0 || q1 < q0 || q1 > total_rows || q1 - q0 > max_q_len || (b == 0 && q0 != 0) || L < 0 || (cached && L < q1 - q0) || nblk > max_blocks)
+            atomicMin(&bad_req, b);
     }
     __syncthreads();
     const int good = min(bad_req, batch);   // the lengths of the requests in front of the first bad one bound the reads of the table
@@ -148,7 +149,7 @@ __global__ __launch_bounds__(256) void validate_chunk_kernel(const int32_t *bloc
         if (b == 0 && q0 != 0) r = {CK_QSTART, b, q0, 0};
         else if (q1 < q0 || q1 - q0 > max_q_len) r = {CK_CHUNK_ROWS, b, q1 - q0, max_q_len};
         else if (q0 < 0 || q1 > total_rows) r = {CK_CHUNK_ROWS, b, q1, total_rows};
-        else if (L < 0) r = {CK_KVLEN, b, L, q1 - q0};
+        else if (L < 0 || (cached && L < q1 - q0)) r = {CK_KVLEN, b, L, q1 - q0};
         else r = {CK_BLOCKS, b, L, max_blocks};
     }
     if (tid != 0) return;
@@ -232,13 +233,13 @@ int32_t validate_batch(const int32_t *block_table, const int32_t *kv_len, const 
 }
 
 int32_t validate_chunk(const int32_t *block_table, const int32_t *kv_len, const int32_t *q_indptr, int batch, int max_blocks,
-                       int num_blocks, int total_rows, int max_q_len, hipStream_t stream, const char *what)
+                       int num_blocks, int total_rows, int max_q_len, bool cached, hipStream_t stream, const char *what)
 {
     CheckRecord *host = nullptr, *dev = nullptr;
     const int32_t rc = record(&host, &dev);
     if (rc != SS_OK) return rc;
     hipLaunchKernelGGL(validate_chunk_kernel, dim3(1), dim3(256), 0, stream, block_table, kv_len, q_indptr, batch, max_blocks, num_blocks, total_rows,
-                       max_q_len, dev);
+                       max_q_len, cached ? 1 : 0, dev);
     SS_HIP_CHECK(hipGetLastError(), "launch validate_chunk_kernel");
     SS_HIP_CHECK(hipStreamSynchronize(stream), "hipStreamSynchronize (validation)");
     return report(*host, what);
