@@ -298,7 +298,7 @@ def alloc_attention_outputs(d: Dict[str, object], device="cuda:0", max_q_len: in
 # --------------------------------------------------------------------------------------------
 # What stands behind an address is looked at first: a 64-bit slot map (torch's own kind of index) would be read as pairs, and these calls write where it says.
 # What a call gets of its own is checked at each call, the batch that it gets it for where outputs and workspaces are allocated (all of it at each call
-# would be 2 of 10 us).
+# would be 2 of 10 us); the books of shared blocks at each call, too.
 _INT32 = torch.int32
 _SIZE = {"f32": 4, "bf16": 2, "fp8": 1}
 
@@ -494,18 +494,21 @@ def alloc_tree_verify_outputs(d: Dict[str, object], device="cuda:0"):
 
 
 def _books(d: Dict[str, object]):
-    """Descriptors of a batch's table and of its cache's free blocks, which are looked at where their workspace is allocated."""
-    bt = ss_batch(d["batch"], d["max_blocks_per_seq"], 0, 0, d["block_table"].data_ptr(), d["kv_len"].data_ptr(), 0, 0)
-    return bt, ss_block_pool(d["num_blocks"], d["free_ids"].data_ptr(), d["free_count"].data_ptr())
+    """Descriptors of a batch's table and of its cache's free blocks, and the addresses of what requests hold and share.  All of it is looked at in every call: these write where lengths
+    and ids say, a program makes new lengths in every step, and 64-bit ones would be read as pairs (1.1 to 1.6 of the 7 to 8 us that a call takes of the host)."""
+    B, N, shares = d["batch"], d["num_blocks"], d["shares"]
+    bt = ss_batch(B, d["max_blocks_per_seq"], 0, 0, _ints("block_table", d["block_table"], B * d["max_blocks_per_seq"]), _ints("kv_len", d["kv_len"], B), 0, 0)
+    pool = ss_block_pool(N, _ints("free_ids", d["free_ids"], N), _ints("free_count", d["free_count"], 1))
+    return bt, pool, _ints("held", d["held"], B), 0 if shares is None else _ints("shares", shares, N)
 
 
 def ss_block_fork(d: Dict[str, object], parent: torch.Tensor, child: torch.Tensor, length: Optional[torch.Tensor], copy_src: torch.Tensor,
                   copy_dst: torch.Tensor, status: torch.Tensor, workspace: torch.Tensor) -> None:
     """Enqueue the forks parent[i] -> child[i] (int32) of the first length[i] tokens (None: all): `block_table`, `kv_len`, `held`, `shares` and `free_count` in
     place, and the blocks that ss_block_copy is to copy."""
-    bt, pool = _books(d)
+    bt, pool, held, shares = _books(d)
     n = parent.numel()
-    _check(lib().ss_block_fork(ctypes.byref(bt), ctypes.byref(pool), d["shares"].data_ptr(), d["held"].data_ptr(), n,
+    _check(lib().ss_block_fork(ctypes.byref(bt), ctypes.byref(pool), shares, held, n,
                                _ints("parent", parent, n), _ints("child", child, n), 0 if length is None else _ints("length", length, n),
                                _ints("copy_src", copy_src, n), _ints("copy_dst", copy_dst, n), _ints("status", status, 1), workspace.data_ptr(),
                                workspace.nbytes, _stream()))
@@ -513,27 +516,22 @@ def ss_block_fork(d: Dict[str, object], parent: torch.Tensor, child: torch.Tenso
 
 def ss_block_release(d: Dict[str, object], status: torch.Tensor, workspace: torch.Tensor) -> None:
     """Enqueue the return of what requests hold beyond their `kv_len`: `held`, `shares`, `free_ids` and `free_count` in place."""
-    bt, pool = _books(d)
-    _check(lib().ss_block_release(ctypes.byref(bt), ctypes.byref(pool), d["shares"].data_ptr(), d["held"].data_ptr(),
-                                  _ints("status", status, 1), workspace.data_ptr(), workspace.nbytes, _stream()))
+    bt, pool, held, shares = _books(d)
+    _check(lib().ss_block_release(ctypes.byref(bt), ctypes.byref(pool), shares, held, _ints("status", status, 1), workspace.data_ptr(), workspace.nbytes, _stream()))
 
 
 def ss_block_compact(d: Dict[str, object], remap: Optional[torch.Tensor], copy_src: torch.Tensor, copy_dst: torch.Tensor, num_copies: torch.Tensor,
                      status: torch.Tensor, workspace: torch.Tensor) -> None:
     """Enqueue the renumbering of the blocks in use to the front of the cache (`block_table`, `shares` and `free_ids` in place), and what ss_block_copy is to copy."""
-    bt, pool = _books(d)
-    N, shares = d["num_blocks"], d["shares"]
-    _check(lib().ss_block_compact(ctypes.byref(bt), ctypes.byref(pool), _ptr(shares), d["held"].data_ptr(),
-                                  0 if remap is None else _ints("remap", remap, N), _ints("copy_src", copy_src, N // 2), _ints("copy_dst", copy_dst, N // 2),
+    bt, pool, held, shares = _books(d)
+    N = d["num_blocks"]
+    _check(lib().ss_block_compact(ctypes.byref(bt), ctypes.byref(pool), shares, held, 0 if remap is None else _ints("remap", remap, N), _ints("copy_src", copy_src, N // 2), _ints("copy_dst", copy_dst, N // 2),
                                   _ints("num_copies", num_copies, 1), _ints("status", status, 1), workspace.data_ptr(), workspace.nbytes, _stream()))
 
 
 def alloc_block_share_workspace(d: Dict[str, object], device="cuda:0", num_forks: int = 0) -> torch.Tensor:
-    """A workspace that ss_block_fork (of up to num_forks), ss_block_release and ss_block_compact can take in turn, for a batch whose arrays are looked at here."""
-    B, N = d["batch"], d["num_blocks"]
-    for name, n in (("block_table", B * d["max_blocks_per_seq"]), ("kv_len", B), ("held", B), ("shares", N if d["shares"] is not None else 0), ("free_ids", N), ("free_count", 1)):
-        if d[name] is not None:
-            _ints(name, d[name], n)
+    """A workspace that ss_block_fork (of up to num_forks), ss_block_release and ss_block_compact can take in turn."""
+    _books(d)
     sizes = (lib().ss_block_fork_workspace(d["batch"], num_forks), lib().ss_block_release_workspace(d["batch"], d["max_blocks_per_seq"], d["num_blocks"]),
              lib().ss_block_compact_workspace(d["num_blocks"]))
     if 0 in sizes:
