@@ -477,9 +477,10 @@ int32_t ss_tree_attn(const ss_paged_kv *kv, const ss_batch *batch, const uint32_
  *   node_tokens     device int32 [total_rows]: the nodes' tokens (node 0's is not looked at)
  *   target_logits   rows of vocab entries, row_stride elements apart (>= vocab), in logit_dtype (SS_F32 or SS_BF16), 16-byte aligned; minus
  *                   infinity and NaN are masked.  A row with an infinite logit gives the first such token, one with nothing but masked ones token 0
- *   uniforms        device float [total_rows] in [0, 1), one for the draw at each node; NULL if temperature is NULL and temperature_scalar <= 0
+ *   uniforms        device float [total_rows] in [0, 1), one for the draw at each node; NULL if temperature is NULL and temperature_scalar 0
  *   temperature     device float [batch], or NULL to use temperature_scalar for all; 0 and below (and NaN): the largest logit's token; infinity: any
- *                   token that is not masked, all alike
+ *                   token that is not masked, all alike.  temperature_scalar, which the host sees, must be 0 or above (infinity included) where it is
+ *                   used: below 0 and NaN are refused
  *   accepted_len    device int32 [batch]: accepted nodes n (0 for a request without rows, whose other outputs are all -1 and 0; so is one whose rows lie
  *                   outside [0, total_rows])
  *   out_tokens      device int32 [batch][SS_OUT_WIDTH]: the n + 1 emitted tokens, then -1
