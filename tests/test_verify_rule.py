@@ -63,3 +63,8 @@ def test_a_workspace_serves_every_smaller_step(size, batch, vocab):
 def test_workspaces_stay_small(size):
     for vocab in (5000, 32000, 128256, 600_001):
         assert size(1, 1 << 13, vocab) < 1 << 20 and size(64, 1 << 13, vocab) < 1 << 20
+
+
+def test_few_rows_are_taken_at_once_and_many_are_not(rule):
+    assert rule.all_rows(1, 25, 32000, 6) and rule.all_rows(64, 64 * 12, 32000, 8) and rule.all_rows(64, 64, 128256, 20)
+    assert not rule.all_rows(64, 64 * 40, 128256, 8) and not rule.all_rows(20000, 60000, 1000, 8) and not rule.all_rows(1000, 48000, 100, 8)
