@@ -65,6 +65,12 @@ def test_workspaces_stay_small(size):
         assert size(1, 1 << 13, vocab) < 1 << 20 and size(64, 1 << 13, vocab) < 1 << 20
 
 
+def test_the_cases_of_rounds_are_taken_in_rounds(rule):
+    from .test_gpu_tree_rounds import SHAPES
+    for nodes, vocab, depth in SHAPES.values():
+        assert not rule.all_rows(len(nodes), sum(nodes), vocab, depth or DEEPEST)
+
+
 def test_few_rows_are_taken_at_once_and_many_are_not(rule):
     assert rule.all_rows(1, 25, 32000, 6) and rule.all_rows(64, 64 * 12, 32000, 8) and rule.all_rows(64, 64, 128256, 20)
     assert not rule.all_rows(64, 64 * 40, 128256, 8) and not rule.all_rows(20000, 60000, 1000, 8) and not rule.all_rows(1000, 48000, 100, 8)
