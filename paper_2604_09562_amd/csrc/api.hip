@@ -6,6 +6,7 @@
 #include <atomic>
 #include <vector>
 
+#include "kvcache.h"
 #include "prefill.h"
 
 namespace ss {

@@ -1,7 +1,7 @@
 // KV append before the verify step, compaction of an accepted tree path and commit after acceptance
 // (decode KV = prefill KV with the new tokens appended).  One wavefront per (request, new token, KV head); a lane owns head_dim/64
 // consecutive elements of the key and of the value.
-#include "common.h"
+#include "kvcache.h"
 
 #include <type_traits>
 
