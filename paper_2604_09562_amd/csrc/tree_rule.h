@@ -7,11 +7,15 @@
 // behind 300 | 1000 | 4000 | 10000 tokens 10.2 | 14.4 | 30 | 59 (10 | 14 | 30 | 62); 16 requests behind 300 | 4000 20 | 76 (21 | 77); 16 of 64 nodes behind 4000 151 (153); e4m3 with 8
 // query heads, one of 25 nodes behind 10000 87 (88), 16 behind 4000 163 (174); 64-wide heads, 16 of 64 nodes behind 10000 94 (95).
 //
-// The other kernel: what a call costs it without keys, as soon as tiles are cut 6 more (openings, partial results and their merge), and steps of 32 keys for 256 rows: of bf16 1.06, of
-// e4m3 1.27, of 64-wide heads 0.6 to each compute unit, three quarters of that where a tile has 128 rows or less.
+// The other kernel: what a call costs it without keys, as soon as tiles are cut 6 more (openings, partial results and their merge), and steps of 32 keys for 256 rows: of bf16 1.0, of
+// e4m3 1.25 (measured where all compute units are busy: 1.06 and 1.27), of 64-wide heads 0.6 to each compute unit, three quarters of that where a tile has 128 rows or less; of those
+// that the bound of the lengths gives, six tenths.
 //
 // Of 282 calls of 1 .. 64 requests with 6 .. 150 nodes behind up to 30000 tokens (lengths from half of the bound on; 32 heads over 8 of 128 in bf16, 64 over 8 in e4m3, 16 over 2 of
-// 64 in bf16) the rule takes the fastest form that was measured, or one within 15 %, in 274, and 2 % more time than the fastest in the mean.
+// 64 in bf16) the rule takes the fastest form, or one within 15 %, in 274, and 1.8 % more time than the fastest in the mean (profiles/tree_attention_forms.txt has them all).
+//
+// A table wider than the lengths makes calls look longer than they are.  25 nodes behind 300 tokens with 21 | 64 | 256 | 2048 columns: 10.1 | 12.8 | 13.9 | 18.5 us, 16 requests of
+// them 19 | 19 | 25 | 25; the fp32 call of four, 64 | 256 columns, 12.6 | 24.4; long calls are level.
 #pragma once
 
 #include <stdint.h>
@@ -62,8 +66,8 @@ inline TreeUnitChoice tree_unit_rule(int batch, int num_kv_heads, int64_t rows, 
 // The same choice for calls in fp32 (attn_tree_unit_f32.hip): tiles that are taken side by side, 0 for the other kernel, whose tiles have 64 rows that share its steps of 64 keys.
 // Both are bound by the fp32 matrix rate where they are large.  Short calls: 7 us, and 3.15 us a round of 256 keys (64-wide heads: two requests of 25 nodes behind 0 | 300 | 1000 |
 // 4000 | 10000 tokens 8.6 | 11.0 | 20 | 57 | 134) or 3.4 of 128 (128-wide: 7.8 | 17.4 | 36 | 114 | 271), once for every workgroup to a compute unit; the other kernel on the same 17 |
-// 24.5 | 23 | 28 | 39 and 23.5 | 38 | 35 | 67 | 142, sixteen of 64 nodes behind 300 36 | 90 (here 22.5 | 128).  Of 293 calls of 2 .. 64 requests with 6 .. 150 nodes behind up to 10000
-// tokens of one length (three types, both widths) the choice is within 15 % of the faster in 279, and 2.5 % above it in the mean.
+// 24.5 | 23 | 28 | 39 and 23.5 | 38 | 35 | 67 | 142, sixteen of 64 nodes behind 300 36 | 90 (here 22.5 | 128).  Of 373 calls of 1 .. 64 requests with 6 .. 150 nodes behind up to 10000
+// tokens of one length (three types, both widths) the choice is within 15 % of the faster in 358, and 1.9 % above it in the mean.
 inline int32_t tree_unit_f32_rule(int batch, int num_kv_heads, int64_t rows, int64_t max_keys, int head_dim, int cus)
 {
     const int64_t each = (rows + kTreeUnitRowsF32 - 1) / kTreeUnitRowsF32, wgs = each * batch * num_kv_heads;
